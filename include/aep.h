@@ -62,7 +62,8 @@ typedef enum { AEP_POLICY_MTFS = 0, AEP_POLICY_FLFS = 1, AEP_POLICY_DEFRAG = 2 }
 
 typedef struct {
   int32_t n_layers;    /* MoE layers (blocks) whose queues live in this context */
-  int32_t n_experts;   /* routed experts per layer, E (routing needs E <= 64)   */
+  int32_t n_experts;   /* routed experts per layer, E (routing needs E <= 64, or */
+                       /* E <= 512 with a layer's own router: aep_set_router)   */
   int32_t n_shared;    /* shared experts per layer (see every token, weight 1)  */
   int32_t d_model;     /* d: multiple of 64                                      */
   int32_t d_ffn;       /* f: multiple of 64                                      */
@@ -174,6 +175,56 @@ aep_status aep_set_expert_weights(aep_ctx* ctx, int32_t layer, int32_t expert, c
  * exceed max_tokens_per_layer. */
 aep_status aep_route_enqueue(aep_ctx* ctx, int32_t layer, const void* x, const float* logits, int32_t T,
                              int32_t* idx_out, float* w_out, void* stream);
+
+/* ---- Routing by scores: softmax or sigmoid, balance bias, expert groups ----
+ * The rule of layers whose router is more than a top-k of the logits.  For
+ * each token, with l the logits of E = n_experts experts:
+ *   score   s_e = exp(l_e - max l) / sum_i exp(l_i - max l)   (SOFTMAX), or
+ *           s_e = 1 / (1 + exp(-l_e))                         (SIGMOID);
+ *   choice  c_e = s_e + bias_e, compared as binary64 values; without a bias
+ *           experts are compared by their logits, which are ordered alike;
+ *   groups  experts form n_groups groups of E / n_groups consecutive ids.  A
+ *           group is worth the sum of its group_top largest c_e (group_top 1
+ *           without a bias: its largest logit).  The top_groups groups worth
+ *           most keep their experts;
+ *   pick    the top_k largest choices among the kept experts, larger first;
+ *   weight  w_j = scale * s_j, with renorm scale * s_j / (sum of the top_k
+ *           s_j), 0 where that sum is 0.
+ * Equal values go to the lower expert (or group) id.  A logit of -infinity
+ * masks its expert: it comes after every other one of the kept groups, adds
+ * nothing to its group, has score 0 and, if it must be picked, weight 0; a
+ * group with all experts masked comes after every other one.  NaN, +infinity
+ * and a choice that is not finite (a bias that is not) mask as well and are
+ * reported. */
+typedef enum { AEP_SCORE_SOFTMAX = 0, AEP_SCORE_SIGMOID = 1 } aep_score;
+typedef struct {
+  int32_t n_experts;   /* E: 1..512                                              */
+  int32_t top_k;       /* 1..min(E, 16)                                          */
+  int32_t score;       /* aep_score                                              */
+  int32_t n_groups;    /* 1..64, a divisor of E; 1: no groups                    */
+  int32_t top_groups;  /* 1..n_groups, holding at least top_k experts            */
+  int32_t group_top;   /* 1 or 2                                                 */
+  int32_t renorm;      /* 0 or 1                                                 */
+  float scale;         /* finite, > 0                                            */
+} aep_router;
+
+/* Route T tokens without queues (an attention rank that sends its rows to
+ * other GPUs).  Device pointers: logits f32, row t at logits + t * ld_logits
+ * (ld_logits >= E), bias [E] f32 or NULL, idx [T][top_k] int32, w [T][top_k]
+ * f32, flag one int32 or NULL, set to 1 (and never cleared) where a value is
+ * reported as above.  Needs no context.  T == 0 is a no-op.
+ * AEP_ERR_UNSUPPORTED for more than 512 experts or a top_k above 16. */
+aep_status aep_route_topk(const aep_router* r, const float* logits, int64_t ld_logits, const float* bias, int32_t T,
+                          int32_t* idx, float* w, int32_t* flag, void* stream);
+
+/* Give `layer` this router (copied; n_experts and top_k as the context's):
+ * aep_route_enqueue and aep_route_enqueue_ids on it then route by this rule
+ * instead of the context's, and for any number of experts that it allows;
+ * reported values are reported by aep_sync.  bias: device [E] f32, borrowed,
+ * or NULL; its values are read by every later routing call.  r == NULL (bias
+ * NULL) takes the layer back to the context's own rule.  Host state only;
+ * kept when a workspace is bound again. */
+aep_status aep_set_router(aep_ctx* ctx, int32_t layer, const aep_router* r, const float* bias);
 
 /* Receptor for rows routed elsewhere: appends n rows to queue (layer,
  * expert) in order.  Device pointers: rows [n][d] act dtype (referenced,
@@ -397,6 +448,48 @@ aep_status aep_sync(aep_ctx* ctx, void* stream);
  * turns the probe off (the default).  The f32 path records nothing.  The
  * buffer is borrowed and must stay valid while the probe is on. */
 aep_status aep_set_clock_probe(aep_ctx* ctx, uint64_t* d_buf, int32_t n_pairs);
+
+/* ---- Dense product with its epilogue ----
+ *   y = f(s * (x W^T) + b) + r
+ * x [m][k], W [n][k], y and r [m][n]; s per output channel (FP8 weights), b a
+ * bias per output channel, f an activation, r a residual.  Sums and the
+ * epilogue are f32, y is rounded once.  With f32 output and few channels this
+ * makes the gate logits that aep_route_enqueue and aep_route_topk take; with a
+ * residual, the projection that closes an attention block.
+ * Activations: RELU max(v, 0); SILU v / (1 + e^-v); GELU v (1 + erf(v /
+ * sqrt 2)) / 2; GELU_TANH v / (1 + e^-2u), u = sqrt(2 / pi) (v + 0.044715 v^3),
+ * which is its usual form with tanh(u). */
+typedef enum {
+  AEP_FN_NONE = 0, AEP_FN_RELU = 1, AEP_FN_SILU = 2, AEP_FN_GELU = 3, AEP_FN_GELU_TANH = 4
+} aep_fn;
+typedef struct {
+  int32_t m, n, k;       /* m >= 0; n, k >= 1                                      */
+  int32_t x_dtype;       /* aep_dtype: F32 or BF16                                 */
+  int32_t w_dtype;       /* F32 (with F32 x), BF16 or FP8_E4M3 (with BF16 x)       */
+  int32_t y_dtype;       /* F32, or BF16 (with BF16 x)                             */
+  int32_t bias_dtype;    /* F32 or BF16 (ignored without a bias)                   */
+  int32_t res_dtype;     /* F32 or BF16 (ignored without a residual)               */
+  int32_t fn;            /* aep_fn                                                 */
+  int64_t ldx, ldw;      /* elements from one row to the next, >= k                */
+  int64_t ldy, ldr;      /* >= n (ldr ignored without a residual)                  */
+} aep_linear_desc;
+
+/* Bytes of device scratch with which aep_linear is fastest for this product
+ * (host only; 0 for many). */
+aep_status aep_linear_workspace(const aep_linear_desc* l, size_t* bytes);
+
+/* Run it.  Device pointers: x, w, y as described, aligned to their elements
+ * (rows of 16-byte aligned x and w, as rows of a multiple of 8 elements, 16
+ * for FP8, in an aligned matrix are, take the fast loads); scale [n] bf16 for
+ * FP8 weights and NULL for others; bias [n] or NULL; residual or NULL.  y may
+ * be the residual itself (same type and row stride); apart from that it must
+ * not overlap any input.  d_ws: 16-byte aligned scratch of ws_bytes, or NULL:
+ * the product then runs without it where less than aep_linear_workspace is
+ * given.  Nothing in d_ws is kept from call to call, and calls that may
+ * overlap on the GPU need one each.  Needs no context.  Results do not depend
+ * on other calls, and equal calls give equal bits.  m == 0 is a no-op. */
+aep_status aep_linear(const aep_linear_desc* l, const void* x, const void* w, const void* scale, const void* bias,
+                      const void* residual, void* y, void* d_ws, size_t ws_bytes, void* stream);
 
 /* Utility: decode n OCP e4m3fn codes (device) to bf16 (device); exact. */
 aep_status aep_fp8_e4m3_to_bf16(const uint8_t* codes, uint16_t* out, int64_t n, void* stream);

@@ -7,5 +7,6 @@ this package only marshals torch tensors and streams into that ABI.
 
 from ._lib import AEPError, LIB_PATH  # noqa: F401
 from .context import BatchView, Context, fp8_e4m3_to_bf16  # noqa: F401
+from .ops import Linear, Router, linear, route  # noqa: F401
 
-__all__ = ["Context", "BatchView", "AEPError", "fp8_e4m3_to_bf16", "LIB_PATH"]
+__all__ = ["Context", "BatchView", "AEPError", "Linear", "Router", "fp8_e4m3_to_bf16", "linear", "route", "LIB_PATH"]

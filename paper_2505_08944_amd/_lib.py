@@ -19,6 +19,8 @@ AEP_OK, AEP_ERR_INVALID_ARG, AEP_ERR_CAPACITY, AEP_ERR_EMPTY, AEP_ERR_STATE, AEP
     AEP_ERR_UNSUPPORTED = range(7)
 AEP_F32, AEP_BF16, AEP_FP8_E4M3 = range(3)
 AEP_POLICY_MTFS, AEP_POLICY_FLFS, AEP_POLICY_DEFRAG = range(3)
+AEP_SCORE_SOFTMAX, AEP_SCORE_SIGMOID = range(2)
+AEP_FN_NONE, AEP_FN_RELU, AEP_FN_SILU, AEP_FN_GELU, AEP_FN_GELU_TANH = range(5)
 AEP_STATIC_WORKSPACE_BYTES = 96 << 20   # include/aep.h
 
 STATUS_NAMES = {0: "AEP_OK", 1: "AEP_ERR_INVALID_ARG", 2: "AEP_ERR_CAPACITY", 3: "AEP_ERR_EMPTY",
@@ -44,6 +46,17 @@ class Batch(ctypes.Structure):
                 ("counts", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("row_token", ctypes.c_void_p),
                 ("row_weight", ctypes.c_void_p), ("token_pos", ctypes.c_void_p),
                 ("token_weight", ctypes.c_void_p)]
+
+
+class RouterDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_experts", "top_k", "score", "n_groups", "top_groups", "group_top",
+                                              "renorm")] + [("scale", ctypes.c_float)]
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("m", "n", "k", "x_dtype", "w_dtype", "y_dtype", "bias_dtype",
+                                              "res_dtype", "fn")] + \
+               [(n, ctypes.c_int64) for n in ("ldx", "ldw", "ldy", "ldr")]
 
 
 class SimConfig(ctypes.Structure):
@@ -97,6 +110,10 @@ _SIG = {
     "aep_rebatch_expert": (ctypes.c_int, [_P, _I32, _I32, ctypes.POINTER(Batch), _P]),
     "aep_pool_accumulate": (ctypes.c_int, [_P, ctypes.POINTER(Batch), _P, _P]),
     "aep_pool_release": (ctypes.c_int, [_P, _I32, _P, _P, _P]),
+    "aep_route_topk": (ctypes.c_int, [_P, _P, _I64, _P, _I32, _P, _P, _P, _P]),
+    "aep_set_router": (ctypes.c_int, [_P, _I32, _P, _P]),
+    "aep_linear_workspace": (ctypes.c_int, [_P, _P]),
+    "aep_linear": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "aep_sched_pick": (ctypes.c_int, [_P, _I32, _I32, _I32, ctypes.c_double, _I32, ctypes.POINTER(_I32),
                                       ctypes.POINTER(_I32)]),
     "aep_sim_run": (ctypes.c_int, [ctypes.POINTER(SimConfig), ctypes.POINTER(SimTrace),

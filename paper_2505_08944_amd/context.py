@@ -15,6 +15,7 @@ import numpy as np
 import torch
 
 from . import _lib as L
+from .ops import Router
 
 _ACT = {"f32": (L.AEP_F32, torch.float32), "bf16": (L.AEP_BF16, torch.bfloat16)}
 _WDT = {"f32": L.AEP_F32, "bf16": L.AEP_BF16, "fp8": L.AEP_FP8_E4M3}
@@ -123,6 +124,7 @@ class Context:
                     "aep_bind_workspace")
         self.workspace_need = nbytes.value
         self._frag_refs: Dict[int, List[torch.Tensor]] = {l: [] for l in range(n_layers)}
+        self._bias_refs: Dict[int, Optional[torch.Tensor]] = {}
         self._w_refs: Dict[Tuple[int, int], Tuple[torch.Tensor, ...]] = {}
 
     def __del__(self):
@@ -153,6 +155,18 @@ class Context:
         self._w_refs[(layer, expert)] = (gate, up, down, scale_gate_up, scale_down)
 
     # ------------------------------------------------------------- receptor
+    def set_router(self, layer: int, router: Optional[Router], bias: Optional[torch.Tensor] = None) -> None:
+        """Route this layer's fragments by ``router`` (an ``aep.Router``), its
+        choices with bias [E] float32 (kept, not copied); None: by the
+        context's own rule again."""
+        if bias is not None:
+            _need(bias, "bias", torch.float32, (self.n_experts,))
+            if bias.device != self.device:
+                raise ValueError(f"bias must be on {self.device}")
+        L.check(self.lib.aep_set_router(self.h, layer, None if router is None else ctypes.byref(router.desc),
+                                        _ptr(bias)), "aep_set_router")
+        self._bias_refs[layer] = bias
+
     def route_enqueue(self, layer: int, x: torch.Tensor, logits: torch.Tensor,
                       routing_out: bool = False) -> Optional[Tuple[torch.Tensor, torch.Tensor]]:
         T = x.shape[0]

@@ -188,6 +188,44 @@ hipError_t launch_ffn(int stage, int act_dtype, int w_dtype, const GroupDesc* gr
                       unsigned long long* clk, int clk_n, hipStream_t s);
 hipError_t launch_combine(int act_dtype, const void* y, int64_t N, int n_tokens, int S, int k,
                           const int32_t* pos, const float* posw, void* out, int d, hipStream_t s);
+// Routing by scores (aep_router, checked).
+constexpr int kMaxScoredExperts = 512;
+constexpr int kMaxScoredTopK = 16;
+constexpr int kMaxRouteGroups = 64;
+struct RouterArgs {
+  int E, k, sigmoid, n_groups, top_groups, group_top, renorm;
+  float scale;
+};
+// Routes T tokens: idx, w [T][k], and a second copy if idx2 / w2 are not null.
+// flag (may be null) gets kErrNonFinite.
+hipError_t launch_route_scored(const float* logits, int64_t ld, const float* bias, int T, const RouterArgs& r,
+                               int32_t* idx, float* w, int32_t* idx2, float* w2, int32_t* flag, hipStream_t s);
+// Appends them to the queues; blockcnt [E][ceil(T / kRouteTokens)] is scratch,
+// the rest as in launch_append.
+hipError_t launch_append_scored(const int32_t* r_idx, const float* r_w, int32_t* r_rank, int32_t* blockcnt, int T, int E,
+                                int k, const char* x, int64_t row_bytes, int32_t token_base, const int32_t* depth_cur,
+                                int32_t* depth_nxt, QEntry* q, int64_t q_stride, const void** tok_row,
+                                const int32_t* token_ids, int n_ids, int32_t* live, int32_t* pend, int32_t* err,
+                                hipStream_t s);
+
+// Element types and activations as in aep.h (aep_dtype, aep_fn).
+constexpr int kF32 = 0, kBF16 = 1, kFP8 = 2;
+constexpr int kFnNone = 0, kFnRelu = 1, kFnSilu = 2, kFnGelu = 3, kFnGeluTanh = 4;
+
+// A checked dense product.  aligned: rows of x and w start at 16 bytes and
+// end there (k a multiple of what 16 bytes hold), vec_*: four
+// consecutive columns of a row, from a multiple of four on, may be read or
+// written at once.
+struct LinearArgs {
+  int m, n, k;
+  int x_dtype, w_dtype, y_dtype, bias_dtype, res_dtype, fn;
+  int64_t ldx, ldw, ldy, ldr;
+  const void *x, *w, *scale, *bias, *res;
+  void* y;
+  bool aligned, vec_scale, vec_bias, vec_res, vec_y;
+};
+hipError_t launch_linear(const LinearArgs& p, hipStream_t s);
+
 hipError_t launch_fp8_to_bf16(const uint8_t* codes, uint16_t* out, int64_t n, hipStream_t s);
 
 }  // namespace aep

@@ -12,8 +12,7 @@
 #include <new>
 #include <vector>
 
-#include "aep.h"
-#include "aep_internal.h"
+#include "ops.h"
 
 using namespace aep;
 
@@ -26,6 +25,9 @@ struct LayerState {
   bool pool = false;           // fed by aep_route_enqueue_ids (token-pool mode)
   int cur = 0;                 // current half of the depth ping-pong
   std::vector<uint8_t> have_w; // weights registered, per group
+  bool scored = false;         // routed by its own router (aep_set_router)
+  aep_router router{};
+  const float* router_bias = nullptr;
 
   void clear() {
     tokens = 0;
@@ -396,7 +398,7 @@ static aep_status route_common(Ctx* c, int32_t layer, const void* x, const float
   if (T == 0) return AEP_OK;
   if (!x || !logits) return AEP_ERR_INVALID_ARG;
   const int E = c->cfg.n_experts, k = c->cfg.top_k;
-  if (E > kMaxRouteExperts) return AEP_ERR_UNSUPPORTED;
+  if (!L.scored && E > kMaxRouteExperts) return AEP_ERR_UNSUPPORTED;
   int64_t ub = 0;
   for (int e = 0; e < E; ++e) ub = std::max(ub, L.bound[e]);
   if (ub + T > c->tmax() || L.rows + (int64_t)T * k > c->row_cap()) return AEP_ERR_CAPACITY;
@@ -408,7 +410,16 @@ static aep_status route_common(Ctx* c, int32_t layer, const void* x, const float
   int32_t* live = want_pool ? c->live(layer) : nullptr;
   int32_t* pend = want_pool ? c->pend(layer) : nullptr;
   int32_t *cur = c->depth(layer, L.cur), *nxt = c->depth(layer, L.cur ^ 1);
-  if (T <= kFusedTokens) {
+  if (L.scored) {
+    int32_t* ridx = c->at<int32_t>(c->off_ridx);
+    float* rw = c->at<float>(c->off_rw);
+    if (launch_route_scored(logits, E, L.router_bias, T, router_args(L.router), ridx, rw, idx_out, w_out, c->err(),
+                            s) != hipSuccess ||
+        launch_append_scored(ridx, rw, c->at<int32_t>(c->off_rrank), c->at<int32_t>(c->off_blockcnt), T, E, k, rows,
+                             row_bytes, base, cur, nxt, c->q(layer), c->tmax(), c->tokrow(layer), token_ids,
+                             (int)c->tmax(), live, pend, c->err(), s) != hipSuccess)
+      return AEP_ERR_DEVICE;
+  } else if (T <= kFusedTokens) {
     if (launch_route_append(logits, T, E, k, c->cfg.renorm, idx_out, w_out, rows, row_bytes, base, cur, nxt,
                             c->q(layer), c->tmax(), c->tokrow(layer), token_ids, (int)c->tmax(), live, pend, c->err(),
                             s) != hipSuccess)
@@ -430,6 +441,26 @@ static aep_status route_common(Ctx* c, int32_t layer, const void* x, const float
   L.pool = want_pool;
   L.rows += (int64_t)T * k;
   for (int e = 0; e < E; ++e) L.bound[e] += T;
+  return AEP_OK;
+}
+
+aep_status aep_set_router(aep_ctx* ctx, int32_t layer, const aep_router* r, const float* bias) {
+  Ctx* c = as_ctx(ctx);
+  if (!c || layer < 0 || layer >= c->cfg.n_layers) return AEP_ERR_INVALID_ARG;
+  LayerState& L = c->layers[layer];
+  if (!r) {
+    if (bias) return AEP_ERR_INVALID_ARG;
+    L.scored = false;
+    L.router_bias = nullptr;
+    return AEP_OK;
+  }
+  const aep_status st = check_router(r);
+  if (st != AEP_OK) return st;
+  if (r->n_experts != c->cfg.n_experts || r->top_k != c->cfg.top_k) return AEP_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(bias) & 3) return AEP_ERR_INVALID_ARG;
+  L.scored = true;
+  L.router = *r;
+  L.router_bias = bias;
   return AEP_OK;
 }
 

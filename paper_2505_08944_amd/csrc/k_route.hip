@@ -34,6 +34,7 @@
 #include <limits.h>
 
 #include "aep_internal.h"
+#include "route_token_id.h"
 
 namespace aep {
 
@@ -217,24 +218,6 @@ __global__ __launch_bounds__(kRouteThreads) void route_count_kernel(
   __threadfence();
   scan_counts(blockcnt, (int)gridDim.x, E, depth_cur, depth_nxt);
   if (tid == 0) *done = 0;  // ready for the next launch
-}
-
-// The layer-local id of token t of a fragment: token_base + t, or the
-// caller's id, whose pool entry lane 0 claims (an id still claimed, or out of
-// range, is an error; the row is filed under a clamped id).
-__device__ __forceinline__ int token_id(int t, int g, int k, int token_base, const int32_t* __restrict__ token_ids,
-                                        int n_ids, int32_t* __restrict__ live, int32_t* __restrict__ pend,
-                                        int32_t* __restrict__ err) {
-  if (!token_ids) return token_base + t;
-  int tok = token_ids[t];
-  if (tok < 0 || tok >= n_ids) {
-    if (g == 0) atomicOr(err, kErrTokenRange);
-    tok = tok < 0 ? 0 : n_ids - 1;
-  } else if (g == 0 && atomicExch(&live[tok], 1) != 0) {
-    atomicOr(err, kErrCollision);
-  }
-  if (g == 0) pend[tok] = k;
-  return tok;
 }
 
 // A whole fragment of at most TOK tokens in one workgroup: route, rank, write

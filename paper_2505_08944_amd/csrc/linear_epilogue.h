@@ -1,0 +1,97 @@
+// The epilogue of the dense product, shared by its kernels.
+#pragma once
+
+#include "aep_device.h"
+#include "aep_internal.h"
+
+namespace aep {
+
+// Four consecutive values of a bf16 or f32 row from column c on; vec: they may
+// be read at once (16 or 8 byte aligned), else only the first n of them are.
+__device__ __forceinline__ float4 load4(const void* p, int dtype, int64_t at, int n, bool vec) {
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (dtype == kF32) {
+    const float* q = reinterpret_cast<const float*>(p) + at;
+    if (vec && n >= 4) return *reinterpret_cast<const float4*>(q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) v[i] = q[i];
+  } else {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + at;
+    if (vec && n >= 4) {
+      const uint2 w = *reinterpret_cast<const uint2*>(q);
+      return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) v[i] = bf16_lo(q[i]);
+  }
+  return make_float4(v[0], v[1], v[2], v[3]);
+}
+
+// f32 -> bf16, to nearest even; NaN stays NaN.
+__device__ __forceinline__ uint32_t bf16_bits(float f) { return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)f); }
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef __bf16 v2 __attribute__((ext_vector_type(2)));
+  v2 v;
+  v[0] = (__bf16)a;
+  v[1] = (__bf16)b;
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+__device__ __forceinline__ void store4(void* p, int dtype, int64_t at, int n, bool vec, const float4 v) {
+  const float a[4] = {v.x, v.y, v.z, v.w};
+  if (dtype == kF32) {
+    float* q = reinterpret_cast<float*>(p) + at;
+    if (vec && n >= 4) {
+      *reinterpret_cast<float4*>(q) = v;
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) q[i] = a[i];
+  } else {
+    uint16_t* q = reinterpret_cast<uint16_t*>(p) + at;
+    if (vec && n >= 4) {
+      *reinterpret_cast<uint2*>(q) = make_uint2(bf16_pair(a[0], a[1]), bf16_pair(a[2], a[3]));
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (i < n) q[i] = (uint16_t)bf16_bits(a[i]);
+  }
+}
+
+// v / (1 + e^-u) for f32 results: to within a few units of 2^-24.
+__device__ __forceinline__ float gate(float v, float u) { return v / (1.f + expf(-u)); }
+
+// The activation, accurate enough for an f32 result.  GELU through erfc, which
+// keeps its relative accuracy where 1 + erf cancels; GELU_TANH as v / (1 +
+// e^-2u), which does the same.
+__device__ __forceinline__ float linear_fn(int fn, float v) {
+  switch (fn) {
+    case kFnRelu: return v > 0.f ? v : v == v ? 0.f : v;  // NaN stays NaN
+    case kFnSilu: return gate(v, v);
+    case kFnGelu: return 0.5f * v * erfcf(v * -0.70710678118654752f);
+    case kFnGeluTanh: return gate(v, 2.f * 0.79788456080286536f * (v + 0.044715f * v * v * v));
+    default: return v;
+  }
+}
+
+// Four columns [c, c + 4) of row m: bias, activation, residual, one rounding.
+// left: columns of the matrix from c on (may exceed 4).
+__device__ __forceinline__ void linear_out4(const LinearArgs& p, int64_t m, int c, int left, float4 s) {
+  const int64_t at = m * p.ldr + c;
+  float4 b = make_float4(0.f, 0.f, 0.f, 0.f), r = b;
+  if (p.scale) {
+    const float4 q = load4(p.scale, kBF16, c, left, p.vec_scale);
+    s = make_float4(s.x * q.x, s.y * q.y, s.z * q.z, s.w * q.w);
+  }
+  if (p.bias) b = load4(p.bias, p.bias_dtype, c, left, p.vec_bias);
+  if (p.res) r = load4(p.res, p.res_dtype, at, left, p.vec_res);
+  s = make_float4(linear_fn(p.fn, s.x + b.x) + r.x, linear_fn(p.fn, s.y + b.y) + r.y, linear_fn(p.fn, s.z + b.z) + r.z,
+                  linear_fn(p.fn, s.w + b.w) + r.w);
+  store4(p.y, p.y_dtype, m * p.ldy + c, left, p.vec_y, s);
+}
+
+}  // namespace aep

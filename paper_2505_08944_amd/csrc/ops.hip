@@ -1,0 +1,122 @@
+// Host side of the calls that need no context: the dense product and routing
+// without queues.
+#include <cmath>
+
+#include "ops.h"
+
+using namespace aep;
+
+namespace aep {
+
+aep_status check_router(const aep_router* r) {
+  if (!r) return AEP_ERR_INVALID_ARG;
+  if (r->n_experts < 1 || r->top_k < 1 || r->top_k > r->n_experts) return AEP_ERR_INVALID_ARG;
+  if (r->score != AEP_SCORE_SOFTMAX && r->score != AEP_SCORE_SIGMOID) return AEP_ERR_INVALID_ARG;
+  if (r->n_groups < 1 || r->n_groups > kMaxRouteGroups || r->n_experts % r->n_groups) return AEP_ERR_INVALID_ARG;
+  if (r->top_groups < 1 || r->top_groups > r->n_groups) return AEP_ERR_INVALID_ARG;
+  if ((int64_t)r->top_groups * (r->n_experts / r->n_groups) < r->top_k) return AEP_ERR_INVALID_ARG;
+  if (r->group_top != 1 && r->group_top != 2) return AEP_ERR_INVALID_ARG;
+  if (r->renorm != 0 && r->renorm != 1) return AEP_ERR_INVALID_ARG;
+  if (!std::isfinite(r->scale) || !(r->scale > 0.f)) return AEP_ERR_INVALID_ARG;
+  if (r->n_experts > kMaxScoredExperts || r->top_k > kMaxScoredTopK) return AEP_ERR_UNSUPPORTED;
+  return AEP_OK;
+}
+
+RouterArgs router_args(const aep_router& r) {
+  return RouterArgs{r.n_experts, r.top_k, r.score == AEP_SCORE_SIGMOID, r.n_groups, r.top_groups, r.group_top, r.renorm,
+                    r.scale};
+}
+
+}  // namespace aep
+
+namespace {
+
+bool off(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+int esize(int32_t t) { return t == AEP_F32 ? 4 : t == AEP_BF16 ? 2 : 1; }
+
+aep_status check_linear(const aep_linear_desc* l) {
+  if (!l || l->m < 0 || l->n < 1 || l->k < 1) return AEP_ERR_INVALID_ARG;
+  const int32_t types[] = {l->x_dtype, l->w_dtype, l->y_dtype, l->bias_dtype, l->res_dtype};
+  for (int32_t t : types)
+    if (t < AEP_F32 || t > AEP_FP8_E4M3) return AEP_ERR_INVALID_ARG;
+  if (l->fn < AEP_FN_NONE || l->fn > AEP_FN_GELU_TANH) return AEP_ERR_INVALID_ARG;
+  if (l->ldx < l->k || l->ldw < l->k || l->ldy < l->n) return AEP_ERR_INVALID_ARG;
+  const bool f32 = l->x_dtype == AEP_F32 && l->w_dtype == AEP_F32 && l->y_dtype == AEP_F32;
+  const bool bf = l->x_dtype == AEP_BF16 && (l->w_dtype == AEP_BF16 || l->w_dtype == AEP_FP8_E4M3) &&
+                  (l->y_dtype == AEP_BF16 || l->y_dtype == AEP_F32);
+  if (!f32 && !bf) return AEP_ERR_UNSUPPORTED;
+  if (l->bias_dtype == AEP_FP8_E4M3 || l->res_dtype == AEP_FP8_E4M3) return AEP_ERR_UNSUPPORTED;
+  return AEP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+aep_status aep_route_topk(const aep_router* r, const float* logits, int64_t ld_logits, const float* bias, int32_t T,
+                          int32_t* idx, float* w, int32_t* flag, void* stream) {
+  const aep_status st = check_router(r);
+  if (st != AEP_OK) return st;
+  if (T < 0 || ld_logits < r->n_experts) return AEP_ERR_INVALID_ARG;
+  if (T == 0) return AEP_OK;
+  if (!logits || !idx || !w) return AEP_ERR_INVALID_ARG;
+  if (off(logits, 4) || off(bias, 4) || off(idx, 4) || off(w, 4) || off(flag, 4)) return AEP_ERR_INVALID_ARG;
+  return launch_route_scored(logits, ld_logits, bias, T, router_args(*r), idx, w, nullptr, nullptr, flag,
+                             reinterpret_cast<hipStream_t>(stream)) == hipSuccess
+             ? AEP_OK
+             : AEP_ERR_DEVICE;
+}
+
+aep_status aep_linear_workspace(const aep_linear_desc* l, size_t* bytes) {
+  const aep_status st = check_linear(l);
+  if (st != AEP_OK) return st;
+  if (!bytes) return AEP_ERR_INVALID_ARG;
+  *bytes = 0;
+  return AEP_OK;
+}
+
+aep_status aep_linear(const aep_linear_desc* l, const void* x, const void* w, const void* scale, const void* bias,
+                      const void* residual, void* y, void* d_ws, size_t ws_bytes, void* stream) {
+  const aep_status st = check_linear(l);
+  if (st != AEP_OK) return st;
+  if (residual && l->ldr < l->n) return AEP_ERR_INVALID_ARG;
+  if (l->m == 0) return AEP_OK;
+  if (!x || !w || !y) return AEP_ERR_INVALID_ARG;
+  if ((l->w_dtype == AEP_FP8_E4M3) != (scale != nullptr)) return AEP_ERR_INVALID_ARG;
+  const int xs = esize(l->x_dtype), ws = esize(l->w_dtype), ys = esize(l->y_dtype), bs = esize(l->bias_dtype),
+            rs = esize(l->res_dtype);
+  if (off(x, xs) || off(w, ws) || off(y, ys) || off(scale, 2) || off(bias, bs) || (residual && off(residual, rs)) ||
+      off(d_ws, 16))
+    return AEP_ERR_INVALID_ARG;
+  // y may be the residual, element for element, and nothing else of it
+  if (residual == y && (l->res_dtype != l->y_dtype || (l->ldr != l->ldy && l->m > 1))) return AEP_ERR_INVALID_ARG;
+  LinearArgs p{};
+  p.m = l->m;
+  p.n = l->n;
+  p.k = l->k;
+  p.x_dtype = l->x_dtype;
+  p.w_dtype = l->w_dtype;
+  p.y_dtype = l->y_dtype;
+  p.bias_dtype = l->bias_dtype;
+  p.res_dtype = l->res_dtype;
+  p.fn = l->fn;
+  p.ldx = l->ldx;
+  p.ldw = l->ldw;
+  p.ldy = l->ldy;
+  p.ldr = l->ldr;
+  p.x = x;
+  p.w = w;
+  p.scale = scale;
+  p.bias = bias;
+  p.res = residual;
+  p.y = y;
+  p.aligned = !off(x, 16) && !off(w, 16) && (l->ldx * xs) % 16 == 0 && (l->ldw * ws) % 16 == 0 &&
+              ((int64_t)l->k * xs) % 16 == 0 && ((int64_t)l->k * ws) % 16 == 0;
+  p.vec_scale = !off(scale, 8);
+  p.vec_bias = !off(bias, 4 * bs);
+  p.vec_res = !off(residual, 4 * rs) && l->ldr % 4 == 0;
+  p.vec_y = !off(y, 4 * ys) && l->ldy % 4 == 0;
+  return launch_linear(p, reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? AEP_OK : AEP_ERR_DEVICE;
+}
+
+}  // extern "C"

@@ -1,0 +1,205 @@
+"""The operators in front of the queues that need no context: the dense
+product with its epilogue and routing by scores.
+
+As in ``context``, torch provides memory and the stream, and the work runs in
+libaep.  A call runs on the device of its tensors, on torch's current stream
+there.  Tensors are read on that stream: a caller that uses tensors of another
+stream orders the two, as for any torch operation.  Forward only: results do
+not take part in autograd.
+"""
+
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Tuple
+
+import torch
+
+from . import _lib as L
+
+_CODE = {torch.float32: L.AEP_F32, torch.bfloat16: L.AEP_BF16, torch.float8_e4m3fn: L.AEP_FP8_E4M3,
+         torch.uint8: L.AEP_FP8_E4M3}
+_FN = {"none": L.AEP_FN_NONE, "relu": L.AEP_FN_RELU, "silu": L.AEP_FN_SILU, "gelu": L.AEP_FN_GELU,
+       "gelu_tanh": L.AEP_FN_GELU_TANH}
+_SCORE = {"softmax": L.AEP_SCORE_SOFTMAX, "sigmoid": L.AEP_SCORE_SIGMOID}
+
+
+def _rows(t: torch.Tensor, name: str, dtypes, shape, device) -> None:
+    """A matrix on ``device`` whose rows are contiguous."""
+    if not isinstance(t, torch.Tensor) or t.device != device:
+        raise ValueError(f"{name} must be a tensor on {device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
+    if t.dim() != len(shape) or any(s is not None and a != s for a, s in zip(t.shape, shape)):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    if t.dim() == 2 and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name}: rows must not overlap")
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Elements from one row to the next (a single row has no next one)."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+class _on:
+    """Makes a device the current one for a call, where it is not already."""
+
+    __slots__ = ("guard",)
+
+    def __init__(self, device: torch.device):
+        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+class Linear:
+    """y = f(scale * (x W^T) + bias) + residual (``aep_linear``).
+
+    weight [n, k]: float32 (x float32), bfloat16 or float8_e4m3fn / uint8 codes
+    (x bfloat16), the latter with scale [n] bfloat16; rows may be strided.
+    bias [n] float32 or bfloat16.  activation: none, relu, silu, gelu or
+    gelu_tanh.  out_dtype: x's type (the default) or float32.  The tensors are
+    kept, not copied: values written to them later are used by later calls.
+    """
+
+    def __init__(self, weight: torch.Tensor, *, scale: Optional[torch.Tensor] = None,
+                 bias: Optional[torch.Tensor] = None, activation: str = "none",
+                 out_dtype: Optional[torch.dtype] = None):
+        if not isinstance(weight, torch.Tensor) or not weight.is_cuda:
+            raise ValueError("weight must be a CUDA (HIP) tensor")
+        dev = weight.device
+        _rows(weight, "weight", (torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.uint8), (None, None), dev)
+        n, k = weight.shape
+        if n < 1 or k < 1:
+            raise ValueError(f"weight has shape {tuple(weight.shape)}")
+        fp8 = _CODE[weight.dtype] == L.AEP_FP8_E4M3
+        if fp8 != (scale is not None):
+            raise ValueError("scale goes with fp8 weights, and only with them")
+        for t, name, dtypes in ((scale, "scale", (torch.bfloat16,)),
+                                (bias, "bias", (torch.float32, torch.bfloat16))):
+            if t is not None:
+                _rows(t, name, dtypes, (n,), dev)
+        if activation not in _FN:
+            raise ValueError(f"activation {activation!r}, expected one of {', '.join(_FN)}")
+        self.x_dtype = torch.float32 if weight.dtype == torch.float32 else torch.bfloat16
+        out_dtype = out_dtype or self.x_dtype
+        if out_dtype not in (torch.float32, self.x_dtype):
+            raise ValueError(f"out_dtype {out_dtype}, expected {self.x_dtype} or torch.float32")
+        self.weight, self.scale, self.bias = weight, scale, bias
+        self.activation, self.out_dtype, self.device = activation, out_dtype, dev
+        self.n, self.k = n, k
+        self._lib = L.lib()
+        self._fixed = (n, k, _CODE[self.x_dtype], _CODE[weight.dtype], _CODE[out_dtype],
+                       L.AEP_F32 if bias is None else _CODE[bias.dtype])
+        self._fn = _FN[activation]
+        self._ldw = _ld(weight)
+        self._ws_need = {}  # bytes of scratch by (m, row strides)
+        self._desc = L.LinearDesc()
+        self._at = ctypes.byref(self._desc)
+
+    def __call__(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                 out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x [m, k] -> [m, n].  residual [m, n] float32 or bfloat16; out may be
+        the residual itself, and must not overlap anything else.  Not to be
+        called on one object from two threads at once."""
+        dev = self.device
+        _rows(x, "x", (self.x_dtype,), (None, self.k), dev)
+        m, n = x.shape[0], self.n
+        if residual is not None:
+            _rows(residual, "residual", (torch.float32, torch.bfloat16), (m, n), dev)
+        if out is not None:
+            _rows(out, "out", (self.out_dtype,), (m, n), dev)
+        with _on(dev):
+            if out is None:
+                out = torch.empty((m, n), dtype=self.out_dtype, device=dev)
+            d = self._desc
+            ldx, ldy = _ld(x), _ld(out)
+            (d.n, d.k, d.x_dtype, d.w_dtype, d.y_dtype, d.bias_dtype) = self._fixed
+            d.m, d.fn, d.ldx, d.ldw, d.ldy = m, self._fn, ldx, self._ldw, ldy
+            if residual is not None:
+                d.res_dtype, d.ldr = _CODE[residual.dtype], _ld(residual)
+            else:
+                d.res_dtype, d.ldr = L.AEP_F32, n
+            need = self._ws_need.get((m, ldx))
+            if need is None:
+                b = ctypes.c_size_t()
+                L.check(self._lib.aep_linear_workspace(self._at, ctypes.byref(b)), "aep_linear_workspace")
+                need = self._ws_need[(m, ldx)] = b.value
+            ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+            L.check(self._lib.aep_linear(
+                self._at, x.data_ptr(), self.weight.data_ptr(), None if self.scale is None else self.scale.data_ptr(),
+                None if self.bias is None else self.bias.data_ptr(),
+                None if residual is None else residual.data_ptr(), out.data_ptr(),
+                None if ws is None else ws.data_ptr(), need,
+                torch.cuda.current_stream().cuda_stream), "aep_linear")
+        return out
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, *, scale: Optional[torch.Tensor] = None,
+           bias: Optional[torch.Tensor] = None, activation: str = "none", residual: Optional[torch.Tensor] = None,
+           out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """``Linear`` for one call."""
+    return Linear(weight, scale=scale, bias=bias, activation=activation, out_dtype=out_dtype)(x, residual, out)
+
+
+class Router:
+    """How a layer picks its experts (``aep_router``): softmax or sigmoid
+    scores; experts in n_groups groups of consecutive ids, of which the
+    top_groups best stay, each worth the sum of its group_top (1 or 2) best
+    choices; the top_k best choices (score + bias); weights from the scores,
+    renormalised over the chosen or not, times scale."""
+
+    def __init__(self, n_experts: int, top_k: int, *, score: str = "softmax", n_groups: int = 1, top_groups: int = 1,
+                 group_top: int = 1, renorm: bool = True, scale: float = 1.0):
+        if score not in _SCORE:
+            raise ValueError(f"score {score!r}, expected one of {', '.join(_SCORE)}")
+        self.n_experts, self.top_k, self.score = n_experts, top_k, score
+        self.n_groups, self.top_groups, self.group_top = n_groups, top_groups, group_top
+        self.renorm, self.scale = bool(renorm), float(scale)
+        self.desc = L.RouterDesc(n_experts, top_k, _SCORE[score], n_groups, top_groups, group_top, int(self.renorm),
+                                 self.scale)
+        self._at = ctypes.byref(self.desc)
+        self._lib = L.lib()
+        # the library checks the values; routing no tokens does nothing else
+        L.check(self._lib.aep_route_topk(self._at, None, max(n_experts, 0), None, 0, None, None, None, None),
+                "aep_route_topk")
+
+
+def route(router: Router, logits: torch.Tensor, bias: Optional[torch.Tensor] = None, *,
+          idx: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None,
+          flag: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Expert ids [T, k] int32 and gate weights [T, k] float32 of logits [T, E]
+    float32 (``aep_route_topk``).  bias [E] float32 is added to the scores for
+    the choice only.  flag: int32 [1], set to 1 where a logit is NaN or +inf
+    (-inf masks an expert) or a bias is not finite."""
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+        raise ValueError("logits must be a CUDA (HIP) tensor")
+    dev = logits.device
+    _rows(logits, "logits", (torch.float32,), (None, router.n_experts), dev)
+    T, k = logits.shape[0], router.top_k
+    if bias is not None:
+        _rows(bias, "bias", (torch.float32,), (router.n_experts,), dev)
+    for t, name, dtype, shape in ((idx, "idx", torch.int32, (T, k)), (weights, "weights", torch.float32, (T, k)),
+                                  (flag, "flag", torch.int32, (1,))):
+        if t is not None:
+            _rows(t, name, (dtype,), shape, dev)
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+    with _on(dev):
+        if idx is None:
+            idx = torch.empty((T, k), dtype=torch.int32, device=dev)
+        if weights is None:
+            weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+        L.check(router._lib.aep_route_topk(
+            router._at, logits.data_ptr(), _ld(logits), None if bias is None else bias.data_ptr(),
+            T, idx.data_ptr(), weights.data_ptr(), None if flag is None else flag.data_ptr(),
+            torch.cuda.current_stream().cuda_stream), "aep_route_topk")
+    return idx, weights
