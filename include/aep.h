@@ -463,7 +463,7 @@ typedef enum {
   AEP_FN_NONE = 0, AEP_FN_RELU = 1, AEP_FN_SILU = 2, AEP_FN_GELU = 3, AEP_FN_GELU_TANH = 4
 } aep_fn;
 typedef struct {
-  int32_t m, n, k;       /* m >= 0; n, k >= 1                                      */
+  int32_t m, n, k;       /* m >= 0; n, k >= 1; none above 2^30, m n at most 2^38   */
   int32_t x_dtype;       /* aep_dtype: F32 or BF16                                 */
   int32_t w_dtype;       /* F32 (with F32 x), BF16 or FP8_E4M3 (with BF16 x)       */
   int32_t y_dtype;       /* F32, or BF16 (with BF16 x)                             */

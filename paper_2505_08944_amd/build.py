@@ -23,7 +23,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libaep.so")
 
 SOURCES = ["api.hip", "k_route.hip", "k_rebatch.hip", "k_ffn.hip", "k_combine.hip", "k_pool.hip", "sched.hip",
-           "k_router.hip", "k_linear.hip", "ops.hip"]
+           "k_router.hip", "k_linear.hip", "k_linear_tiles.hip", "linear_cut.hip", "ops.hip"]
 ARCH = "gfx950"
 CFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

@@ -223,8 +223,10 @@ struct LinearArgs {
   const void *x, *w, *scale, *bias, *res;
   void* y;
   bool aligned, vec_scale, vec_bias, vec_res, vec_y;
+  bool wide;  // bf16 y, and the residual if any: eight columns from a multiple of eight on at once, n a multiple of 8
 };
-hipError_t launch_linear(const LinearArgs& p, hipStream_t s);
+// nwg: workgroups of a persistent launch; scratch may be null with 0 floats.
+hipError_t launch_linear(const LinearArgs& p, int nwg, float* scratch, int64_t scratch_floats, hipStream_t s);
 
 hipError_t launch_fp8_to_bf16(const uint8_t* codes, uint16_t* out, int64_t n, hipStream_t s);
 

@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "linear_epilogue.h"
+#include "linear_tiles.h"
 
 namespace aep {
 
@@ -192,7 +193,16 @@ static hipError_t rows_align(const LinearArgs& p, hipStream_t s) {
   return aligned ? rows_tile<XT, WT, true>(p, s) : rows_tile<XT, WT, false>(p, s);
 }
 
-hipError_t launch_linear(const LinearArgs& p, hipStream_t s) {
+// Tiles need aligned rows, and offsets within a tile that fit 32 bits.
+bool linear_uses_tiles(const LinearArgs& p) {
+  if (p.w_dtype == kF32 || !p.aligned) return false;
+  if (std::max(p.ldx, p.ldw) > (1 << 22)) return false;
+  return p.m > 64 && p.n > 64;
+}
+
+hipError_t launch_linear(const LinearArgs& p, int nwg, float* scratch, int64_t scratch_floats, hipStream_t s) {
+  if (linear_uses_tiles(p))
+    return launch_linear_tiles(p, linear_cut(p.m, p.n, p.k, p.w_dtype == kFP8, nwg, scratch_floats), nwg, scratch, s);
   if (p.w_dtype == kF32) return rows_align<float, float>(p, s);
   if (p.w_dtype == kBF16) return rows_align<uint16_t, uint16_t>(p, s);
   return rows_align<uint16_t, uint8_t>(p, s);

@@ -1,7 +1,11 @@
 // Host side of the calls that need no context: the dense product and routing
 // without queues.
+#include <algorithm>
+#include <atomic>
+#include <climits>
 #include <cmath>
 
+#include "linear_tiles.h"
 #include "ops.h"
 
 using namespace aep;
@@ -46,7 +50,57 @@ aep_status check_linear(const aep_linear_desc* l) {
                   (l->y_dtype == AEP_BF16 || l->y_dtype == AEP_F32);
   if (!f32 && !bf) return AEP_ERR_UNSUPPORTED;
   if (l->bias_dtype == AEP_FP8_E4M3 || l->res_dtype == AEP_FP8_E4M3) return AEP_ERR_UNSUPPORTED;
+  // indices and tile counts are 32-bit (an output of 2^38 values does not fit any GPU)
+  if (std::max({l->m, l->n, l->k}) > 1 << 30 || (int64_t)l->m * l->n > (int64_t)1 << 38) return AEP_ERR_UNSUPPORTED;
   return AEP_OK;
+}
+
+// One workgroup per CU of the current device, a multiple of the 8 XCDs.
+int persistent_workgroups() {
+  constexpr int kDevices = 64;
+  static std::atomic<int> seen[kDevices];  // 0: not asked yet
+  int dev = -1, n = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kDevices) return 256;
+  if ((n = seen[dev].load(std::memory_order_relaxed)) > 0) return n;
+  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 256;
+  n = ffn_grid(n);
+  seen[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+LinearArgs linear_args(const aep_linear_desc& l, const void* x, const void* w, const void* scale, const void* bias,
+                       const void* residual, void* y) {
+  const int xs = esize(l.x_dtype), ws = esize(l.w_dtype), ys = esize(l.y_dtype), bs = esize(l.bias_dtype),
+            rs = esize(l.res_dtype);
+  LinearArgs p{};
+  p.m = l.m;
+  p.n = l.n;
+  p.k = l.k;
+  p.x_dtype = l.x_dtype;
+  p.w_dtype = l.w_dtype;
+  p.y_dtype = l.y_dtype;
+  p.bias_dtype = l.bias_dtype;
+  p.res_dtype = l.res_dtype;
+  p.fn = l.fn;
+  p.ldx = l.ldx;
+  p.ldw = l.ldw;
+  p.ldy = l.ldy;
+  p.ldr = l.ldr;
+  p.x = x;
+  p.w = w;
+  p.scale = scale;
+  p.bias = bias;
+  p.res = residual;
+  p.y = y;
+  p.aligned = !off(x, 16) && !off(w, 16) && (l.ldx * xs) % 16 == 0 && (l.ldw * ws) % 16 == 0 &&
+              ((int64_t)l.k * xs) % 16 == 0 && ((int64_t)l.k * ws) % 16 == 0;
+  p.vec_scale = !off(scale, 8);
+  p.vec_bias = !off(bias, 4 * bs);
+  p.vec_res = !off(residual, 4 * rs) && l.ldr % 4 == 0;
+  p.vec_y = !off(y, 4 * ys) && l.ldy % 4 == 0;
+  p.wide = l.y_dtype == AEP_BF16 && l.n % 8 == 0 && !off(y, 16) && l.ldy % 8 == 0 &&
+           (!residual || (l.res_dtype == AEP_BF16 && !off(residual, 16) && l.ldr % 8 == 0));
+  return p;
 }
 
 }  // namespace
@@ -72,6 +126,11 @@ aep_status aep_linear_workspace(const aep_linear_desc* l, size_t* bytes) {
   if (st != AEP_OK) return st;
   if (!bytes) return AEP_ERR_INVALID_ARG;
   *bytes = 0;
+  if (l->m == 0) return AEP_OK;
+  // as for aligned pointers
+  const LinearArgs p = linear_args(*l, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
+  if (linear_uses_tiles(p))
+    *bytes = (size_t)linear_cut(p.m, p.n, p.k, p.w_dtype == kFP8, persistent_workgroups(), INT64_MAX).floats(p.n) * 4;
   return AEP_OK;
 }
 
@@ -83,40 +142,17 @@ aep_status aep_linear(const aep_linear_desc* l, const void* x, const void* w, co
   if (l->m == 0) return AEP_OK;
   if (!x || !w || !y) return AEP_ERR_INVALID_ARG;
   if ((l->w_dtype == AEP_FP8_E4M3) != (scale != nullptr)) return AEP_ERR_INVALID_ARG;
-  const int xs = esize(l->x_dtype), ws = esize(l->w_dtype), ys = esize(l->y_dtype), bs = esize(l->bias_dtype),
-            rs = esize(l->res_dtype);
-  if (off(x, xs) || off(w, ws) || off(y, ys) || off(scale, 2) || off(bias, bs) || (residual && off(residual, rs)) ||
-      off(d_ws, 16))
+  if (off(x, esize(l->x_dtype)) || off(w, esize(l->w_dtype)) || off(y, esize(l->y_dtype)) || off(scale, 2) ||
+      off(bias, esize(l->bias_dtype)) || off(residual, esize(l->res_dtype)) || off(d_ws, 16))
     return AEP_ERR_INVALID_ARG;
   // y may be the residual, element for element, and nothing else of it
   if (residual == y && (l->res_dtype != l->y_dtype || (l->ldr != l->ldy && l->m > 1))) return AEP_ERR_INVALID_ARG;
-  LinearArgs p{};
-  p.m = l->m;
-  p.n = l->n;
-  p.k = l->k;
-  p.x_dtype = l->x_dtype;
-  p.w_dtype = l->w_dtype;
-  p.y_dtype = l->y_dtype;
-  p.bias_dtype = l->bias_dtype;
-  p.res_dtype = l->res_dtype;
-  p.fn = l->fn;
-  p.ldx = l->ldx;
-  p.ldw = l->ldw;
-  p.ldy = l->ldy;
-  p.ldr = l->ldr;
-  p.x = x;
-  p.w = w;
-  p.scale = scale;
-  p.bias = bias;
-  p.res = residual;
-  p.y = y;
-  p.aligned = !off(x, 16) && !off(w, 16) && (l->ldx * xs) % 16 == 0 && (l->ldw * ws) % 16 == 0 &&
-              ((int64_t)l->k * xs) % 16 == 0 && ((int64_t)l->k * ws) % 16 == 0;
-  p.vec_scale = !off(scale, 8);
-  p.vec_bias = !off(bias, 4 * bs);
-  p.vec_res = !off(residual, 4 * rs) && l->ldr % 4 == 0;
-  p.vec_y = !off(y, 4 * ys) && l->ldy % 4 == 0;
-  return launch_linear(p, reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? AEP_OK : AEP_ERR_DEVICE;
+  const LinearArgs p = linear_args(*l, x, w, scale, bias, residual, y);
+  return launch_linear(p, persistent_workgroups(), reinterpret_cast<float*>(d_ws),
+                       d_ws ? (int64_t)std::min<size_t>(ws_bytes / 4, INT64_MAX / 4) : 0,
+                       reinterpret_cast<hipStream_t>(stream)) == hipSuccess
+             ? AEP_OK
+             : AEP_ERR_DEVICE;
 }
 
 }  // extern "C"

@@ -85,7 +85,8 @@ BAD_LINEARS = [
     (dict(fn=5), 1), (dict(fn=-1), 1), (dict(x_dtype=3), 1), (dict(w_dtype=-1), 1), (dict(y_dtype=9), 1),
     (dict(bias_dtype=4), 1), (dict(res_dtype=-2), 1), (dict(x_dtype=2), 6), (dict(w_dtype=0), 6),
     (dict(x_dtype=0), 6), (dict(x_dtype=0, w_dtype=0), 6), (dict(y_dtype=2), 6), (dict(bias_dtype=2), 6),
-    (dict(res_dtype=2), 6),
+    (dict(res_dtype=2), 6), (dict(m=(1 << 30) + 1), 6), (dict(k=(1 << 30) + 1, ldx=1 << 31, ldw=1 << 31), 6),
+    (dict(m=1 << 20, n=(1 << 18) + 1, ldy=1 << 20, ldr=1 << 20), 6),
 ]
 
 
