@@ -195,18 +195,32 @@ constexpr int kMaxRouteGroups = 64;
 struct RouterArgs {
   int E, k, sigmoid, n_groups, top_groups, group_top, renorm;
   float scale;
+  int inv_per;  // e * inv_per >> 20 is expert e's group
+  int row;      // doubles of a token's LDS row
 };
-// Routes T tokens: idx, w [T][k], and a second copy if idx2 / w2 are not null.
-// flag (may be null) gets kErrNonFinite.
+// Where a routed fragment goes: the queues of a layer (arguments as in
+// launch_append).
+struct AppendArgs {
+  const char* x;
+  int64_t row_bytes;
+  int32_t token_base;
+  const int32_t* depth_cur;
+  int32_t* depth_nxt;
+  QEntry* q;
+  int64_t q_stride;
+  const void** tok_row;
+  const int32_t* token_ids;
+  int n_ids;
+  int32_t *live, *pend, *err;
+};
+// Routes T tokens: idx, w [T][k].  flag (may be null) gets kErrNonFinite.
 hipError_t launch_route_scored(const float* logits, int64_t ld, const float* bias, int T, const RouterArgs& r,
-                               int32_t* idx, float* w, int32_t* idx2, float* w2, int32_t* flag, hipStream_t s);
-// Appends them to the queues; blockcnt [E][ceil(T / kRouteTokens)] is scratch,
-// the rest as in launch_append.
-hipError_t launch_append_scored(const int32_t* r_idx, const float* r_w, int32_t* r_rank, int32_t* blockcnt, int T, int E,
-                                int k, const char* x, int64_t row_bytes, int32_t token_base, const int32_t* depth_cur,
-                                int32_t* depth_nxt, QEntry* q, int64_t q_stride, const void** tok_row,
-                                const int32_t* token_ids, int n_ids, int32_t* live, int32_t* pend, int32_t* err,
-                                hipStream_t s);
+                               int32_t* idx, float* w, int32_t* flag, hipStream_t s);
+// Routes them into the queues.  r_idx, r_w, r_rank [T][k] and blockcnt
+// [E][ceil(T / kRouteTokens)] are scratch, idx_out and w_out may be null.
+hipError_t launch_route_queue(const float* logits, const float* bias, int T, const RouterArgs& r, int32_t* r_idx,
+                              float* r_w, int32_t* r_rank, int32_t* blockcnt, int32_t* idx_out, float* w_out,
+                              const AppendArgs& a, hipStream_t s);
 
 // Element types and activations as in aep.h (aep_dtype, aep_fn).
 constexpr int kF32 = 0, kBF16 = 1, kFP8 = 2;

@@ -411,13 +411,11 @@ static aep_status route_common(Ctx* c, int32_t layer, const void* x, const float
   int32_t* pend = want_pool ? c->pend(layer) : nullptr;
   int32_t *cur = c->depth(layer, L.cur), *nxt = c->depth(layer, L.cur ^ 1);
   if (L.scored) {
-    int32_t* ridx = c->at<int32_t>(c->off_ridx);
-    float* rw = c->at<float>(c->off_rw);
-    if (launch_route_scored(logits, E, L.router_bias, T, router_args(L.router), ridx, rw, idx_out, w_out, c->err(),
-                            s) != hipSuccess ||
-        launch_append_scored(ridx, rw, c->at<int32_t>(c->off_rrank), c->at<int32_t>(c->off_blockcnt), T, E, k, rows,
-                             row_bytes, base, cur, nxt, c->q(layer), c->tmax(), c->tokrow(layer), token_ids,
-                             (int)c->tmax(), live, pend, c->err(), s) != hipSuccess)
+    const AppendArgs a{rows,      row_bytes,       base,      cur,           nxt,  c->q(layer), c->tmax(),
+                       c->tokrow(layer), token_ids, (int)c->tmax(), live, pend,        c->err()};
+    if (launch_route_queue(logits, L.router_bias, T, router_args(L.router), c->at<int32_t>(c->off_ridx),
+                           c->at<float>(c->off_rw), c->at<int32_t>(c->off_rrank), c->at<int32_t>(c->off_blockcnt),
+                           idx_out, w_out, a, s) != hipSuccess)
       return AEP_ERR_DEVICE;
   } else if (T <= kFusedTokens) {
     if (launch_route_append(logits, T, E, k, c->cfg.renorm, idx_out, w_out, rows, row_bytes, base, cur, nxt,

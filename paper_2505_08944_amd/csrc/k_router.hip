@@ -2,170 +2,606 @@
 // groups, top-k, weights from the scores of the chosen (the rule is stated at
 // aep_router in aep.h).
 //
-// Choices are compared in binary64: a sigmoid plus a bias of like size has
-// neighbours that binary32 cannot tell apart, and the same logits must give
-// the same experts on every rank.
+// A token takes 16 lanes of a wave (32 above 256 experts), each holding up to
+// 16 of its experts.  Experts are compared as one f64 per expert: the f32 choice
+// (or logit) in its upper bits, the expert's id in the 29 that an f32 leaves
+// free, so that a single maximum orders by choice, then by id.  Every lane
+// sorts its keys with a network of maxima and minima; a selection round is then
+// a maximum over the lanes' heads by DPP, and the winner's lane moves up.
+//
+// The rule compares choices in binary64, as a score plus a bias of like size
+// has neighbours that binary32 cannot tell apart, and the same logits must give
+// the same experts on every rank.  Where all neighbours in the order, and the last kept and first dropped group,
+// are further apart than that, f32 has given the rule's answer.  Where they are
+// not (one token in a few hundred), the choices in question, one per lane, or
+// the groups, are compared again in f64.  Logits without a bias are compared as
+// they are, exactly.
 #include <float.h>
 #include <limits.h>
+
+#include <type_traits>
+#include <utility>
 
 #include "aep_internal.h"
 #include "route_token_id.h"
 
 namespace aep {
 
-// The larger key, equal: the lower id; id INT_MAX: none.
+// ------------------------------------------------------- lanes of one token
+// Lane l's value from lane l ^ 1, l ^ 2 (within four), 7 - l (within eight),
+// 15 - l (within 16): after a reduction over the steps before, each completes
+// the next one.  Step 4 (two rows of 16) goes through LDS permutes.
+template <int STEP>
+__device__ __forceinline__ int partner(int v) {
+  if constexpr (STEP == 4) return __shfl_xor(v, 16);
+  constexpr int ctrl = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 /* row_half_mirror */ : 0x140 /* row_mirror */;
+  return __builtin_amdgcn_update_dpp(0, v, ctrl, 0xF, 0xF, true);
+}
+template <int STEP>
+__device__ __forceinline__ float partner(float v) {
+  return __int_as_float(partner<STEP>(__float_as_int(v)));
+}
+template <int STEP>
+__device__ __forceinline__ double partner(double v) {
+  return __hiloint2double(partner<STEP>(__double2hiint(v)), partner<STEP>(__double2loint(v)));
+}
+template <int LANES, typename T, typename F>
+__device__ __forceinline__ T reduce(T v, F f) {
+  v = f(v, partner<0>(v));
+  v = f(v, partner<1>(v));
+  v = f(v, partner<2>(v));
+  v = f(v, partner<3>(v));
+  if constexpr (LANES == 32) v = f(v, partner<4>(v));
+  return v;
+}
+__device__ __forceinline__ double max64(double a, double b) { return __builtin_fmax(a, b); }
+template <int LANES>
+__device__ __forceinline__ double reduce_max(double v) {
+  return reduce<LANES>(v, [](double a, double b) { return max64(a, b); });
+}
+
+// -------------------------------------------------------------------- keys
+// f32 value and id (below 512) in one f64: larger value first, equal: lower id.
+constexpr int kIdMask = 511;
+__device__ __forceinline__ double make_key(float v, int id) {
+  const double d = (double)(v + 0.f);  // -0 becomes +0
+  const int lo = __double2loint(d), hi = __double2hiint(d);
+  return __hiloint2double(hi, lo | (hi < 0 ? id : kIdMask - id));
+}
+__device__ __forceinline__ int key_id(double k) {
+  const int lo = __double2loint(k) & kIdMask;
+  return __double2hiint(k) < 0 ? lo : kIdMask - lo;
+}
+// Below every f32: masked experts, by id, and then those that may not be picked.
+__device__ __forceinline__ double masked_key(int id) { return __hiloint2double((int)0xFE000000u, id); }
+__device__ __forceinline__ double never_key() { return -DBL_MAX; }
+__device__ __forceinline__ bool is_live(double k) { return k > -1e100; }
+static_assert(kMaxScoredExperts <= kIdMask + 1, "an id in kIdMask");
+
+// Neighbours a >= b that are further apart than both errors.  A softmax score
+// is off by at most 2^-19.5 of itself (e^x 2^-22, up to 20 additions of 2^-24,
+// the reciprocal 2^-23), a sigmoid by 2^-21.5, so scores, and sums of two
+// softmax scores, by at most 2^-19.5 and sums of two sigmoids by 2^-20.5; every
+// addition by half a step of its result.
+__device__ __forceinline__ bool apart(double a, double b, double slack) {
+  if (!is_live(a) || !is_live(b)) return true;
+  return a - b > slack + 0x1p-21 * (fabs(a) + fabs(b));
+}
+constexpr double kSlackSoftmax = 0x1p-18, kSlackSigmoid = 0x1p-19;
+
+// e^x for x <= 0 to 2^-22: the hardware's 2^x on the rounded x log2(e),
+// corrected for what the rounding lost.  0 below -200, -inf included.
+__device__ __forceinline__ float exp_neg(float x) {
+  x = fmaxf(x, -200.f);
+  const float t = x * 1.44269504f;
+  const float lost = __builtin_fmaf(x, 1.44269504f, -t) + x * 1.925963033e-8f;
+  const float e = __builtin_amdgcn_exp2f(t);
+  return __builtin_fmaf(e, lost * 0.693147181f, e);
+}
+// 1 / (1 + e^-x) to 2^-21.5 of itself or of 2^-1: where |x| times the rounding
+// of the exponent's product counts, s (1 - s) |x| is small.
+__device__ __forceinline__ float sigmoid32(float x) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504f));
+}
+__device__ __forceinline__ double sigmoid64(double x) { return 1.0 / (1.0 + exp(-x)); }
+
+// Sorts a lane's N keys, largest first: odd-even merge sort (Batcher 1968), its
+// comparators listed at compile time so that every key stays in a register.
+template <int N>
+struct SortNet {
+  int n = 0, a[64] = {}, b[64] = {};
+  constexpr SortNet() {
+    for (int p = 1; p < N; p *= 2)
+      for (int q = p; q >= 1; q /= 2)
+        for (int j = q % p; j <= N - 1 - q; j += 2 * q)
+          for (int i = 0; i < q; ++i)
+            if (i + j + q < N && (i + j) / (p * 2) == (i + j + q) / (p * 2)) {
+              a[n] = i + j;
+              b[n] = i + j + q;
+              ++n;
+            }
+  }
+};
+template <int N, size_t... I>
+__device__ __forceinline__ void sort_steps(double (&k)[N], std::index_sequence<I...>) {
+  constexpr SortNet<N> net;
+  auto step = [](double& x, double& y) {
+    const double hi = max64(x, y);
+    y = __builtin_fmin(x, y);
+    x = hi;
+  };
+  (step(k[net.a[I]], k[net.b[I]]), ...);
+}
+template <int N>
+__device__ __forceinline__ void sort_keys(double (&k)[N]) {
+  constexpr SortNet<N> net;
+  sort_steps<N>(k, std::make_index_sequence<net.n>{});
+}
+// The largest L of a lane's N keys, sorted: of 16, two sorted eights whose
+// larger halves (one list against the other reversed) are sorted once more.
+template <int N, int L>
+__device__ __forceinline__ void best_keys(const double (&k)[N], double (&out)[L]) {
+  if constexpr (N == L) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i] = k[i];
+    sort_keys<N>(out);
+  } else {
+    static_assert(N == 2 * L, "two lists");
+    double a[L], b[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      a[i] = k[i];
+      b[i] = k[L + i];
+    }
+    sort_keys<L>(a);
+    sort_keys<L>(b);
+#pragma unroll
+    for (int i = 0; i < L; ++i) out[i] = max64(a[i], b[L - 1 - i]);
+    // a bitonic sequence: log2 L rounds of halves
+#pragma unroll
+    for (int h = L / 2; h >= 1; h /= 2)
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (!(i & h)) {
+          const double hi = max64(out[i], out[i + h]);
+          out[i + h] = __builtin_fmin(out[i], out[i + h]);
+          out[i] = hi;
+        }
+  }
+}
+// The largest of the lanes' sorted lists; its lane moves up, to `end` at last:
+// never_key() where the list held all of the lane's experts, unknown_key(),
+// which is then the largest, where it did not.
+__device__ __forceinline__ double unknown_key() { return DBL_MAX; }
+template <int LANES, int N>
+__device__ __forceinline__ double take_best(double (&k)[N], double end) {
+  const double w = reduce_max<LANES>(k[0]);
+  const bool mine = k[0] == w;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    double a = k[i], b = i + 1 < N ? k[i + 1] : end;
+    asm("" : "+v"(a), "+v"(b));  // a choice of two values: not of two places, which would index registers
+    k[i] = mine ? b : a;
+  }
+  return w;
+}
+
+// The larger value, equal: the lower id; id INT_MAX: none.
 __device__ __forceinline__ void better(double& v, int& e, double ov, int oe) {
   if (oe != INT_MAX && (e == INT_MAX || ov > v || (ov == v && oe < e))) {
     v = ov;
     e = oe;
   }
 }
-__device__ __forceinline__ void wave_best(double& v, int& e) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) better(v, e, __shfl_xor(v, d), __shfl_xor(e, d));
+template <int LANES>
+__device__ __forceinline__ void best_of(double& v, int& e) {
+  better(v, e, partner<0>(v), partner<0>(e));
+  better(v, e, partner<1>(v), partner<1>(e));
+  better(v, e, partner<2>(v), partner<2>(e));
+  better(v, e, partner<3>(v), partner<3>(e));
+  if constexpr (LANES == 32) better(v, e, partner<4>(v), partner<4>(e));
 }
 
-// One wave per token; lane l holds experts l, l + 64, ...
-template <int EPL>
-__global__ __launch_bounds__(256) void route_scored_kernel(const float* __restrict__ logits, int64_t ld,
-                                                           const float* __restrict__ bias, int T, RouterArgs r,
-                                                           int32_t* __restrict__ idx, float* __restrict__ w,
-                                                           int32_t* __restrict__ idx2, float* __restrict__ w2,
-                                                           int32_t* __restrict__ flag) {
-  __shared__ double worth[4][EPL * 64];  // an expert's value to its group
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t t = (int64_t)blockIdx.x * 4 + wave;
-  const bool valid = t < T;
-  const int E = r.E, per = E / r.n_groups;
-  double key[EPL], score[EPL];
-  bool live[EPL];
-  bool bad = false;
-  float l[EPL];
-  float top = -__builtin_inff();
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    const int e = i * 64 + lane;
-    l[i] = valid && e < E ? logits[t * ld + e] : -__builtin_inff();
-    live[i] = __builtin_isfinite(l[i]);
-    if (!live[i] && l[i] != -__builtin_inff()) bad = true;
-    if (live[i]) top = fmaxf(top, l[i]);
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
-  double total = 0.0;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    score[i] = 0.0;
-    if (live[i]) score[i] = r.sigmoid ? 1.0 / (1.0 + exp(-(double)l[i])) : exp((double)l[i] - (double)top);
-    total += score[i];
-  }
-  if (!r.sigmoid) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d);
-#pragma unroll
-    for (int i = 0; i < EPL; ++i)
-      if (live[i]) score[i] = score[i] / total;
-  }
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    const int e = i * 64 + lane;
-    double c = bias ? score[i] + (e < E ? (double)bias[e] : 0.0) : (double)l[i];
-    if (live[i] && !__builtin_isfinite(c)) {
-      live[i] = false;
-      score[i] = 0.0;
-      bad = true;
-    }
-    key[i] = live[i] ? c : -__builtin_inf();
-    worth[wave][e] = !live[i] ? -__builtin_inf() : bias || r.group_top > 1 ? score[i] + (bias ? (double)bias[e] : 0.0) : (double)l[i];
-  }
-  __syncthreads();
+// What a token's lanes share in LDS where experts have groups: a value per
+// expert.  Its lanes are in one wave: ordering the wave's accesses is enough.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
-  // groups: lane g holds group g's value
-  uint64_t kept = ~0ull;
-  if (r.n_groups > 1) {
-    double v = -__builtin_inf();
-    if (lane < r.n_groups) {
-      double second = -__builtin_inf();
-      for (int i = 0; i < per; ++i) {
-        const double x = worth[wave][lane * per + i];
-        if (x > v) {
-          second = v;
-          v = x;
-        } else if (x > second) {
-          second = x;
+// Worths of groups from the experts' values in LDS (-inf: masked): the lanes
+// of a token share the groups, `share` lanes each where groups are few.
+// Returns the kept groups as a mask; certain: no other f32 rounding would have
+// kept others (slack < 0: the values are exact).
+template <int LANES, typename T>
+__device__ __forceinline__ uint64_t pick_groups(const T* __restrict__ val, const RouterArgs& r, int g, double slack,
+                                                bool& certain) {
+  const int per = r.E / r.n_groups;
+  // worth of groups i, i + 1, ... per lane; ids in the key's upper part for f64
+  T worth[4];
+  int share = 1;
+  while (2 * share * r.n_groups <= LANES) share *= 2;
+  const int sub = g & (share - 1), lead = g / share;  // lead: the group, LANES / share apart
+  const int step = LANES / share;
+  const T none = -(T)__builtin_inff();
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int gr = lead + q * step;
+    T a = none, b = none;
+    if (gr < r.n_groups) {
+      // four at a time, so that their reads are in flight together
+      for (int i = sub; i < per; i += 4 * share) {
+        T x[4];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) x[z] = val[gr * per + min(i + z * share, per - 1)];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          x[z] = i + z * share < per ? x[z] : none;
+          b = x[z] > a ? a : (x[z] > b ? x[z] : b);
+          a = x[z] > a ? x[z] : a;
         }
       }
-      if (r.group_top > 1 && second != -__builtin_inf()) v += second;
     }
-    kept = 0;
+    if (share > 1) {
+      // the lanes of a group join their two best (share is a power of two, at most LANES / 2)
+#define JOIN(STEP)                                            \
+  {                                                           \
+    const T oa = partner<STEP>(a), ob = partner<STEP>(b);     \
+    const T lo = oa > a ? a : oa, hi = oa > a ? oa : a;       \
+    const T nb = ob > b ? ob : b;                             \
+    a = hi;                                                   \
+    b = lo > nb ? lo : nb;                                    \
+  }
+      JOIN(0)
+      if (share > 2) JOIN(1)
+      if (share > 4) JOIN(2)
+      if (share > 8) JOIN(3)
+#undef JOIN
+    }
+    worth[q] = r.group_top > 1 && b != none ? a + b : a;
+    if (step * (q + 1) >= r.n_groups) {
+#pragma unroll
+      for (int z = q + 1; z < 4; ++z) worth[z] = none;
+      break;
+    }
+  }
+  uint64_t kept = 0;
+  certain = true;
+  if constexpr (sizeof(T) == 4) {
+    double key[4], last = 0.0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int gr = lead + q * step;
+      key[q] = gr >= r.n_groups ? never_key() : worth[q] == none ? masked_key(gr) : make_key(worth[q], gr);
+    }
+    for (int j = 0; j <= r.top_groups; ++j) {
+      double k = max64(max64(key[0], key[1]), max64(key[2], key[3]));
+      k = reduce_max<LANES>(k);
+      if (j == r.top_groups) {
+        certain = slack < 0.0 || apart(last, k, slack);
+        break;
+      }
+      last = k;
+      kept |= 1ull << key_id(k);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) key[q] = key[q] == k ? never_key() : key[q];
+    }
+  } else {
     for (int j = 0; j < r.top_groups; ++j) {
-      double bv = v;
-      int be = lane < r.n_groups && !((kept >> lane) & 1) ? lane : INT_MAX;
-      wave_best(bv, be);
-      kept |= 1ull << be;
+      double v = none;
+      int id = INT_MAX;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int gr = lead + q * step;
+        if (gr < r.n_groups && !((kept >> gr) & 1)) better(v, id, (double)worth[q], gr);
+      }
+      best_of<LANES>(v, id);
+      kept |= 1ull << id;
     }
+  }
+  return kept;
+}
+
+// The whole selection in f64, for a token with more choices too close to each
+// other than it has lanes: lane j gets slot j's expert.  All of its lanes call it.
+template <int EPL, int LANES>
+__device__ __noinline__ int select_exact(const float* __restrict__ l, const float* __restrict__ bias, RouterArgs r, int g,
+                                         double* __restrict__ val) {
+  const double none = -__builtin_inf();
+  double top = none, total = 0.0;
+  if (!r.sigmoid) {
+    for (int i = 0; i < EPL; ++i) {
+      const int e = i * LANES + g;
+      if (e < r.E && __builtin_isfinite(l[e])) top = max64(top, (double)l[e]);
+    }
+    top = reduce_max<LANES>(top);
+    for (int i = 0; i < EPL; ++i) {
+      const int e = i * LANES + g;
+      if (e < r.E && __builtin_isfinite(l[e])) total += exp((double)l[e] - top);
+    }
+    total = reduce<LANES>(total, [](double a, double b) { return a + b; });
+  }
+  double c[EPL];
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    const int e = i * LANES + g;
+    c[i] = none;
+    if (e < r.E && __builtin_isfinite(l[e])) {
+      const double x = (double)l[e];
+      c[i] = r.sigmoid ? sigmoid64(x) : exp(x - top) / total;
+      if (bias) c[i] += (double)bias[e];
+      if (!__builtin_isfinite(c[i])) c[i] = none;
+    }
+    if (r.n_groups > 1 && e < r.E) val[e] = c[i];
+  }
+  uint64_t kept = ~0ull;
+  if (r.n_groups > 1) {
+    wave_fence();
+    bool certain;
+    kept = pick_groups<LANES, double>(val, r, g, -1.0, certain);
   }
   unsigned avail = 0;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
-    const int e = i * 64 + lane;
-    if (e < E && (r.n_groups == 1 || ((kept >> (e / per)) & 1))) avail |= 1u << i;
+    const int e = i * LANES + g;
+    if (e < r.E && ((kept >> (r.n_groups > 1 ? e / (r.E / r.n_groups) : 0)) & 1)) avail |= 1u << i;
+    // without a bias experts are picked by their logits
+    if (!bias && c[i] != none) c[i] = (double)l[e];
   }
-  double my_s = 0.0, sum = 0.0;
-  int my_e = 0;
+  int mine = 0;
   for (int j = 0; j < r.k; ++j) {
-    double bv = -__builtin_inf(), bs = 0.0;
-    int be = INT_MAX;
+    double v = none;
+    int id = INT_MAX;
 #pragma unroll
     for (int i = 0; i < EPL; ++i)
-      if ((avail >> i) & 1) better(bv, be, key[i], i * 64 + lane);
-    wave_best(bv, be);
+      if ((avail >> i) & 1) better(v, id, c[i], i * LANES + g);
+    best_of<LANES>(v, id);
+    if (id % LANES == g) avail &= ~(1u << (id / LANES));
+    if (g == j) mine = id;
+  }
+  return mine;
+}
+
+// What the selection compares: the logits alone, or scores as well (choices with
+// a bias, sums of two scores as groups' worths).
+enum { kByLogit = 0, kBySoftmax = 1, kBySigmoid = 2 };
+
+// Routes token t on its LANES lanes: lane j < k gets slot j's expert and weight.
+// val: the token's LDS row (of E values; unused without groups).  bad: a value
+// to be reported was seen by this lane.
+template <int EPL, int LANES, int BY>
+__device__ __forceinline__ void route_scored(const float* __restrict__ logits, int64_t ld,
+                                             const float* __restrict__ bias, const RouterArgs& r, int64_t t, int g,
+                                             double* __restrict__ val, int& my_e, float& my_w, bool& bad) {
+  const float* __restrict__ l = logits + t * ld;
+  const float none = -__builtin_inff();
+  float x[EPL], b[EPL];
 #pragma unroll
-    for (int i = 0; i < EPL; ++i)
-      if (be == i * 64 + lane) {
-        bs = score[i];
-        avail &= ~(1u << i);
-      }
-    bs = __shfl(bs, be & 63);
-    sum += bs;
-    if (lane == j) {
-      my_e = be;
-      my_s = bs;
+  for (int i = 0; i < EPL; ++i) x[i] = l[min(i * LANES + g, r.E - 1)];
+  if (BY != kByLogit && bias) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) b[i] = bias[min(i * LANES + g, r.E - 1)];
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) b[i] = 0.f;
+  }
+  bad = false;
+  float top = none;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    // a difference of a finite value with itself is 0, of any other NaN
+    const bool live = x[i] - x[i] == 0.f;
+    bad |= !live && x[i] != none;
+    x[i] = live && i * LANES + g < r.E ? x[i] : none;
+    top = fmaxf(top, x[i]);
+  }
+  float total = 1.f;
+  if (!r.sigmoid) {
+    top = reduce<LANES>(top, [](float a, float b) { return fmaxf(a, b); });
+    top = top == none ? 0.f : top;  // every expert masked
+    if (BY == kBySoftmax || !r.renorm) {
+      total = 0.f;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) total += exp_neg(x[i] - top);
+      total = reduce<LANES>(total, [](float a, float b) { return a + b; });
     }
   }
-  if (r.renorm) my_s = sum > 0.0 ? my_s / sum : 0.0;
-  if (valid && lane < r.k) {
-    const int64_t o = t * r.k + lane;
-    const float v = (float)(my_s * (double)r.scale);
-    idx[o] = my_e;
-    w[o] = v;
-    if (idx2) idx2[o] = my_e;
-    if (w2) w2[o] = v;
+  // choices, or logits; with groups, what an expert is worth to its group
+  const float inv = BY == kBySoftmax ? __builtin_amdgcn_rcpf(total) : 1.f;
+  float* __restrict__ val32 = reinterpret_cast<float*>(val);
+  double key[EPL];
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    const int e = i * LANES + g;
+    float c = x[i];
+    if constexpr (BY == kBySoftmax) c = exp_neg(x[i] - top) * inv + b[i];
+    if constexpr (BY == kBySigmoid) c = sigmoid32(x[i]) + b[i];
+    const bool off = BY != kByLogit && c - c != 0.f && x[i] != none;  // a bias that is not finite
+    bad |= off;
+    c = x[i] == none || off ? none : c;
+    if (r.n_groups > 1 && e < r.E) val32[e] = c;
+    const float by = BY == kByLogit || bias ? c : x[i];
+    key[i] = e >= r.E ? never_key() : c == none ? masked_key(e) : make_key(by, e);
+  }
+  constexpr double slack = BY == kByLogit ? -1.0 : BY == kBySoftmax ? kSlackSoftmax : kSlackSigmoid;
+  // softmax in f64, where it is needed
+  auto total64 = [&] {
+    double z = 0.0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) z += x[i] == none ? 0.0 : exp((double)x[i] - (double)top);
+    return reduce<LANES>(z, [](double a, double b) { return a + b; });
+  };
+  if (r.n_groups > 1) {
+    wave_fence();
+    bool certain;
+    uint64_t kept = pick_groups<LANES, float>(val32, r, g, slack, certain);
+    if (BY != kByLogit && !certain) {
+      const double z = BY == kBySoftmax ? total64() : 1.0;
+      wave_fence();
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        const int e = i * LANES + g;
+        double c = BY == kBySigmoid ? sigmoid64((double)x[i]) : exp((double)x[i] - (double)top) / z;
+        c += (double)b[i];
+        if (e < r.E) val[e] = is_live(key[i]) ? c : -__builtin_inf();
+      }
+      wave_fence();
+      kept = pick_groups<LANES, double>(val, r, g, -1.0, certain);
+    }
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      const int e = i * LANES + g;
+      if (!((kept >> ((e * r.inv_per) >> 20)) & 1)) key[i] = never_key();
+    }
+  }
+  constexpr int L = EPL > 8 ? 8 : EPL;
+  double list[L];
+  best_keys<EPL, L>(key, list);
+  const double end = L < EPL ? unknown_key() : never_key();
+  my_e = 0;
+  bool close = false, lost = false;  // choices too close to each other; more of them than were kept at hand
+  double last = 0.0;
+  for (int j = 0; j < r.k; ++j) {
+    const double w = take_best<LANES, L>(list, end);
+    lost |= w == unknown_key();
+    if (BY != kByLogit && bias) close |= j > 0 && !apart(last, w, slack);
+    last = w;
+    if (g == j) my_e = key_id(w);
+  }
+  if (BY != kByLogit && bias) {
+    // the candidates go on to the first one that is clearly behind
+    int n = r.k;
+    for (;; ++n) {
+      const double w = take_best<LANES, L>(list, end);
+      lost |= w == unknown_key();
+      if (lost || apart(last, w, slack)) break;
+      close = true;
+      if (n == LANES) {
+        lost = true;
+        break;
+      }
+      last = w;
+      if (g == n) my_e = key_id(w);
+    }
+    if (close && !lost) {
+      // lane j's candidate, in f64, takes the slot of its rank
+      const double z = BY == kBySoftmax ? total64() : 1.0;
+      const double none64 = -__builtin_inf();
+      double c = none64;
+      int id = INT_MAX;
+      if (g < n) {
+        id = my_e;
+        const double v = (double)l[id], bv = (double)bias[id];
+        if (v - v == 0.0 && bv - bv == 0.0) c = (BY == kBySigmoid ? sigmoid64(v) : exp(v - (double)top) / z) + bv;
+      }
+      int rank = 0;
+      for (int d = 1; d < LANES; ++d) {
+        const int from = (g + d) & (LANES - 1);
+        const double oc = __shfl(c, from, LANES);
+        const int oid = __shfl(id, from, LANES);
+        rank += oid != INT_MAX && (oc > c || (oc == c && oid < id));
+      }
+      // lanes without a candidate keep to their own places behind
+      rank = g < n ? rank : g;
+      const int at = ((threadIdx.x & 63 & ~(LANES - 1)) + rank) * 4;
+      my_e = __builtin_amdgcn_ds_permute(at, my_e);
+    }
+  }
+  if (lost) my_e = select_exact<EPL, LANES>(l, bias, r, g, val);
+
+  // weights, from the chosen ones' scores in f64
+  double s = 0.0;
+  if (g < r.k) {
+    const float v = l[my_e];
+    const bool live = __builtin_isfinite(v) && (!bias || __builtin_isfinite(bias[my_e]));
+    if (live) s = r.sigmoid ? sigmoid64((double)v) : exp((double)v - (double)top);
+  }
+  if (r.renorm) {
+    const double sum = reduce<LANES>(s, [](double a, double b) { return a + b; });
+    s = sum > 0.0 ? s / sum : 0.0;
+  } else if (!r.sigmoid) {
+    s = total > 0.f ? s / (double)total : 0.0;  // 0: every expert masked
+  }
+  my_w = (float)(s * (double)r.scale);
+}
+
+// Tokens without queues.
+template <int EPL, int LANES, int BY>
+__global__ __launch_bounds__(256) void route_scored_kernel(const float* __restrict__ logits, int64_t ld,
+                                                           const float* __restrict__ bias, int T, RouterArgs r,
+                                                           int32_t* __restrict__ idx, float* __restrict__ w,
+                                                           int32_t* __restrict__ flag) {
+  extern __shared__ double vals[];
+  const int g = threadIdx.x & (LANES - 1), tb = threadIdx.x / LANES;
+  const int64_t t = (int64_t)blockIdx.x * (blockDim.x / LANES) + tb;
+  int e;
+  float v;
+  bool bad;
+  // (the last tokens' lanes repeat the last one: a wave has no idle rows)
+  route_scored<EPL, LANES, BY>(logits, ld, bias, r, t < T ? t : T - 1, g, vals + tb * r.row, e, v, bad);
+  if (t < T && g < r.k) {
+    idx[t * r.k + g] = e;
+    w[t * r.k + g] = v;
   }
   if (bad && flag) atomicOr(flag, kErrNonFinite);
 }
 
-// Rank of each (token, slot) among its block's rows of the same expert, and
-// the block's rows per expert: blockcnt [E][nb].
-__global__ __launch_bounds__(kRouteThreads) void rank_scored_kernel(const int32_t* __restrict__ r_idx, int T, int E,
-                                                                    int k, int32_t* __restrict__ r_rank,
-                                                                    int32_t* __restrict__ blockcnt) {
+// A fragment for the queues, 32 tokens per workgroup: routed, and each (token,
+// slot) ranked among the workgroup's rows of its expert (as in k_route.hip: the
+// tokens that picked an expert are a mask).  A fragment of one workgroup gets
+// its queue entries and depths written here; else blockcnt [E][workgroups] gets
+// the workgroup's rows per expert.
+template <int EPL, int LANES, int BY>
+__global__ __launch_bounds__(32 * LANES) void route_queue_kernel(
+    const float* __restrict__ logits, const float* __restrict__ bias, int T, RouterArgs r, int32_t* __restrict__ r_idx,
+    float* __restrict__ r_w, int32_t* __restrict__ r_rank, int32_t* __restrict__ blockcnt,
+    int32_t* __restrict__ idx_out, float* __restrict__ w_out, AppendArgs a) {
+  extern __shared__ double vals[];
   __shared__ uint32_t tok_mask[kMaxScoredExperts];
-  const int tid = threadIdx.x, g = tid & (kRouteLanes - 1), tb = tid / kRouteLanes;
-  const int t = blockIdx.x * kRouteTokens + tb;
-  const bool on = t < T && g < k;
-  for (int e = tid; e < E; e += kRouteThreads) tok_mask[e] = 0;
+  const int tid = threadIdx.x, g = tid & (LANES - 1), tb = tid / LANES;
+  const int t = blockIdx.x * 32 + tb;
+  for (int e = tid; e < r.E; e += 32 * LANES) tok_mask[e] = 0;
   __syncthreads();
-  const int64_t o = (int64_t)t * k + g;
-  const int e = on ? r_idx[o] : 0;
+  int e;
+  float w;
+  bool bad;
+  route_scored<EPL, LANES, BY>(logits, r.E, bias, r, t < T ? t : T - 1, g, vals + tb * r.row, e, w, bad);
+  const bool on = t < T && g < r.k;
   if (on) atomicOr(&tok_mask[e], 1u << tb);
   __syncthreads();
-  for (int x = tid; x < E; x += kRouteThreads) blockcnt[(int64_t)x * gridDim.x + blockIdx.x] = __popc(tok_mask[x]);
-  if (on) r_rank[o] = __popc(tok_mask[e] & ((1u << tb) - 1u));
+  const int rank = on ? __popc(tok_mask[e] & ((1u << tb) - 1u)) : 0;
+  const int64_t o = (int64_t)t * r.k + g;
+  if (on) {
+    if (idx_out) idx_out[o] = e;
+    if (w_out) w_out[o] = w;
+  }
+  if (bad) atomicOr(a.err, kErrNonFinite);
+  if (gridDim.x == 1) {
+    if (t < T) {
+      const char* row = a.x + (int64_t)t * a.row_bytes;
+      const int tok = token_id(t, g, r.k, a.token_base, a.token_ids, a.n_ids, a.live, a.pend, a.err);
+      if (on) {
+        QEntry en;
+        en.row = row;
+        en.token_slot = tok | (g << kTokenBits);
+        en.w = w;
+        a.q[(int64_t)e * a.q_stride + a.depth_cur[e] + rank] = en;
+      }
+      if (g == 0) a.tok_row[tok] = row;
+    }
+    for (int x = tid; x < r.E; x += 32 * LANES) a.depth_nxt[x] = a.depth_cur[x] + __popc(tok_mask[x]);
+  } else {
+    for (int x = tid; x < r.E; x += 32 * LANES) blockcnt[(int64_t)x * gridDim.x + blockIdx.x] = __popc(tok_mask[x]);
+    if (on) {
+      r_idx[o] = e;
+      r_w[o] = w;
+      r_rank[o] = rank;
+    }
+  }
 }
 
-// One wave per expert: its block counts become the blocks' first queue slots,
-// and its depth after the fragment is published.
+// One wave per expert: its workgroup counts become the workgroups' first queue
+// slots, and its depth after the fragment is published.
 __global__ __launch_bounds__(64) void scan_scored_kernel(int32_t* __restrict__ blockcnt, int nb,
                                                          const int32_t* __restrict__ depth_cur,
                                                          int32_t* __restrict__ depth_nxt) {
@@ -187,16 +623,33 @@ __global__ __launch_bounds__(64) void scan_scored_kernel(int32_t* __restrict__ b
   if (lane == 0) depth_nxt[e] = base;
 }
 
-__global__ __launch_bounds__(kRouteThreads) void append_scored_kernel(
-    const int32_t* __restrict__ r_idx, const float* __restrict__ r_w, const int32_t* __restrict__ r_rank,
-    const int32_t* __restrict__ first, int T, int k, const char* x, int64_t row_bytes, int32_t token_base,
-    QEntry* __restrict__ q, int64_t q_stride, const void** __restrict__ tok_row, const int32_t* __restrict__ token_ids,
-    int n_ids, int32_t* __restrict__ live, int32_t* __restrict__ pend, int32_t* __restrict__ err) {
-  const int tid = threadIdx.x, g = tid & (kRouteLanes - 1);
+// Queue entries of routed and ranked tokens, 32 per workgroup.  first: the
+// scanned counts, or (direct) the counts themselves, of which every workgroup
+// adds the ones before its own, and the last one publishes the depths.
+__global__ __launch_bounds__(kRouteThreads) void append_scored_kernel(const int32_t* __restrict__ r_idx,
+                                                                      const float* __restrict__ r_w,
+                                                                      const int32_t* __restrict__ r_rank,
+                                                                      const int32_t* __restrict__ first, bool direct,
+                                                                      int T, int E, int k, AppendArgs a) {
+  __shared__ int32_t base[kMaxScoredExperts];
+  const int tid = threadIdx.x, nb = gridDim.x;
+  for (int e = tid; e < E; e += kRouteThreads) {
+    const int32_t* c = first + (int64_t)e * nb;
+    int v = c[blockIdx.x];
+    if (direct) {
+      int sum = a.depth_cur[e];
+      for (int b = 0; b < (int)blockIdx.x; ++b) sum += c[b];
+      if ((int)blockIdx.x == nb - 1) a.depth_nxt[e] = sum + v;
+      v = sum;
+    }
+    base[e] = v;
+  }
+  __syncthreads();
+  const int g = tid & (kRouteLanes - 1);
   const int t = blockIdx.x * kRouteTokens + tid / kRouteLanes;
   if (t >= T) return;
-  const char* row = x + (int64_t)t * row_bytes;
-  const int tok = token_id(t, g, k, token_base, token_ids, n_ids, live, pend, err);
+  const char* row = a.x + (int64_t)t * a.row_bytes;
+  const int tok = token_id(t, g, k, a.token_base, a.token_ids, a.n_ids, a.live, a.pend, a.err);
   if (g < k) {
     const int64_t o = (int64_t)t * k + g;
     const int e = r_idx[o];
@@ -204,38 +657,61 @@ __global__ __launch_bounds__(kRouteThreads) void append_scored_kernel(
     en.row = row;
     en.token_slot = tok | (g << kTokenBits);
     en.w = r_w[o];
-    q[(int64_t)e * q_stride + first[(int64_t)e * gridDim.x + blockIdx.x] + r_rank[o]] = en;
+    a.q[(int64_t)e * a.q_stride + base[e] + r_rank[o]] = en;
   }
-  if (g == 0) tok_row[tok] = row;
+  if (g == 0) a.tok_row[tok] = row;
+}
+
+// Calls f(EPL, LANES, BY) as constants.
+template <typename F>
+static void by_rule(const RouterArgs& r, bool bias, F f) {
+  auto sized = [&](auto by) {
+    if (r.E <= 64)
+      f(std::integral_constant<int, 4>{}, std::integral_constant<int, 16>{}, by);
+    else if (r.E <= 128)
+      f(std::integral_constant<int, 8>{}, std::integral_constant<int, 16>{}, by);
+    else if (r.E <= 256)
+      f(std::integral_constant<int, 16>{}, std::integral_constant<int, 16>{}, by);
+    else
+      f(std::integral_constant<int, 16>{}, std::integral_constant<int, 32>{}, by);
+  };
+  if (!bias && !(r.n_groups > 1 && r.group_top > 1))
+    sized(std::integral_constant<int, kByLogit>{});
+  else if (r.sigmoid)
+    sized(std::integral_constant<int, kBySigmoid>{});
+  else
+    sized(std::integral_constant<int, kBySoftmax>{});
 }
 
 hipError_t launch_route_scored(const float* logits, int64_t ld, const float* bias, int T, const RouterArgs& r,
-                               int32_t* idx, float* w, int32_t* idx2, float* w2, int32_t* flag, hipStream_t s) {
-  const int nb = (int)(((int64_t)T + 3) / 4);
-  if (r.E <= 64)
-    route_scored_kernel<1><<<nb, 256, 0, s>>>(logits, ld, bias, T, r, idx, w, idx2, w2, flag);
-  else if (r.E <= 128)
-    route_scored_kernel<2><<<nb, 256, 0, s>>>(logits, ld, bias, T, r, idx, w, idx2, w2, flag);
-  else if (r.E <= 256)
-    route_scored_kernel<4><<<nb, 256, 0, s>>>(logits, ld, bias, T, r, idx, w, idx2, w2, flag);
-  else
-    route_scored_kernel<8><<<nb, 256, 0, s>>>(logits, ld, bias, T, r, idx, w, idx2, w2, flag);
+                               int32_t* idx, float* w, int32_t* flag, hipStream_t s) {
+  by_rule(r, bias != nullptr, [&](auto epl, auto lanes, auto by) {
+    // few tokens: a wave per workgroup, so that they spread over the CUs
+    const int threads = T <= 4096 ? 64 : 256, tokens = threads / lanes();
+    const size_t lds = r.n_groups > 1 ? (size_t)tokens * r.row * 8 : 0;
+    route_scored_kernel<epl(), lanes(), by()><<<(T + (int64_t)tokens - 1) / tokens, threads, lds, s>>>(logits, ld, bias, T, r, idx,
+                                                                                               w, flag);
+  });
   return hipGetLastError();
 }
 
-hipError_t launch_append_scored(const int32_t* r_idx, const float* r_w, int32_t* r_rank, int32_t* blockcnt, int T, int E,
-                                int k, const char* x, int64_t row_bytes, int32_t token_base, const int32_t* depth_cur,
-                                int32_t* depth_nxt, QEntry* q, int64_t q_stride, const void** tok_row,
-                                const int32_t* token_ids, int n_ids, int32_t* live, int32_t* pend, int32_t* err,
-                                hipStream_t s) {
-  const int nb = (T + kRouteTokens - 1) / kRouteTokens;
-  rank_scored_kernel<<<nb, kRouteThreads, 0, s>>>(r_idx, T, E, k, r_rank, blockcnt);
+hipError_t launch_route_queue(const float* logits, const float* bias, int T, const RouterArgs& r, int32_t* r_idx,
+                              float* r_w, int32_t* r_rank, int32_t* blockcnt, int32_t* idx_out, float* w_out,
+                              const AppendArgs& a, hipStream_t s) {
+  const int nb = (T + 31) / 32;
+  by_rule(r, bias != nullptr, [&](auto epl, auto lanes, auto by) {
+    const size_t lds = r.n_groups > 1 ? (size_t)32 * r.row * 8 : 0;
+    route_queue_kernel<epl(), lanes(), by()><<<nb, 32 * lanes(), lds, s>>>(logits, bias, T, r, r_idx, r_w, r_rank, blockcnt,
+                                                                         idx_out, w_out, a);
+  });
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  scan_scored_kernel<<<E, 64, 0, s>>>(blockcnt, nb, depth_cur, depth_nxt);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  append_scored_kernel<<<nb, kRouteThreads, 0, s>>>(r_idx, r_w, r_rank, blockcnt, T, k, x, row_bytes, token_base, q,
-                                                    q_stride, tok_row, token_ids, n_ids, live, pend, err);
+  if (e != hipSuccess || nb == 1) return e;
+  const bool direct = nb <= kDirectPrefixBlocks;
+  if (!direct) {
+    scan_scored_kernel<<<r.E, 64, 0, s>>>(blockcnt, nb, a.depth_cur, a.depth_nxt);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  append_scored_kernel<<<nb, kRouteThreads, 0, s>>>(r_idx, r_w, r_rank, blockcnt, direct, T, r.E, r.k, a);
   return hipGetLastError();
 }
 

@@ -27,8 +27,9 @@ aep_status check_router(const aep_router* r) {
 }
 
 RouterArgs router_args(const aep_router& r) {
-  return RouterArgs{r.n_experts, r.top_k, r.score == AEP_SCORE_SIGMOID, r.n_groups, r.top_groups, r.group_top, r.renorm,
-                    r.scale};
+  const int per = r.n_experts / r.n_groups;
+  return RouterArgs{r.n_experts, r.top_k,  r.score == AEP_SCORE_SIGMOID, r.n_groups,       r.top_groups, r.group_top,
+                    r.renorm,    r.scale, ((1 << 20) + per - 1) / per,  r.n_experts | 1};
 }
 
 }  // namespace aep
@@ -115,7 +116,7 @@ aep_status aep_route_topk(const aep_router* r, const float* logits, int64_t ld_l
   if (T == 0) return AEP_OK;
   if (!logits || !idx || !w) return AEP_ERR_INVALID_ARG;
   if (off(logits, 4) || off(bias, 4) || off(idx, 4) || off(w, 4) || off(flag, 4)) return AEP_ERR_INVALID_ARG;
-  return launch_route_scored(logits, ld_logits, bias, T, router_args(*r), idx, w, nullptr, nullptr, flag,
+  return launch_route_scored(logits, ld_logits, bias, T, router_args(*r), idx, w, flag,
                              reinterpret_cast<hipStream_t>(stream)) == hipSuccess
              ? AEP_OK
              : AEP_ERR_DEVICE;

@@ -1,6 +1,8 @@
 """Routing by scores against a 64-bit form of the rule: ids equal, weights
 within a few roundings of f32 (they are rounded once from 64 bits: half a step,
-2^-24 relative, and 2^-40 for the 64-bit steps before it)."""
+2^-24 relative, and 2^-40 for the 64-bit steps before it; a softmax that is not
+renormalised divides by a sum of f32 exponentials, each off by at most 2^-22,
+added up in at most 20 steps of 2^-24 each: 2^-19.5)."""
 
 import numpy as np
 import pytest
@@ -61,7 +63,8 @@ def check(c, l, b, idx, w):
     bad = np.argwhere((gi != ri).any(1)).ravel()
     assert not bad.size, (c, bad[:3], gi[bad[:2]], ri[bad[:2]])
     # results below f32's normal range are rounded to its fixed step there
-    assert np.all(np.abs(gw - rw) <= W_TOL * rw + 2.0 ** -149), (c, np.abs(gw - rw).max())
+    tol = W_TOL + (2.0 ** -19.5 if c.get("score", "softmax") == "softmax" and not c.get("renorm", True) else 0.0)
+    assert np.all(np.abs(gw - rw) <= tol * rw + 2.0 ** -149), (c, np.abs(gw - rw).max())
 
 
 @pytest.mark.parametrize("c", RULES, ids=lambda c: "-".join(f"{k}{v}" for k, v in c.items()))
