@@ -236,8 +236,8 @@ struct LinearArgs {
   int64_t ldx, ldw, ldy, ldr;
   const void *x, *w, *scale, *bias, *res;
   void* y;
-  bool aligned, vec_scale, vec_bias, vec_res, vec_y;
-  bool wide;  // bf16 y, and the residual if any: eight columns from a multiple of eight on at once, n a multiple of 8
+  int aligned, vec_scale, vec_bias, vec_res, vec_y;  // 0 or 1 (words: read through the scalar cache)
+  int wide;  // bf16 y, and the residual if any: eight columns from a multiple of eight on at once, n a multiple of 8
 };
 // nwg: workgroups of a persistent launch; scratch may be null with 0 floats.
 hipError_t launch_linear(const LinearArgs& p, int nwg, float* scratch, int64_t scratch_floats, hipStream_t s);

@@ -18,51 +18,54 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 // ------------------------------------------------------------- row kernel
-// Element types of the operands: what one lane holds of a chunk of K, and how.
-// bf16 / fp8: a chunk is 64 values of k; lane quarter h = lane / 16 holds k =
-// 16 h .. 16 h + 15 of its row, in both operands alike, so MFMA step s pairs k
-// = 16 h + 8 s + j of both.  f32: 32 values, k = 8 h .. 8 h + 7, eight steps
-// of 16x16x4.
-// N values of T from p on: 16-byte loads where the rows are aligned, else
-// unaligned ones; values from `left` on are zeros.
-template <typename T, int N, bool ALIGNED>
-__device__ __forceinline__ void load_row(uint4* __restrict__ out, const T* __restrict__ p, int left, bool whole) {
-  constexpr int PER = 16 / (int)sizeof(T);  // values per 16 bytes
-  constexpr int Q = N / PER;
-  if (whole) {
+// A chunk of K is 128 bytes of an x row (64 bf16 or 32 f32 values) and the
+// same values of k of a W row.  A wave reads 16 rows by 64 bytes per load, the
+// four lanes of a quad 64 consecutive bytes: lanes that read a row each, as an
+// MFMA operand lies in them, take the load path 64 cycles per load, four times
+// as long (32 x 4096 x 4096: 13.4 us).  The way from that order to the
+// operand's is through the wave's own LDS, in order and without a barrier:
+// lane l's 16 bytes go to place l; piece q of row r comes to lie at place 4 r +
+// (q ^ (r / 4)), from where 16 lanes that read one piece of 16 rows hit all banks.
+
+// 16 bytes of a row at p: unaligned ones where the rows are.
+template <bool ALIGNED, typename T>
+__device__ __forceinline__ uint4 load16(const T* __restrict__ p) {
+  uint4 v;
+  if constexpr (ALIGNED)
+    v = *reinterpret_cast<const uint4*>(p);
+  else
+    __builtin_memcpy(&v, p, 16);
+  return v;
+}
+// The same at the end of a row: values from `left` on are zeros.
+template <bool ALIGNED, typename T>
+__device__ __forceinline__ uint4 load16_end(const T* __restrict__ p, int left) {
+  constexpr int PER = 16 / (int)sizeof(T);
+  if constexpr (ALIGNED) {  // 16 bytes end where the row does
+    return left > 0 ? *reinterpret_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0);
+  } else {
+    T v[PER];
 #pragma unroll
-    for (int i = 0; i < Q; ++i) {
-      if constexpr (ALIGNED)
-        out[i] = *reinterpret_cast<const uint4*>(p + i * PER);
-      else
-        __builtin_memcpy(&out[i], p + i * PER, 16);
-    }
-    return;
-  }
-#pragma unroll
-  for (int i = 0; i < Q; ++i) {
-    if constexpr (ALIGNED) {  // 16 bytes end where the row does
-      out[i] = make_uint4(0, 0, 0, 0);
-      if (i * PER < left) out[i] = *reinterpret_cast<const uint4*>(p + i * PER);
-    } else {
-      T v[PER];
-#pragma unroll
-      for (int j = 0; j < PER; ++j) v[j] = i * PER + j < left ? p[i * PER + j] : T(0);
-      __builtin_memcpy(&out[i], v, 16);
-    }
+    for (int j = 0; j < PER; ++j) v[j] = j < left ? p[j] : T(0);
+    uint4 o;
+    __builtin_memcpy(&o, v, 16);
+    return o;
   }
 }
 
 // XT / WT: storage types (uint16_t bf16, uint8_t e4m3, float).  RF x CF
-// fragments of 16 x 16 outputs per workgroup.
-template <typename XT, typename WT, int RF, int CF, int WAVES, bool ALIGNED>
+// fragments of 16 x 16 outputs per workgroup, WAVES waves, which split K, each
+// with D chunks of it in flight.
+template <typename XT, typename WT, int RF, int CF, int WAVES, int D, bool ALIGNED>
 __global__ __launch_bounds__(WAVES * 64) void linear_rows_kernel(const LinearArgs p) {
-  constexpr bool F32 = sizeof(XT) == 4;
-  constexpr int KC = F32 ? 32 : 64;      // k per chunk
-  constexpr int LK = KC / 4;             // k per lane and chunk
-  constexpr int XQ = LK * (int)sizeof(XT) / 16, WQ = LK * (int)sizeof(WT) / 16;
+  constexpr bool F32 = sizeof(XT) == 4, FP8 = sizeof(WT) == 1;
+  constexpr int KC = 128 / (int)sizeof(XT);  // k per chunk
+  constexpr int XQ = 2, WQ = FP8 ? 1 : 2;    // loads per fragment and chunk
+  constexpr int XP = 16 / (int)sizeof(XT), WP = 16 / (int)sizeof(WT);  // values per 16 bytes
   constexpr int TM = RF * 16, TN = CF * 16, PITCH = TN + 4;
-  __shared__ float part[WAVES][TM][PITCH];
+  constexpr int kStage = (RF * XQ + CF * WQ) * 1024;  // a wave's chunk
+  constexpr int kPart = TM * PITCH * 4;               // its sums
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[WAVES * (kStage > kPart ? kStage : kPart)];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rr = lane & 15, hh = lane >> 4;
   // an XCD gets a contiguous run of tiles, row tiles of a column band adjacent
@@ -72,16 +75,18 @@ __global__ __launch_bounds__(WAVES * 64) void linear_rows_kernel(const LinearArg
   if (tile >= (int64_t)tm * ((p.n + TN - 1) / TN)) return;
   const int ti = (int)(tile % tm), tj = (int)(tile / tm);
   const int m0 = ti * TM, n0 = tj * TN;
-  const int K = p.k, nch = (K + KC - 1) / KC;
+  const int K = p.k, nch = K / KC;  // whole chunks
 
+  // this lane's row and 16-byte piece of a load
+  const int lr = lane >> 2, lq = (lane & 3) ^ (lane >> 4);
   const XT* xr[RF];
   const WT* wr[CF];
 #pragma unroll
   for (int i = 0; i < RF; ++i)
-    xr[i] = reinterpret_cast<const XT*>(p.x) + (int64_t)min(m0 + i * 16 + rr, p.m - 1) * p.ldx + hh * LK;
+    xr[i] = reinterpret_cast<const XT*>(p.x) + (int64_t)min(m0 + i * 16 + lr, p.m - 1) * p.ldx + lq * XP;
 #pragma unroll
   for (int j = 0; j < CF; ++j)
-    wr[j] = reinterpret_cast<const WT*>(p.w) + (int64_t)min(n0 + j * 16 + rr, p.n - 1) * p.ldw + hh * LK;
+    wr[j] = reinterpret_cast<const WT*>(p.w) + (int64_t)min(n0 + j * 16 + lr, p.n - 1) * p.ldw + lq * WP;
 
   f32x4_t acc[RF][CF];
 #pragma unroll
@@ -89,123 +94,192 @@ __global__ __launch_bounds__(WAVES * 64) void linear_rows_kernel(const LinearArg
 #pragma unroll
     for (int j = 0; j < CF; ++j) acc[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-  uint4 xa[2][RF][XQ], wa[2][CF][WQ];
+  uint4 xa[D][RF][XQ], wa[D][CF][WQ];
   auto load = [&](int b, int c) {
-    const int k0 = c * KC, left = K - k0 - hh * LK;
-    const bool whole = k0 + KC <= K;
+    const int k0 = c * KC;
 #pragma unroll
-    for (int j = 0; j < CF; ++j) load_row<WT, LK, ALIGNED>(wa[b][j], wr[j] + k0, left, whole);
+    for (int j = 0; j < CF; ++j)
 #pragma unroll
-    for (int i = 0; i < RF; ++i) load_row<XT, LK, ALIGNED>(xa[b][i], xr[i] + k0, left, whole);
+      for (int q = 0; q < WQ; ++q) wa[b][j][q] = load16<ALIGNED>(wr[j] + k0 + q * 4 * WP);
+#pragma unroll
+    for (int i = 0; i < RF; ++i)
+#pragma unroll
+      for (int q = 0; q < XQ; ++q) xa[b][i][q] = load16<ALIGNED>(xr[i] + k0 + q * 4 * XP);
+  };
+  unsigned char* mine = smem + wave * kStage;
+  // 16 bytes of row rr of a fragment: piece q (of 8, or 4 for fp8 W)
+  auto piece = [&](const unsigned char* frag, int q) {
+    return *reinterpret_cast<const uint4*>(frag + (q >> 2) * 1024 + (rr * 4 + ((q & 3) ^ (rr >> 2))) * 16);
   };
   auto mma = [&](int b) {
-    if constexpr (F32) {
+    unsigned char* at = mine;
 #pragma unroll
-      for (int q = 0; q < XQ; ++q) {
+    for (int j = 0; j < CF; ++j)
 #pragma unroll
-        for (int i = 0; i < RF; ++i)
+      for (int q = 0; q < WQ; ++q, at += 1024) *reinterpret_cast<uint4*>(at + lane * 16) = wa[b][j][q];
 #pragma unroll
-          for (int j = 0; j < CF; ++j) {
-            const uint4 a = wa[b][j][q], v = xa[b][i][q];
+    for (int i = 0; i < RF; ++i)
+#pragma unroll
+      for (int q = 0; q < XQ; ++q, at += 1024) *reinterpret_cast<uint4*>(at + lane * 16) = xa[b][i][q];
+    const unsigned char* xs = mine + CF * WQ * 1024;
+    uint4 x[RF][2], w[CF][2];
+#pragma unroll
+    for (int j = 0; j < CF; ++j) {
+      if constexpr (FP8) {
+        const uint4 v = piece(mine + j * 1024, hh);  // k = 16 hh ..
+        const uint2 w0 = e4m3x4_to_bf16x4(v.x), w1 = e4m3x4_to_bf16x4(v.y);
+        const uint2 w2 = e4m3x4_to_bf16x4(v.z), w3 = e4m3x4_to_bf16x4(v.w);
+        w[j][0] = make_uint4(w0.x, w0.y, w1.x, w1.y);
+        w[j][1] = make_uint4(w2.x, w2.y, w3.x, w3.y);
+      } else {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) w[j][s] = piece(mine + j * 2048, 4 * s + hh);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < RF; ++i)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) x[i][s] = piece(xs + i * 2048, FP8 ? 2 * hh + s : 4 * s + hh);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int j = 0; j < CF; ++j) {
+          if constexpr (F32) {
+            const uint4 a = w[j][s], v = x[i][s];
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(v.x), acc[i][j], 0, 0, 0);
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(v.y), acc[i][j], 0, 0, 0);
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(v.z), acc[i][j], 0, 0, 0);
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(v.w), acc[i][j], 0, 0, 0);
+          } else {
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w[j][s]),
+                                                                __builtin_bit_cast(bf16x8_t, x[i][s]), acc[i][j], 0, 0, 0);
           }
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < CF; ++j) {
-        bf16x8_t w[2];
-        if constexpr (sizeof(WT) == 1) {
-          const uint4 v = wa[b][j][0];
-          const uint2 w0 = e4m3x4_to_bf16x4(v.x), w1 = e4m3x4_to_bf16x4(v.y);
-          const uint2 w2 = e4m3x4_to_bf16x4(v.z), w3 = e4m3x4_to_bf16x4(v.w);
-          w[0] = __builtin_bit_cast(bf16x8_t, make_uint4(w0.x, w0.y, w1.x, w1.y));
-          w[1] = __builtin_bit_cast(bf16x8_t, make_uint4(w2.x, w2.y, w3.x, w3.y));
-        } else {
-          w[0] = __builtin_bit_cast(bf16x8_t, wa[b][j][0]);
-          w[1] = __builtin_bit_cast(bf16x8_t, wa[b][j][1]);
         }
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int i = 0; i < RF; ++i)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[s], __builtin_bit_cast(bf16x8_t, xa[b][i][s]),
-                                                                acc[i][j], 0, 0, 0);
-      }
-    }
   };
 
-  int c = wave;
-  if (c < nch) {
-    load(0, c);
-    for (;;) {
-      if (c + WAVES < nch) load(1, c + WAVES);
-      mma(0);
-      if ((c += WAVES) >= nch) break;
-      if (c + WAVES < nch) load(0, c + WAVES);
-      mma(1);
-      if ((c += WAVES) >= nch) break;
+  // This wave's chunks, D at a time.  No branch stands between the loads of the
+  // loop, so that the wait for one chunk leaves the later ones in flight.
+  int c = wave, n = (nch - wave + WAVES - 1) / WAVES;
+  if (n >= D) {
+#pragma unroll
+    for (int b = 0; b < D; ++b) load(b, c + b * WAVES);
+    for (; n >= 2 * D; n -= D, c += D * WAVES) {
+#pragma unroll
+      for (int b = 0; b < D; ++b) {
+        mma(b);
+        load(b, c + (b + D) * WAVES);
+      }
     }
+#pragma unroll
+    for (int b = 0; b < D; ++b) {
+      mma(b);
+      if (b < n - D) load(b, c + (b + D) * WAVES);
+    }
+    n -= D;
+  } else {
+#pragma unroll
+    for (int b = 0; b < D - 1; ++b)
+      if (b < n) load(b, c + b * WAVES);
+  }
+#pragma unroll
+  for (int b = 0; b < D - 1; ++b)
+    if (b < n) mma(b);
+  if (K % KC && wave == nch % WAVES) {
+    const int k0 = nch * KC;
+#pragma unroll
+    for (int j = 0; j < CF; ++j)
+#pragma unroll
+      for (int q = 0; q < WQ; ++q)
+        wa[0][j][q] = load16_end<ALIGNED>(wr[j] + k0 + q * 4 * WP, K - k0 - (q * 4 + lq) * WP);
+#pragma unroll
+    for (int i = 0; i < RF; ++i)
+#pragma unroll
+      for (int q = 0; q < XQ; ++q)
+        xa[0][i][q] = load16_end<ALIGNED>(xr[i] + k0 + q * 4 * XP, K - k0 - (q * 4 + lq) * XP);
+    mma(0);
   }
 
   // lane: output row rr of a fragment, four consecutive columns 4 hh ..
+  __syncthreads();  // the sums take the chunks' place
+  float* part = reinterpret_cast<float*>(smem);
 #pragma unroll
   for (int i = 0; i < RF; ++i)
 #pragma unroll
     for (int j = 0; j < CF; ++j)
-      *reinterpret_cast<f32x4_t*>(&part[wave][i * 16 + rr][j * 16 + hh * 4]) = acc[i][j];
+      *reinterpret_cast<f32x4_t*>(part + (wave * TM + i * 16 + rr) * PITCH + j * 16 + hh * 4) = acc[i][j];
   __syncthreads();
   for (int e = tid; e < TM * (TN / 4); e += WAVES * 64) {
     const int r = e / (TN / 4), q = (e % (TN / 4)) * 4;
     if (m0 + r >= p.m || n0 + q >= p.n) continue;
-    float4 s = *reinterpret_cast<const float4*>(&part[0][r][q]);
+    float4 s = *reinterpret_cast<const float4*>(part + r * PITCH + q);
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) {
-      const float4 v = *reinterpret_cast<const float4*>(&part[w][r][q]);
+      const float4 v = *reinterpret_cast<const float4*>(part + (w * TM + r) * PITCH + q);
       s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
     }
     linear_out4(p, m0 + r, n0 + q, p.n - n0 - q, s);
   }
 }
 
-template <typename XT, typename WT, int RF, int CF, bool ALIGNED>
+template <typename XT, typename WT, int RF, int CF, int WAVES, int D, bool ALIGNED>
 static hipError_t rows_launch(const LinearArgs& p, hipStream_t s) {
   const int64_t tiles = (int64_t)((p.m + RF * 16 - 1) / (RF * 16)) * ((p.n + CF * 16 - 1) / (CF * 16));
   const int64_t grid = ((tiles + 7) / 8) * 8;
   if (grid > INT_MAX) return hipErrorInvalidValue;
-  linear_rows_kernel<XT, WT, RF, CF, 8, ALIGNED><<<(unsigned)grid, 512, 0, s>>>(p);
+  linear_rows_kernel<XT, WT, RF, CF, WAVES, D, ALIGNED><<<(unsigned)grid, WAVES * 64, 0, s>>>(p);
   return hipGetLastError();
 }
 
+// The tile with the least to load for the busiest CU: ceil(tiles / CUs) tiles of
+// 16 (RF + CF) rows of K, at about 76 GB/s per CU, equal: the larger tile.  us
+// of the choice and of the next best ones, operands in the Infinity Cache:
+// 64 x 4096 x 4096 2x2 9.2, 1x4 10.5, 4x1 11.1, 4x2 12.6; 512 x 256 x 7168 1x2
+// 12.0, 2x1 12.3, 2x2 13.5, 1x1 15.9; 128 x 4096 x 4096 2x4 12.9, 4x2 13.0, 2x2
+// 14.9; 32 x 256 x 2048 1x1 4.6, 2x1 5.0, 2x2 5.4.
 template <typename XT, typename WT, bool ALIGNED>
-static hipError_t rows_tile(const LinearArgs& p, hipStream_t s) {
-  if (p.m <= 16) return rows_launch<XT, WT, 1, 1, ALIGNED>(p, s);
-  if (p.m <= 32) return rows_launch<XT, WT, 2, 1, ALIGNED>(p, s);
-  if (p.n <= 64) return rows_launch<XT, WT, 2, 4, ALIGNED>(p, s);
-  return rows_launch<XT, WT, 4, 2, ALIGNED>(p, s);
+static hipError_t rows_tile(const LinearArgs& p, int ncu, hipStream_t s) {
+  constexpr int kShapes[][2] = {{2, 4}, {4, 2}, {2, 2}, {2, 1}, {1, 2}, {1, 1}};
+  int best = 0;
+  int64_t least = INT64_MAX;
+  for (int i = 0; i < 6; ++i) {
+    const int rf = kShapes[i][0], cf = kShapes[i][1];
+    const int64_t tiles = ((int64_t)(p.m + rf * 16 - 1) / (rf * 16)) * ((p.n + cf * 16 - 1) / (cf * 16));
+    const int64_t load = (tiles + ncu - 1) / ncu * (rf + cf);
+    if (load < least) {
+      least = load;
+      best = i;
+    }
+  }
+  switch (best) {
+    case 0: return rows_launch<XT, WT, 2, 4, 4, 2, ALIGNED>(p, s);
+    case 1: return rows_launch<XT, WT, 4, 2, 4, 2, ALIGNED>(p, s);
+    case 2: return rows_launch<XT, WT, 2, 2, 4, 2, ALIGNED>(p, s);
+    case 3: return rows_launch<XT, WT, 2, 1, 4, 4, ALIGNED>(p, s);
+    case 4: return rows_launch<XT, WT, 1, 2, 4, 4, ALIGNED>(p, s);
+    default: return rows_launch<XT, WT, 1, 1, 8, 4, ALIGNED>(p, s);
+  }
 }
 
 template <typename XT, typename WT>
-static hipError_t rows_align(const LinearArgs& p, hipStream_t s) {
-  const bool aligned = p.aligned;
-  return aligned ? rows_tile<XT, WT, true>(p, s) : rows_tile<XT, WT, false>(p, s);
+static hipError_t rows_align(const LinearArgs& p, int ncu, hipStream_t s) {
+  return p.aligned ? rows_tile<XT, WT, true>(p, ncu, s) : rows_tile<XT, WT, false>(p, ncu, s);
 }
 
 // Tiles need aligned rows, and offsets within a tile that fit 32 bits.
 bool linear_uses_tiles(const LinearArgs& p) {
   if (p.w_dtype == kF32 || !p.aligned) return false;
-  if (std::max(p.ldx, p.ldw) > (1 << 22)) return false;
+  if (std::max({p.ldx, p.ldw, p.ldy, p.res ? p.ldr : 0}) >= 1 << 22) return false;
   return p.m > 64 && p.n > 64;
 }
 
 hipError_t launch_linear(const LinearArgs& p, int nwg, float* scratch, int64_t scratch_floats, hipStream_t s) {
   if (linear_uses_tiles(p))
     return launch_linear_tiles(p, linear_cut(p.m, p.n, p.k, p.w_dtype == kFP8, nwg, scratch_floats), nwg, scratch, s);
-  if (p.w_dtype == kF32) return rows_align<float, float>(p, s);
-  if (p.w_dtype == kBF16) return rows_align<uint16_t, uint16_t>(p, s);
-  return rows_align<uint16_t, uint8_t>(p, s);
+  if (p.w_dtype == kF32) return rows_align<float, float>(p, nwg, s);
+  if (p.w_dtype == kBF16) return rows_align<uint16_t, uint16_t>(p, nwg, s);
+  return rows_align<uint16_t, uint8_t>(p, nwg, s);
 }
 
 }  // namespace aep

@@ -1,6 +1,8 @@
 // The epilogue of the dense product, shared by its kernels.
 #pragma once
 
+#include <type_traits>
+
 #include "aep_device.h"
 #include "aep_internal.h"
 
@@ -79,25 +81,37 @@ __device__ __forceinline__ float linear_fn(int fn, float v) {
 }
 
 // The activation for bf16 results, short enough to be laid out for every value
-// of a tile: SILU and GELU_TANH as v / (1 + e^-u), u = v (c0 + c1 v^2), with the
-// hardware's exponential and reciprocal (2^-20 at |u| < 20; beyond, one of 1
+// of a tile: SILU and GELU_TANH as v / (1 + e^-u), with the hardware's exponential and reciprocal (2^-20 at |u| < 20; beyond, one of 1
 // and e^-u is lost); GELU with erf from Abramowitz and Stegun 7.1.26, whose
 // error is at most 1.5e-7 (half of it here, times |v|).
-__device__ __forceinline__ float linear_fn_bf16(int fn, float c0, float c1, float v) {
-  if (fn == kFnNone) return v;
-  if (fn == kFnRelu) return v > 0.f ? v : v == v ? 0.f : v;
-  if (fn == kFnGelu) {
-    const float z = fabsf(v) * 0.70710678f;
-    const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * z);
-    const float q = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
-    const float tail = 0.5f * q * __expf(-z * z);  // Phi(-|v|)
-    return v * (v > 0.f ? 1.f - tail : tail);
+template <int FN>
+__device__ __forceinline__ float linear_fn_bf16(float v) {
+  if constexpr (FN == kFnNone) return v;
+  if constexpr (FN == kFnRelu) return v > 0.f ? v : v == v ? 0.f : v;
+  if constexpr (FN == kFnSilu) return v * __builtin_amdgcn_rcpf(1.f + __expf(-v));
+  if constexpr (FN == kFnGeluTanh) {
+    constexpr float c0 = 2.f * 0.79788456f, c1 = 2.f * 0.79788456f * 0.044715f;
+    return v * __builtin_amdgcn_rcpf(1.f + __expf(-v * (c0 + c1 * v * v)));
   }
-  return v * __builtin_amdgcn_rcpf(1.f + __expf(-v * (c0 + c1 * v * v)));
+  const float z = fabsf(v) * 0.70710678f;
+  const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * z);
+  const float q = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+  const float tail = 0.5f * q * __expf(-z * z);  // Phi(-|v|)
+  return v * (v > 0.f ? 1.f - tail : tail);
 }
-__device__ __forceinline__ void linear_fn_coefs(int fn, float& c0, float& c1) {
-  c0 = fn == kFnGeluTanh ? 2.f * 0.79788456f : 1.f;
-  c1 = fn == kFnGeluTanh ? 2.f * 0.79788456f * 0.044715f : 0.f;
+// Calls f(activation) with the activation as a constant.
+template <typename F>
+__device__ __forceinline__ void by_fn(int fn, F f) {
+  if (fn == kFnNone)
+    f(std::integral_constant<int, kFnNone>{});
+  else if (fn == kFnRelu)
+    f(std::integral_constant<int, kFnRelu>{});
+  else if (fn == kFnSilu)
+    f(std::integral_constant<int, kFnSilu>{});
+  else if (fn == kFnGelu)
+    f(std::integral_constant<int, kFnGelu>{});
+  else
+    f(std::integral_constant<int, kFnGeluTanh>{});
 }
 
 // Four columns [c, c + 4) of row m: bias, activation, residual, one rounding.

@@ -25,16 +25,19 @@ _SCORE = {"softmax": L.AEP_SCORE_SOFTMAX, "sigmoid": L.AEP_SCORE_SIGMOID}
 
 
 def _rows(t: torch.Tensor, name: str, dtypes, shape, device) -> None:
-    """A matrix on ``device`` whose rows are contiguous."""
+    """A matrix (or vector) on ``device`` whose rows are contiguous and apart."""
     if not isinstance(t, torch.Tensor) or t.device != device:
         raise ValueError(f"{name} must be a tensor on {device}")
     if t.dtype not in dtypes:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {' or '.join(map(str, dtypes))}")
-    if t.dim() != len(shape) or any(s is not None and a != s for a, s in zip(t.shape, shape)):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
+    have = t.shape
+    if len(have) != len(shape) or have[-1] != shape[-1] and shape[-1] is not None or \
+            have[0] != shape[0] and shape[0] is not None:
+        raise ValueError(f"{name} has shape {tuple(have)}, expected {shape}")
+    step = t.stride()
+    if step[-1] != 1 and have[-1] > 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    if t.dim() == 2 and t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    if len(have) == 2 and have[0] > 1 and step[0] < have[1]:
         raise ValueError(f"{name}: rows must not overlap")
 
 
@@ -43,21 +46,10 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-class _on:
-    """Makes a device the current one for a call, where it is not already."""
-
-    __slots__ = ("guard",)
-
-    def __init__(self, device: torch.device):
-        self.guard = None if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+# The raw current stream of a device: torch builds a Stream object around it
+# otherwise, which takes longer than everything else here but the launch.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 class Linear:
@@ -101,46 +93,51 @@ class Linear:
                        L.AEP_F32 if bias is None else _CODE[bias.dtype])
         self._fn = _FN[activation]
         self._ldw = _ld(weight)
-        self._ws_need = {}  # bytes of scratch by (m, row strides)
-        self._desc = L.LinearDesc()
-        self._at = ctypes.byref(self._desc)
+        self._calls = {}  # by sizes, strides and types: the description of such a call and its bytes of scratch
 
     def __call__(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None,
                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x [m, k] -> [m, n].  residual [m, n] float32 or bfloat16; out may be
-        the residual itself, and must not overlap anything else.  Not to be
-        called on one object from two threads at once."""
-        dev = self.device
+        the residual itself, and must not overlap anything else."""
+        dev, n = self.device, self.n
+        if dev.index != torch.cuda.current_device():
+            with torch.cuda.device(dev):
+                return self(x, residual, out)
         _rows(x, "x", (self.x_dtype,), (None, self.k), dev)
-        m, n = x.shape[0], self.n
-        if residual is not None:
-            _rows(residual, "residual", (torch.float32, torch.bfloat16), (m, n), dev)
-        if out is not None:
+        m = x.shape[0]
+        if out is None:
+            out = torch.empty((m, n), dtype=self.out_dtype, device=dev)
+        else:
             _rows(out, "out", (self.out_dtype,), (m, n), dev)
-        with _on(dev):
-            if out is None:
-                out = torch.empty((m, n), dtype=self.out_dtype, device=dev)
-            d = self._desc
-            ldx, ldy = _ld(x), _ld(out)
-            (d.n, d.k, d.x_dtype, d.w_dtype, d.y_dtype, d.bias_dtype) = self._fixed
-            d.m, d.fn, d.ldx, d.ldw, d.ldy = m, self._fn, ldx, self._ldw, ldy
-            if residual is not None:
-                d.res_dtype, d.ldr = _CODE[residual.dtype], _ld(residual)
-            else:
-                d.res_dtype, d.ldr = L.AEP_F32, n
-            need = self._ws_need.get((m, ldx))
-            if need is None:
-                b = ctypes.c_size_t()
-                L.check(self._lib.aep_linear_workspace(self._at, ctypes.byref(b)), "aep_linear_workspace")
-                need = self._ws_need[(m, ldx)] = b.value
-            ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-            L.check(self._lib.aep_linear(
-                self._at, x.data_ptr(), self.weight.data_ptr(), None if self.scale is None else self.scale.data_ptr(),
-                None if self.bias is None else self.bias.data_ptr(),
-                None if residual is None else residual.data_ptr(), out.data_ptr(),
-                None if ws is None else ws.data_ptr(), need,
-                torch.cuda.current_stream().cuda_stream), "aep_linear")
+        if residual is None:
+            key = (m, x.stride(0), out.stride(0))
+        else:
+            _rows(residual, "residual", (torch.float32, torch.bfloat16), (m, n), dev)
+            key = (m, x.stride(0), out.stride(0), residual.stride(0), residual.dtype)
+        call = self._calls.get(key) or self._describe(key, x, residual, out)
+        need = call[1]
+        ws = torch.empty(need, dtype=torch.uint8, device=dev).data_ptr() if need else None
+        scale, bias = self.scale, self.bias
+        st = self._lib.aep_linear(call[0], x.data_ptr(), self.weight.data_ptr(),
+                                  None if scale is None else scale.data_ptr(),
+                                  None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(),
+                                  out.data_ptr(), ws, need, _raw_stream(dev.index))
+        if st:
+            L.check(st, "aep_linear")
         return out
+
+    def _describe(self, key, x, residual, out):
+        """(description, bytes of scratch) of a call, kept for the next ones like it."""
+        n, k, x_dtype, w_dtype, y_dtype, bias_dtype = self._fixed
+        d = L.LinearDesc(key[0], n, k, x_dtype, w_dtype, y_dtype, bias_dtype,
+                         L.AEP_F32 if residual is None else _CODE[residual.dtype], self._fn, _ld(x), self._ldw,
+                         _ld(out), n if residual is None else _ld(residual))
+        b = ctypes.c_size_t()
+        L.check(self._lib.aep_linear_workspace(ctypes.byref(d), ctypes.byref(b)), "aep_linear_workspace")
+        if len(self._calls) >= 1024:
+            self._calls.clear()
+        call = self._calls[key] = (ctypes.byref(d), b.value)
+        return call
 
 
 def linear(x: torch.Tensor, weight: torch.Tensor, *, scale: Optional[torch.Tensor] = None,
@@ -183,23 +180,27 @@ def route(router: Router, logits: torch.Tensor, bias: Optional[torch.Tensor] = N
     if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
         raise ValueError("logits must be a CUDA (HIP) tensor")
     dev = logits.device
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            return route(router, logits, bias, idx=idx, weights=weights, flag=flag)
     _rows(logits, "logits", (torch.float32,), (None, router.n_experts), dev)
     T, k = logits.shape[0], router.top_k
     if bias is not None:
         _rows(bias, "bias", (torch.float32,), (router.n_experts,), dev)
-    for t, name, dtype, shape in ((idx, "idx", torch.int32, (T, k)), (weights, "weights", torch.float32, (T, k)),
-                                  (flag, "flag", torch.int32, (1,))):
-        if t is not None:
-            _rows(t, name, (dtype,), shape, dev)
-            if not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous")
-    with _on(dev):
-        if idx is None:
-            idx = torch.empty((T, k), dtype=torch.int32, device=dev)
-        if weights is None:
-            weights = torch.empty((T, k), dtype=torch.float32, device=dev)
-        L.check(router._lib.aep_route_topk(
-            router._at, logits.data_ptr(), _ld(logits), None if bias is None else bias.data_ptr(),
-            T, idx.data_ptr(), weights.data_ptr(), None if flag is None else flag.data_ptr(),
-            torch.cuda.current_stream().cuda_stream), "aep_route_topk")
+    if idx is not None or weights is not None or flag is not None:
+        for t, name, dtype, shape in ((idx, "idx", torch.int32, (T, k)), (weights, "weights", torch.float32, (T, k)),
+                                      (flag, "flag", torch.int32, (1,))):
+            if t is not None:
+                _rows(t, name, (dtype,), shape, dev)
+                if not t.is_contiguous():
+                    raise ValueError(f"{name} must be contiguous")
+    if idx is None:
+        idx = torch.empty((T, k), dtype=torch.int32, device=dev)
+    if weights is None:
+        weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+    st = router._lib.aep_route_topk(
+        router._at, logits.data_ptr(), _ld(logits), None if bias is None else bias.data_ptr(), T, idx.data_ptr(),
+        weights.data_ptr(), None if flag is None else flag.data_ptr(), _raw_stream(dev.index))
+    if st:
+        L.check(st, "aep_route_topk")
     return idx, weights
