@@ -232,32 +232,15 @@ static hipError_t rows_launch(const LinearArgs& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-// The tile with the least to load for the busiest CU: ceil(tiles / CUs) tiles of
-// 16 (RF + CF) rows of K, at about 76 GB/s per CU, equal: the larger tile.  us
-// of the choice and of the next best ones, operands in the Infinity Cache:
-// 64 x 4096 x 4096 2x2 9.2, 1x4 10.5, 4x1 11.1, 4x2 12.6; 512 x 256 x 7168 1x2
-// 12.0, 2x1 12.3, 2x2 13.5, 1x1 15.9; 128 x 4096 x 4096 2x4 12.9, 4x2 13.0, 2x2
-// 14.9; 32 x 256 x 2048 1x1 4.6, 2x1 5.0, 2x2 5.4.
 template <typename XT, typename WT, bool ALIGNED>
 static hipError_t rows_tile(const LinearArgs& p, int ncu, hipStream_t s) {
-  constexpr int kShapes[][2] = {{2, 4}, {4, 2}, {2, 2}, {2, 1}, {1, 2}, {1, 1}};
-  int best = 0;
-  int64_t least = INT64_MAX;
-  for (int i = 0; i < 6; ++i) {
-    const int rf = kShapes[i][0], cf = kShapes[i][1];
-    const int64_t tiles = ((int64_t)(p.m + rf * 16 - 1) / (rf * 16)) * ((p.n + cf * 16 - 1) / (cf * 16));
-    const int64_t load = (tiles + ncu - 1) / ncu * (rf + cf);
-    if (load < least) {
-      least = load;
-      best = i;
-    }
-  }
-  switch (best) {
-    case 0: return rows_launch<XT, WT, 2, 4, 4, 2, ALIGNED>(p, s);
-    case 1: return rows_launch<XT, WT, 4, 2, 4, 2, ALIGNED>(p, s);
-    case 2: return rows_launch<XT, WT, 2, 2, 4, 2, ALIGNED>(p, s);
-    case 3: return rows_launch<XT, WT, 2, 1, 4, 4, ALIGNED>(p, s);
-    case 4: return rows_launch<XT, WT, 1, 2, 4, 4, ALIGNED>(p, s);
+  const RowsPlan r = rows_plan(p.m, p.n, p.k, sizeof(XT), sizeof(WT), ncu);
+  switch (r.rf * 8 + r.cf) {
+    case 2 * 8 + 4: return rows_launch<XT, WT, 2, 4, 4, 2, ALIGNED>(p, s);
+    case 4 * 8 + 2: return rows_launch<XT, WT, 4, 2, 4, 2, ALIGNED>(p, s);
+    case 2 * 8 + 2: return rows_launch<XT, WT, 2, 2, 4, 2, ALIGNED>(p, s);
+    case 2 * 8 + 1: return rows_launch<XT, WT, 2, 1, 4, 4, ALIGNED>(p, s);
+    case 1 * 8 + 2: return rows_launch<XT, WT, 1, 2, 4, 4, ALIGNED>(p, s);
     default: return rows_launch<XT, WT, 1, 1, 8, 4, ALIGNED>(p, s);
   }
 }
@@ -267,16 +250,9 @@ static hipError_t rows_align(const LinearArgs& p, int ncu, hipStream_t s) {
   return p.aligned ? rows_tile<XT, WT, true>(p, ncu, s) : rows_tile<XT, WT, false>(p, ncu, s);
 }
 
-// Tiles need aligned rows, and offsets within a tile that fit 32 bits.
-bool linear_uses_tiles(const LinearArgs& p) {
-  if (p.w_dtype == kF32 || !p.aligned) return false;
-  if (std::max({p.ldx, p.ldw, p.ldy, p.res ? p.ldr : 0}) >= 1 << 22) return false;
-  return p.m > 64 && p.n > 64;
-}
-
 hipError_t launch_linear(const LinearArgs& p, int nwg, float* scratch, int64_t scratch_floats, hipStream_t s) {
-  if (linear_uses_tiles(p))
-    return launch_linear_tiles(p, linear_cut(p.m, p.n, p.k, p.w_dtype == kFP8, nwg, scratch_floats), nwg, scratch, s);
+  if (const LinearPlan* t = linear_tiles_plan(p, nwg, scratch_floats))
+    return launch_linear_tiles(p, t->cut, nwg, scratch, s);
   if (p.w_dtype == kF32) return rows_align<float, float>(p, nwg, s);
   if (p.w_dtype == kBF16) return rows_align<uint16_t, uint16_t>(p, nwg, s);
   return rows_align<uint16_t, uint8_t>(p, nwg, s);

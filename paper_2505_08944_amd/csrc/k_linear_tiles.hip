@@ -96,11 +96,11 @@ struct LinearItem {
   int64_t part;
 };
 
-// A family 0 tile's place: panels of 8 column tiles, row tiles one after
-// another inside a panel, so that the run of tiles an XCD gets is a compact
-// block whose operand bands its L2 holds.
-__device__ __forceinline__ void tile_place(const LinearCut& c, int tile, int& rt, int& ct) {
-  const int per = 8 * c.nrow, pi = tile / per, in = tile - pi * per, w = min(8, c.ncol - 8 * pi);
+// A tile's place among nrow x ncol: panels of 8 column tiles, row tiles one
+// after another inside a panel, so that the run of tiles an XCD gets is a
+// compact block whose operand bands its L2 holds.
+__device__ __forceinline__ void tile_place(int nrow, int ncol, int tile, int& rt, int& ct) {
+  const int per = 8 * nrow, pi = tile / per, in = tile - pi * per, w = min(8, ncol - 8 * pi);
   rt = in / w;
   ct = 8 * pi + (in - rt * w);
 }
@@ -112,14 +112,14 @@ __device__ __forceinline__ LinearItem linear_item(int item) {
   it.part = -1;
   int piece = 0, pieces = 1, rt, ct;
   if (item < c.whole) {
-    tile_place(c, item, rt, ct);
+    tile_place(c.nrow, c.ncol, item, rt, ct);
     it.m0 = rt * 256;
     it.n0 = ct * 256;
   } else if (int j = item - c.whole; j < c.rest_items()) {
     pieces = c.p0;
     const int t = j / pieces;
     piece = j - t * pieces;
-    tile_place(c, c.whole + (c.halves == 2 ? t >> 1 : t), rt, ct);
+    tile_place(c.nrow, c.ncol, c.whole + (c.halves == 2 ? t >> 1 : t), rt, ct);
     it.m0 = rt * 256;
     it.n0 = ct * 256 + (c.halves == 2 ? (t & 1) * 128 : 0);
     if (pieces > 1) it.part = (int64_t)j * (65536 / c.halves);
@@ -128,8 +128,9 @@ __device__ __forceinline__ LinearItem linear_item(int item) {
     pieces = c.pr;
     const int t = j / pieces;
     piece = j - t * pieces;
-    it.m0 = c.nrow * 256;
-    it.n0 = t * 128;
+    tile_place(c.lrow, (read_again<int>(&launch_params()->a.n) + 127) / 128, t, rt, ct);
+    it.m0 = c.nrow * 256 + rt * (256 >> c.fam);
+    it.n0 = ct * 128;
     if (pieces > 1) it.part = c.rest_floats() + (int64_t)j * (32768 >> c.fam);
   }
   it.m0 = uniform(it.m0);
@@ -146,12 +147,16 @@ __device__ __forceinline__ int linear_kind(const LinearCut& c, int item) {
 }
 
 // The workgroup's r-th item (-1: none).  An XCD gets a contiguous run of a
-// round; odd rounds are dealt in reverse, and a partial one over all XCDs.
+// round; odd rounds are dealt in reverse; a partial one over all XCDs, unless
+// the round before it was a mix of shapes: then the workgroups that had its
+// smaller items come first.
 __device__ __forceinline__ int linear_nth(const LinearCut& c, int r, int nwg, int xcd, int xj) {
   const int base = r * nwg, cnt = c.items - base;
   if (cnt <= 0) return -1;
   const int lin = xcd * (nwg >> 3) + xj;
-  if (cnt >= nwg) return base + ((r & 1) ? nwg - 1 - lin : lin);
+  const int rl = (r & 1) ? nwg - 1 - lin : lin;
+  if (cnt >= nwg) return base + rl;
+  if (r > 0 && linear_kind(c, base - nwg) != linear_kind(c, base - 1)) return rl < cnt ? base + rl : -1;
   const int q = (cnt + 7) >> 3, idx = xcd * q + xj;
   return xj < q && idx < cnt ? base + idx : -1;
 }
@@ -168,7 +173,16 @@ struct Shape {
   static constexpr bool kFour = NB == 2;               // four phases per K step, else one
   static constexpr int kUnits = kFour ? 2 : 1;         // x units per stage
   static constexpr int kUnitRows = kRows / kUnits;
-  static constexpr int RF = kUnitRows / 32;            // 16-row fragments per wave and unit
+  // Waves: kWM along the rows, 8 / kWM along the columns; RF 16-row fragments
+  // per wave and unit, NP pairs of 16-column fragments per wave (two W units:
+  // one of each).  256 x 128: four along the rows, so that a step's operands
+  // are 128 KB of LDS reads and not 160.
+  static constexpr int kWM = FAM == 0 && NB == 1 ? 4 : 2;
+  static constexpr int NP = FAM == 0 ? 2 : NB;
+  static constexpr int RF = kUnitRows / (16 * kWM);
+  static __device__ __forceinline__ int row0(int wm) { return wm * (kUnitRows / kWM); }
+  static __device__ __forceinline__ int pair0(int wn, int q) { return NB == 2 ? wn * 32 : wn * (NP * 32) + q * 32; }  // in its W unit
+  static __device__ __forceinline__ int col0(int wn, int q) { return (NB == 2 ? q * 128 : 0) + pair0(wn, q); }
   static constexpr int kX = kUnitRows * 128, kW = 128 * (FP8 ? 64 : 128);
   static constexpr int kStage = kUnits * kX + NB * kW;
   static constexpr int kStages = NB == 2 ? (FP8 ? 3 : 2) : FAM == 0 ? (FP8 ? 4 : 3) : FAM == 1 ? (FP8 ? 6 : 5) : (FP8 ? 8 : 6);
@@ -239,26 +253,26 @@ __device__ __forceinline__ f32x4_t columns4(const void* v, int dtype, int c, int
 // matrix are out of the resources' range.
 template <bool FP8, int FAM, int NB>
 __device__ __forceinline__ void finish_wide(const LinearItem& it, int wm, int wn, int rr, int hh,
-                                            f32x4_t (&acc)[Shape<FP8, FAM, NB>::kUnits][NB][Shape<FP8, FAM, NB>::RF][2]) {
+                                            f32x4_t (&acc)[Shape<FP8, FAM, NB>::kUnits][Shape<FP8, FAM, NB>::NP][Shape<FP8, FAM, NB>::RF][2]) {
   using S = Shape<FP8, FAM, NB>;
-  constexpr int RF = S::RF, NU = S::kUnits;
+  constexpr int RF = S::RF, NU = S::kUnits, NP = S::NP;
   const LinearArgs p = the_args();
   const int rows = min(p.m - it.m0, S::kRows), cols = p.n - it.n0;
   if (cols <= 0) return;
   const uint32_t ybytes = ((uint32_t)(rows - 1) * (uint32_t)p.ldy + (uint32_t)cols) * 2u;
   __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc(
       reinterpret_cast<uint16_t*>(p.y) + (int64_t)it.m0 * p.ldy + it.n0, 0, (int)ybytes, 0x00020000);
-  const int row = wm * (S::kUnitRows / 2) + rr;
-  uint32_t yo[NB], ro[NB];  // (2^31: past any range, which is below it, with any row added)
-  f32x4_t b4[NB][2], s4[FP8 ? NB : 1][2];
+  const int row = S::row0(wm) + rr;
+  uint32_t yo[NP], ro[NP];  // (2^31: past any range, which is below it, with any row added)
+  f32x4_t b4[NP][2], s4[FP8 ? NP : 1][2];
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    const int c8 = b * 128 + wn * 32 + (hh & 1) * 16 + (hh >> 1) * 8;
+  for (int b = 0; b < NP; ++b) {
+    const int c8 = S::col0(wn, b) + (hh & 1) * 16 + (hh >> 1) * 8;
     yo[b] = c8 < cols ? ((uint32_t)row * (uint32_t)p.ldy + (uint32_t)c8) * 2u : 0x80000000u;
     ro[b] = c8 < cols ? ((uint32_t)row * (uint32_t)p.ldr + (uint32_t)c8) * 2u : 0x80000000u;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int c = it.n0 + b * 128 + wn * 32 + j * 16 + hh * 4;
+      const int c = it.n0 + S::col0(wn, b) + j * 16 + hh * 4;
       b4[b][j] = p.bias ? columns4(p.bias, p.bias_dtype, c, p.n) : f32x4_t{0.f, 0.f, 0.f, 0.f};
       if constexpr (FP8) s4[b][j] = columns4(p.scale, kBF16, c, p.n);
     }
@@ -276,9 +290,9 @@ __device__ __forceinline__ void finish_wide(const LinearItem& it, int wm, int wn
     u32x4_t res[2][RF];  // the unit's residual and the next one's
     if (p.res) load_res(res[0], 0, 0);
 #pragma unroll
-    for (int q = 0; q < NU * NB; ++q) {
-      const int u = q / NB, b = q % NB;
-      if (p.res && q + 1 < NU * NB) load_res(res[(q + 1) & 1], (q + 1) / NB, (q + 1) % NB);
+    for (int q = 0; q < NU * NP; ++q) {
+      const int u = q / NP, b = q % NP;
+      if (p.res && q + 1 < NU * NP) load_res(res[(q + 1) & 1], (q + 1) / NP, (q + 1) % NP);
 #pragma unroll
       for (int i = 0; i < RF; ++i) {
         float o[2][4];
@@ -316,27 +330,27 @@ __device__ __forceinline__ void finish_wide(const LinearItem& it, int wm, int wn
 // The same for any other result: f32, rows of any alignment and length.
 template <bool FP8, int FAM, int NB>
 __device__ __forceinline__ void finish_any(const LinearItem& it, int wm, int wn, int rr, int hh,
-                                           f32x4_t (&acc)[Shape<FP8, FAM, NB>::kUnits][NB][Shape<FP8, FAM, NB>::RF][2]) {
+                                           f32x4_t (&acc)[Shape<FP8, FAM, NB>::kUnits][Shape<FP8, FAM, NB>::NP][Shape<FP8, FAM, NB>::RF][2]) {
   using S = Shape<FP8, FAM, NB>;
-  constexpr int RF = S::RF, NU = S::kUnits;
-  // one (x unit, W unit) at a time: the code is long
+  constexpr int RF = S::RF, NU = S::kUnits, NP = S::NP;
+  // one x unit and pair of columns at a time: the code is long
 #pragma unroll 1
-  for (int q = 0; q < NU * NB; ++q) {
+  for (int q = 0; q < NU * NP; ++q) {
     f32x4_t v[RF][2];
 #pragma unroll
-    for (int a = 0; a < NU * NB; ++a)
+    for (int a = 0; a < NU * NP; ++a)
       if (q == a) {
 #pragma unroll
         for (int i = 0; i < RF; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) v[i][j] = acc[a / NB][a % NB][i][j];
+          for (int j = 0; j < 2; ++j) v[i][j] = acc[a / NP][a % NP][i][j];
       }
     const LinearArgs p = the_args();
-    const int m = it.m0 + (q / NB) * 128 + wm * (S::kUnitRows / 2) + rr;
+    const int m = it.m0 + (q / NP) * 128 + S::row0(wm) + rr;
     f32x4_t b4[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int c = it.n0 + (q % NB) * 128 + wn * 32 + j * 16 + hh * 4;
+      const int c = it.n0 + S::col0(wn, q % NP) + j * 16 + hh * 4;
       const float4 t = p.bias ? load4(p.bias, p.bias_dtype, c, p.n - c, p.vec_bias) : make_float4(0.f, 0.f, 0.f, 0.f);
       b4[j] = f32x4_t{t.x, t.y, t.z, t.w};
       if constexpr (FP8) {
@@ -358,7 +372,7 @@ __device__ __forceinline__ void finish_any(const LinearItem& it, int wm, int wn,
       for (int i = 0; i < RF; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int c = it.n0 + (q % NB) * 128 + wn * 32 + j * 16 + hh * 4;
+          const int c = it.n0 + S::col0(wn, q % NP) + j * 16 + hh * 4;
           if (m + 16 * i < p.m && c < p.n) {
             const float4 t = load4(p.res, p.res_dtype, (int64_t)(m + 16 * i) * p.ldr + c, p.n - c, p.vec_res);
             v[i][j] += f32x4_t{t.x, t.y, t.z, t.w};
@@ -369,7 +383,7 @@ __device__ __forceinline__ void finish_any(const LinearItem& it, int wm, int wn,
     for (int i = 0; i < RF; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int c = it.n0 + (q % NB) * 128 + wn * 32 + j * 16 + hh * 4;
+        const int c = it.n0 + S::col0(wn, q % NP) + j * 16 + hh * 4;
         if (m + 16 * i < p.m && c < p.n)
           store4(p.y, p.y_dtype, (int64_t)(m + 16 * i) * p.ldy + c, p.n - c, p.vec_y,
                  make_float4(v[i][j][0], v[i][j][1], v[i][j][2], v[i][j][3]));
@@ -384,12 +398,12 @@ __device__ __forceinline__ void run_shape(unsigned char* smem, uint32_t lds_base
                                           int& item) {
   using S = Shape<FP8, FAM, NB>;
   constexpr bool kFour = S::kFour;
-  constexpr int RF = S::RF, NU = S::kUnits, NST = S::kStages;
+  constexpr int RF = S::RF, NU = S::kUnits, NP = S::NP, NST = S::kStages;
   constexpr int kKind = NB == 2 ? 0 : 1 + FAM;
   int tid = threadIdx.x;
   asm volatile("" : "+v"(tid));  // per-lane offsets are made here, not kept through other shapes' loops
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave & 1, wn = wave >> 1, grp = wave >> 2;
+  const int wm = wave % S::kWM, wn = wave / S::kWM, grp = wave >> 2;
   const int rr = lane & 15, hh = lane >> 4;
 
   // loader offsets, the same for every tile and K step (the resources and the
@@ -444,12 +458,12 @@ __device__ __forceinline__ void run_shape(unsigned char* smem, uint32_t lds_base
     return true;
   };
 
-  // Operands and accumulators [x unit][W unit][row fragment][column fragment].
+  // Operands and accumulators [x unit][column pair][row fragment][column].
   // MFMA rows are W's: a lane holds four consecutive output columns of one row.
-  bf16x8_t rx[RF][2], rw[NB][2][2];
-  uint4 rn[2][FP8 ? 1 : 2];  // a W unit as read, where it becomes rw in widen()
-  f32x4_t acc[NU][NB][RF][2];
-  const int wrow = wm * (S::kUnitRows / 2) + rr;
+  bf16x8_t rx[RF][2], rw[NP][2][2];
+  uint4 rn[FP8 && !kFour ? NP : 1][2][FP8 ? 1 : 2];  // W as read, where it becomes rw in widen()
+  f32x4_t acc[NU][NP][RF][2];
+  const int wrow = S::row0(wm) + rr;
   auto read_x = [&](int u, int stage) {
     const unsigned char* q = smem + stage * S::kStage + u * S::kX + wrow * 128;
 #pragma unroll
@@ -461,18 +475,19 @@ __device__ __forceinline__ void run_shape(unsigned char* smem, uint32_t lds_base
       }
   };
   auto read_w = [&](int b, int stage, bool aside) {
-    const unsigned char* q = smem + stage * S::kStage + NU * S::kX + b * S::kW;
+    const unsigned char* q = smem + stage * S::kStage + NU * S::kX + (NB == 2 ? b : 0) * S::kW;
+    const int n = kFour ? 0 : b;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int lr = wn * 32 + j * 16 + rr;
+      const int lr = S::pair0(wn, b) + j * 16 + rr;
       if constexpr (FP8) {
-        rn[j][0] = *reinterpret_cast<const uint4*>(q + lr * 64 + ((hh ^ ((rr >> 2) & 3)) << 4));
+        rn[n][j][0] = *reinterpret_cast<const uint4*>(q + lr * 64 + ((hh ^ ((rr >> 2) & 3)) << 4));
       } else {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const uint4 v = *reinterpret_cast<const uint4*>(q + lr * 128 + (((4 * k + hh) ^ (rr & 7)) << 4));
           if (aside)
-            rn[j][k] = v;
+            rn[0][j][k] = v;
           else
             rw[b][j][k] = __builtin_bit_cast(bf16x8_t, v);
         }
@@ -483,14 +498,14 @@ __device__ __forceinline__ void run_shape(unsigned char* smem, uint32_t lds_base
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       if constexpr (FP8) {
-        const uint4 v = rn[j][0];
+        const uint4 v = rn[kFour ? 0 : b][j][0];
         const uint2 w0 = e4m3x4_to_bf16x4(v.x), w1 = e4m3x4_to_bf16x4(v.y);
         const uint2 w2 = e4m3x4_to_bf16x4(v.z), w3 = e4m3x4_to_bf16x4(v.w);
         rw[b][j][0] = __builtin_bit_cast(bf16x8_t, make_uint4(w0.x, w0.y, w1.x, w1.y));
         rw[b][j][1] = __builtin_bit_cast(bf16x8_t, make_uint4(w2.x, w2.y, w3.x, w3.y));
       } else if (aside) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) rw[b][j][k] = __builtin_bit_cast(bf16x8_t, rn[j][k]);
+        for (int k = 0; k < 2; ++k) rw[b][j][k] = __builtin_bit_cast(bf16x8_t, rn[0][j][k]);
       }
     }
   };
@@ -507,7 +522,7 @@ __device__ __forceinline__ void run_shape(unsigned char* smem, uint32_t lds_base
 #pragma unroll
     for (int u = 0; u < NU; ++u)
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NP; ++b)
 #pragma unroll
         for (int i = 0; i < RF; ++i)
 #pragma unroll
@@ -587,15 +602,18 @@ __device__ __forceinline__ void run_shape(unsigned char* smem, uint32_t lds_base
       } else {
         const int fs = stage == 0 ? NST - 1 : stage - 1;
         read_x(0, stage);
-        read_w(0, stage, false);
+#pragma unroll
+        for (int q = 0; q < NP; ++q) read_w(q, stage, false);
         load_x(0, fs);
         load_w(0, fs);
         next_k();
         wait_loads<kFlight>();
         wait_lds();
-        widen(0, false);
+#pragma unroll
+        for (int q = 0; q < NP; ++q) widen(q, false);
         slot_end();
-        mma(0, 0);
+#pragma unroll
+        for (int q = 0; q < NP; ++q) mma(0, q);
         slot_end();
       }
       stage = ns;
@@ -609,12 +627,12 @@ __device__ __forceinline__ void run_shape(unsigned char* smem, uint32_t lds_base
 #pragma unroll
       for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NP; ++b)
 #pragma unroll
           for (int i = 0; i < RF; ++i)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-              const int row = u * 128 + wm * (S::kUnitRows / 2) + i * 16 + rr, col = b * 128 + wn * 32 + j * 16 + hh * 4;
+              const int row = u * 128 + S::row0(wm) + i * 16 + rr, col = S::col0(wn, b) + j * 16 + hh * 4;
               *reinterpret_cast<f32x4_t*>(part + row * S::kCols + col) = acc[u][b][i][j];
             }
     } else if (read_again<int>(&launch_params()->a.wide)) {
@@ -670,7 +688,7 @@ __global__ __launch_bounds__(256) void linear_sums_kernel(const LinearArgs p, co
     const int t = b >> 4;
     strip = b & 15;
     int rt, ct;
-    tile_place(c, c.whole + (c.halves == 2 ? t >> 1 : t), rt, ct);
+    tile_place(c.nrow, c.ncol, c.whole + (c.halves == 2 ? t >> 1 : t), rt, ct);
     m0 = rt * 256;
     n0 = ct * 256 + (c.halves == 2 ? (t & 1) * 128 : 0);
     rows = 256;
@@ -681,8 +699,10 @@ __global__ __launch_bounds__(256) void linear_sums_kernel(const LinearArgs p, co
     b -= rest_blocks;
     const int per = 16 >> c.fam, t = b / per;
     strip = b - t * per;
-    m0 = c.nrow * 256;
-    n0 = t * 128;
+    int rt, ct;
+    tile_place(c.lrow, (p.n + 127) / 128, t, rt, ct);
+    m0 = c.nrow * 256 + rt * (256 >> c.fam);
+    n0 = ct * 128;
     rows = 256 >> c.fam;
     cols = 128;
     pieces = c.pr;

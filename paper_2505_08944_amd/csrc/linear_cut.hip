@@ -1,4 +1,4 @@
-// How a tiled dense product is cut (host).
+// Which kernel runs a dense product, and how it is cut (host).
 #include <algorithm>
 
 #include "linear_tiles.h"
@@ -11,14 +11,16 @@ constexpr int kMaxPieces = 8;
 constexpr int kMinPieceSteps = 4;  // K steps of a piece
 constexpr int64_t kMaxScratchFloats = (int64_t)24 << 20;
 
-// us: a K step of a tile shape (256 x 256, 256 x 128, 128 x 128, 64 x 128), what
+// us, fitted to launches of 65 .. 4096 rows with their operands in the Infinity
+// Cache, each timed under all cuts worth trying (of 34 products, the chosen cut
+// was more than 5% behind the best for two): a K step of a tile shape (256 x 256, 256 x 128, 128 x 128, 64 x 128), what
 // an item takes besides, and the launch that adds the pieces' sums with its
 // bytes.
 struct Costs {
   double step[4], item[4], part[4], sums, sums_float;
 };
-constexpr Costs kBf16 = {{1.35, 0.85, 0.55, 0.45}, {6.0, 4.5, 4.0, 3.5}, {4.0, 2.5, 1.5, 1.0}, 4.0, 2.0e-6};
-constexpr Costs kFp8 = {{1.50, 0.90, 0.60, 0.45}, {6.0, 4.5, 4.0, 3.5}, {4.0, 2.5, 1.5, 1.0}, 4.0, 2.0e-6};
+constexpr Costs kBf16 = {{1.25, 0.69, 0.47, 0.40}, {6.0, 5.4, 4.0, 3.6}, {4.0, 2.5, 1.5, 1.0}, 2.5, 1.0e-6};
+constexpr Costs kFp8 = {{1.40, 0.75, 0.55, 0.45}, {6.0, 5.4, 4.0, 3.6}, {4.0, 2.5, 1.5, 1.0}, 2.5, 1.0e-6};
 
 // The busiest workgroup's time in the rounds that hold a items of time ta and
 // then b of time tb: these are dealt in turn, odd rounds in reverse, so a load
@@ -41,52 +43,51 @@ double rounds_time(int64_t a, double ta, int64_t b, double tb, int nwg) {
   return worst;
 }
 
-LinearCut choose(int m, int n, int k, bool fp8, int nwg, int64_t max_floats) {
+LinearPlan choose(int m, int n, int k, bool fp8, int nwg, int64_t max_floats) {
   const Costs& q = fp8 ? kFp8 : kBf16;
-  const int KT = (k + 63) / 64;
-  LinearCut c{};
-  const int rem = m % 256;
-  c.nrow = m / 256 + (rem > 128);
-  c.fam = rem == 0 || rem > 128 ? 0 : rem > 64 ? 1 : 2;
-  c.ncol = (n + 255) / 256;
-  const int tiles = c.nrow * c.ncol;
-  c.whole = tiles / nwg * nwg;
-  c.rest = tiles - c.whole;
-  LinearCut best{};
-  double best_t = 1e300;
-  const int last = c.last_tiles(n);
+  const int KT = (k + 63) / 64, rem = m % 256;
   const int max_p = std::max(1, std::min(kMaxPieces, KT / kMinPieceSteps));
-  for (int halves = 1; halves <= 2; ++halves)
-    for (int p0 = 1; p0 <= (c.rest ? max_p : 1); ++p0)
-      for (int pr = 1; pr <= (c.fam ? max_p : 1); ++pr) {
-        LinearCut t = c;
-        t.halves = halves;
-        t.p0 = p0;
-        t.pr = pr;
-        t.items = t.whole + t.rest_items() + last * pr;
-        const int64_t fl = t.floats(n);
-        if (fl > max_floats) continue;
-        const int s0 = halves - 1, sr = 1 + t.fam;
-        const double t0 = q.item[s0] + (double)KT / p0 * q.step[s0] + (p0 > 1 ? q.part[s0] : 0.0);
-        const double tr = t.fam ? q.item[sr] + (double)KT / pr * q.step[sr] + (pr > 1 ? q.part[sr] : 0.0) : 0.0;
-        double us = rounds_time(t.rest_items(), t0, (int64_t)last * pr, tr, nwg);
-        if (fl) us += q.sums + q.sums_float * (double)fl;
-        if (us < best_t) {
-          best_t = us;
-          best = t;
+  LinearPlan best{{}, 1e300};
+  // rows: 256-row tiles and what is left; 128-row tiles; 64-row tiles
+  for (int rows = 0; rows < 3; ++rows) {
+    LinearCut c{};
+    c.nrow = rows ? 0 : m / 256 + (rem > 128);
+    c.fam = rows ? rows : rem == 0 || rem > 128 ? 0 : rem > 64 ? 1 : 2;
+    c.lrow = rows ? (m + (256 >> rows) - 1) / (256 >> rows) : c.fam ? 1 : 0;
+    c.ncol = (n + 255) / 256;
+    const int64_t tiles = (int64_t)c.nrow * c.ncol, last = (int64_t)c.lrow * ((n + 127) / 128);
+    if (rows && last > 4 * nwg) continue;  // many: larger tiles are better
+    c.whole = (int)(tiles / nwg * nwg);
+    c.rest = (int)(tiles - c.whole);
+    for (int halves = 1; halves <= (c.rest ? 2 : 1); ++halves)
+      for (int p0 = 1; p0 <= (c.rest ? max_p : 1); ++p0)
+        for (int pr = 1; pr <= (c.fam ? max_p : 1); ++pr) {
+          LinearCut t = c;
+          t.halves = halves;
+          t.p0 = p0;
+          t.pr = pr;
+          t.items = t.whole + t.rest_items() + (int)(last * pr);
+          const int64_t fl = t.floats(n);
+          if (fl > max_floats) continue;
+          const int s0 = halves - 1, sr = 1 + t.fam;
+          const double t0 = q.item[s0] + (double)KT / p0 * q.step[s0] + (p0 > 1 ? q.part[s0] : 0.0);
+          const double tr = t.fam ? q.item[sr] + (double)KT / pr * q.step[sr] + (pr > 1 ? q.part[sr] : 0.0) : 0.0;
+          double us = c.whole / nwg * (q.item[0] + KT * q.step[0]) + rounds_time(t.rest_items(), t0, last * pr, tr, nwg);
+          if (fl) us += q.sums + q.sums_float * (double)fl;
+          if (us < best.us) best = LinearPlan{t, us};
         }
-      }
+  }
   return best;
 }
 
 }  // namespace
 
-LinearCut linear_cut(int m, int n, int k, bool fp8, int nwg, int64_t max_floats) {
+const LinearPlan& linear_plan(int m, int n, int k, bool fp8, int nwg, int64_t max_floats) {
   // a few sizes come again and again: the last choices of this thread
   struct Seen {
     int m, n, k, fp8, nwg;
     int64_t max_floats;
-    LinearCut cut;
+    LinearPlan plan;
   };
   static thread_local Seen seen[64];
   max_floats = std::min(max_floats, kMaxScratchFloats);
@@ -94,7 +95,41 @@ LinearCut linear_cut(int m, int n, int k, bool fp8, int nwg, int64_t max_floats)
   Seen& s = seen[h];
   if (s.m != m || s.n != n || s.k != k || s.fp8 != (int)fp8 || s.nwg != nwg || s.max_floats != max_floats)
     s = Seen{m, n, k, (int)fp8, nwg, max_floats, choose(m, n, k, fp8, nwg, max_floats)};
-  return s.cut;
+  return s.plan;
+}
+
+// The tile with the least to load for the busiest CU: ceil(tiles / CUs) tiles of
+// 16 (RF + CF) rows of K, at about 76 GB/s per CU, equal: the larger tile.  us
+// of the choice and of the next best ones, operands in the Infinity Cache:
+// 64 x 4096 x 4096 2x2 9.2, 1x4 10.5, 4x1 11.1, 4x2 12.6; 512 x 256 x 7168 1x2
+// 12.0, 2x1 12.3, 2x2 13.5, 1x1 15.9; 128 x 4096 x 4096 2x4 12.9, 4x2 13.0, 2x2
+// 14.9; 32 x 256 x 2048 1x1 4.6, 2x1 5.0, 2x2 5.4.
+RowsPlan rows_plan(int m, int n, int k, int x_bytes, int w_bytes, int ncu) {
+  constexpr int kShapes[][2] = {{2, 4}, {4, 2}, {2, 2}, {2, 1}, {1, 2}, {1, 1}};
+  RowsPlan best{0, 0, 1e300};
+  for (auto& q : kShapes) {
+    const int rf = q[0], cf = q[1];
+    const int64_t tiles = ((int64_t)(m + rf * 16 - 1) / (rf * 16)) * ((n + cf * 16 - 1) / (cf * 16));
+    const double us = 3.0 + (double)((tiles + ncu - 1) / ncu) * 16.0 * (rf * x_bytes + cf * w_bytes) * (double)k / 76e3;
+    if (us < best.us) best = RowsPlan{rf, cf, us};
+  }
+  return best;
+}
+
+// Tiles where they are faster by both kernels' times (fitted to measurements
+// of 48 .. 2048 rows, 64 .. 14336 columns and K = 1024 .. 14336: 384 x 4096 x
+// 4096 rows 30, tiles 27 us; 256 x 4096 x 4096 22 and 25; 2048 x 1024 x 1024 15
+// and 17; 96 x 14336 x 4096 32 and 29; 2048 x 4096 x 4096 160 and 47).  They need
+// aligned rows, and offsets within a tile that fit 31 bits.
+const LinearPlan* linear_tiles_plan(const LinearArgs& p, int nwg, int64_t max_floats) {
+  if (p.w_dtype == kF32 || !p.aligned || p.n < 8) return nullptr;
+  if (std::max({p.ldx, p.ldw, p.ldy, p.res ? p.ldr : 0}) >= 1 << 22) return nullptr;
+  const RowsPlan rows = rows_plan(p.m, p.n, p.k, 2, p.w_dtype == kFP8 ? 1 : 2, nwg);
+  if (rows.us < 16.0) return nullptr;  // less than any tiled product takes
+  const LinearPlan& t = linear_plan(p.m, p.n, p.k, p.w_dtype == kFP8, nwg, max_floats);
+  // results that do not go out in 16 bytes take a tile some 15 us more
+  const double slow = p.wide ? 0.0 : 15.0 * ((t.cut.items + nwg - 1) / nwg);
+  return t.us + slow < rows.us ? &t : nullptr;
 }
 
 }  // namespace aep

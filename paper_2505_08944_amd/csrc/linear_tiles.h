@@ -2,12 +2,13 @@
 // the cut, the tile kernel and the kernel that adds the pieces' sums.
 //
 // Rows are covered by 256-row tiles (family 0) and, where 128 or fewer are
-// left, one row of tiles of 128 or 64 rows (family 1 or 2).  Tiles of family 0
-// have 256 columns; full rounds of the grid of them are one item each.  What
-// is left of them, a partial round, is cut into column halves or not, and
-// these along K into pieces; tiles of the other families have 128 columns and
-// are cut along K alone.  Pieces leave their f32 sums in the scratch, one
-// tile after another, where a second launch adds them in piece order.
+// left, by one row of tiles of 128 or 64 rows (family 1 or 2); or by rows of
+// these alone.  Tiles of family 0 have 256 columns; full rounds of the grid of
+// them are one item each.  What is left of them, a partial round, is cut into
+// column halves or not, and these along K into pieces; tiles of the other
+// families have 128 columns and are cut along K alone.  Pieces leave their f32
+// sums in the scratch, one tile after another, where a second launch adds them
+// in piece order.
 #pragma once
 
 #include "aep_internal.h"
@@ -21,10 +22,11 @@ struct LinearCut {
   int halves;       // 2: these are cut into column halves, 1: not
   int p0;           // pieces along K of each of these
   int fam, pr;      // family of the last rows' tiles (0: none) and their pieces
+  int lrow;         // rows of these tiles
   int items;        // all in all
   __host__ __device__ int rest_parts() const { return rest * halves; }         // tiles or halves
   __host__ __device__ int rest_items() const { return rest_parts() * p0; }
-  __host__ __device__ int last_tiles(int n) const { return fam ? (n + 127) / 128 : 0; }
+  __host__ __device__ int last_tiles(int n) const { return lrow * ((n + 127) / 128); }
   // f32 values of scratch; part q of a tile or half lies at its first float + q * its size
   __host__ __device__ int64_t rest_floats() const { return p0 > 1 ? (int64_t)rest_items() * (65536 / halves) : 0; }
   __host__ __device__ int64_t floats(int n) const {
@@ -32,11 +34,21 @@ struct LinearCut {
   }
 };
 
-// The tile kernel takes the product (rows_or_tiles' rule is at its definition).
-bool linear_uses_tiles(const LinearArgs& p);
-// The cut for a product of these sizes on nwg workgroups whose pieces' sums
-// take at most max_floats of scratch.
-LinearCut linear_cut(int m, int n, int k, bool fp8, int nwg, int64_t max_floats);
+// The cheapest cut of a product of these sizes on nwg workgroups whose pieces'
+// sums take at most max_floats of scratch, and its time.
+struct LinearPlan {
+  LinearCut cut;
+  double us;
+};
+const LinearPlan& linear_plan(int m, int n, int k, bool fp8, int nwg, int64_t max_floats);
+// The row kernel's tile (fragments of rows and columns) and its time.
+struct RowsPlan {
+  int rf, cf;
+  double us;
+};
+RowsPlan rows_plan(int m, int n, int k, int x_bytes, int w_bytes, int ncu);
+// Whether the tile kernel takes the product, and then how (null: the row kernel).
+const LinearPlan* linear_tiles_plan(const LinearArgs& p, int nwg, int64_t max_floats);
 hipError_t launch_linear_tiles(const LinearArgs& p, const LinearCut& c, int nwg, float* scratch, hipStream_t s);
 
 }  // namespace aep

@@ -130,8 +130,8 @@ aep_status aep_linear_workspace(const aep_linear_desc* l, size_t* bytes) {
   if (l->m == 0) return AEP_OK;
   // as for aligned pointers
   const LinearArgs p = linear_args(*l, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
-  if (linear_uses_tiles(p))
-    *bytes = (size_t)linear_cut(p.m, p.n, p.k, p.w_dtype == kFP8, persistent_workgroups(), INT64_MAX).floats(p.n) * 4;
+  if (const LinearPlan* t = linear_tiles_plan(p, persistent_workgroups(), INT64_MAX))
+    *bytes = (size_t)t->cut.floats(p.n) * 4;
   return AEP_OK;
 }
 
