@@ -9,6 +9,7 @@ layer is drained, expert weights while registered).
 from __future__ import annotations
 
 import ctypes
+import math
 from typing import Dict, List, Optional, Tuple
 
 import numpy as np
@@ -23,7 +24,7 @@ _POLICY = {"mtfs": L.AEP_POLICY_MTFS, "flfs": L.AEP_POLICY_FLFS, "defrag": L.AEP
 
 
 def _stream() -> ctypes.c_void_p:
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return ctypes.c_void_p(L.raw_stream(torch.cuda.current_device()))
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -57,8 +58,7 @@ class BatchView:
         if ws is None:
             raise RuntimeError("batch views need a torch-allocated workspace (this context uses the static one)")
         off = ptr - ws.data_ptr()
-        n = int(np.prod(shape)) if shape else 1
-        nbytes = n * torch.empty((), dtype=dtype).element_size()
+        nbytes = math.prod(shape) * dtype.itemsize
         assert 0 <= off and off + nbytes <= ws.numel()
         return ws[off:off + nbytes].view(dtype).view(shape)
 

@@ -195,8 +195,11 @@ constexpr int kMaxRouteGroups = 64;
 struct RouterArgs {
   int E, k, sigmoid, n_groups, top_groups, group_top, renorm;
   float scale;
+  int per;      // experts of a group
   int inv_per;  // e * inv_per >> 20 is expert e's group
+  int share16, share32;  // log2 of how many of a token's 16 or 32 lanes share a group (n_groups << it fits them)
   int row;      // doubles of a token's LDS row
+  int vec4;     // set by the launchers: runs of experts may be read in 16 bytes
 };
 // Where a routed fragment goes: the queues of a layer (arguments as in
 // launch_append).

@@ -11,11 +11,17 @@
 //
 // The rule compares choices in binary64, as a score plus a bias of like size
 // has neighbours that binary32 cannot tell apart, and the same logits must give
-// the same experts on every rank.  Where all neighbours in the order, and the last kept and first dropped group,
-// are further apart than that, f32 has given the rule's answer.  Where they are
-// not (one token in a few hundred), the choices in question, one per lane, or
-// the groups, are compared again in f64.  Logits without a bias are compared as
-// they are, exactly.
+// the same experts on every rank.  Where all neighbours in the order, and the
+// last kept and first dropped group, are further apart than f32's errors, f32 has
+// given the rule's answer.  Where they are not (one token in a few hundred), the
+// choices in question, one per lane, or the groups, are compared again in f64.
+// Logits without a bias are compared as they are, exactly.
+//
+// What bounds it: 8192 tokens of 256 experts in 8 groups, sigmoid and bias, 13.3
+// us (8.9 MB: 1.7 us at the rate of a large copy): 1600 vector instructions per
+// wave of four tokens, two waves per SIMD, so that half the time is their
+// dependences'.  (A wave per token, all of it in f64: 34 us.)  64 tokens: 7.7 us,
+// one wave's chain of loads, sort, rounds and f64 weights.
 #include <float.h>
 #include <limits.h>
 
@@ -78,16 +84,18 @@ __device__ __forceinline__ double never_key() { return -DBL_MAX; }
 __device__ __forceinline__ bool is_live(double k) { return k > -1e100; }
 static_assert(kMaxScoredExperts <= kIdMask + 1, "an id in kIdMask");
 
-// Neighbours a >= b that are further apart than both errors.  A softmax score
-// is off by at most 2^-19.5 of itself (e^x 2^-22, up to 20 additions of 2^-24,
-// the reciprocal 2^-23), a sigmoid by 2^-21.5, so scores, and sums of two
-// softmax scores, by at most 2^-19.5 and sums of two sigmoids by 2^-20.5; every
-// addition by half a step of its result.
+// Neighbours a >= b that are further apart than both errors: slack for the
+// scores' part of them, and 2^-23 of the values for the additions, which are off
+// by half a step, 2^-24, of each result.  A sigmoid is off by less than 2^-22 (the
+// reciprocal 2^-23 and 1 + e^-x 2^-24 of it; e^-x 2^-23, and 2^-24 |x| for its
+// argument, of s (1 - s)), a softmax score by 2^-19.5 of the largest one (e^x
+// 2^-22, up to 20 additions of 2^-24, the reciprocal 2^-23); two scores twice
+// that, two sums of two four times (of softmax scores, whose sum is at most 1,
+// twice).
 __device__ __forceinline__ bool apart(double a, double b, double slack) {
   if (!is_live(a) || !is_live(b)) return true;
-  return a - b > slack + 0x1p-21 * (fabs(a) + fabs(b));
+  return a - b > slack + 0x1p-23 * (fabs(a) + fabs(b));
 }
-constexpr double kSlackSoftmax = 0x1p-18, kSlackSigmoid = 0x1p-19;
 
 // e^x for x <= 0 to 2^-22: the hardware's 2^x on the rounded x log2(e),
 // corrected for what the rounding lost.  0 below -200, -inf included.
@@ -98,8 +106,7 @@ __device__ __forceinline__ float exp_neg(float x) {
   const float e = __builtin_amdgcn_exp2f(t);
   return __builtin_fmaf(e, lost * 0.693147181f, e);
 }
-// 1 / (1 + e^-x) to 2^-21.5 of itself or of 2^-1: where |x| times the rounding
-// of the exponent's product counts, s (1 - s) |x| is small.
+// 1 / (1 + e^-x); its error is stated at apart().
 __device__ __forceinline__ float sigmoid32(float x) {
   return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * -1.44269504f));
 }
@@ -202,6 +209,28 @@ __device__ __forceinline__ void best_of(double& v, int& e) {
   if constexpr (LANES == 32) better(v, e, partner<4>(v), partner<4>(e));
 }
 
+// Calls f with the value and id of each of the token's other lanes.
+template <typename F, size_t... D>
+__device__ __forceinline__ void others_in_row(double v, int e, F f, std::index_sequence<D...>) {
+  auto from = [](int x, auto d) {  // row_ror: a rotation of the 16 lanes
+    return __builtin_amdgcn_update_dpp(0, x, 0x121 + d(), 0xF, 0xF, true);
+  };
+  (f(__hiloint2double(from(__double2hiint(v), std::integral_constant<int, D>{}),
+                      from(__double2loint(v), std::integral_constant<int, D>{})),
+     from(e, std::integral_constant<int, D>{})),
+   ...);
+}
+template <int LANES, typename F>
+__device__ __forceinline__ void others(double v, int e, F f) {
+  others_in_row(v, e, f, std::make_index_sequence<15>{});
+  if constexpr (LANES == 32) {
+    const double w = partner<4>(v);
+    const int o = partner<4>(e);
+    f(w, o);
+    others_in_row(w, o, f, std::make_index_sequence<15>{});
+  }
+}
+
 // What a token's lanes share in LDS where experts have groups: a value per
 // expert.  Its lanes are in one wave: ordering the wave's accesses is enough.
 __device__ __forceinline__ void wave_fence() {
@@ -209,73 +238,62 @@ __device__ __forceinline__ void wave_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Worths of groups from the experts' values in LDS (-inf: masked): the lanes
-// of a token share the groups, `share` lanes each where groups are few.
-// Returns the kept groups as a mask; certain: no other f32 rounding would have
-// kept others (slack < 0: the values are exact).
-template <int LANES, typename T>
-__device__ __forceinline__ uint64_t pick_groups(const T* __restrict__ val, const RouterArgs& r, int g, double slack,
+// ------------------------------------------------------------------ groups
+// How a token's lanes hold its experts.  Without groups, or with groups that
+// do not fit whole lanes, lane g holds g, g + LANES, ...; the groups' worths are
+// then found through LDS.  Where LANES / n_groups lanes hold a group each (16, 8,
+// 4 or 2 groups, and 32 above 256 experts), lane g holds a run of E / LANES experts:
+// a group's worth is a reduction over its lanes, and dropping a group is
+// dropping its lanes' heads.
+enum { kNoGroups = 0, kGroupLanes = 1, kGroupsInLds = 2 };
+
+// The two largest of what has been added (-inf: nothing).
+template <typename T>
+struct Two {
+  T a, b;
+  __device__ __forceinline__ void add(T x) {
+    b = x > a ? a : (x > b ? x : b);
+    a = x > a ? x : a;
+  }
+  template <int STEP>
+  __device__ __forceinline__ void join() {
+    const T oa = partner<STEP>(a), ob = partner<STEP>(b);
+    const T lo = oa > a ? a : oa, nb = ob > b ? ob : b;
+    a = oa > a ? oa : a;
+    b = lo > nb ? lo : nb;
+  }
+  // over `share` lanes, a power of two below LANES
+  __device__ __forceinline__ void join_lanes(int share) {
+    if (share > 1) join<0>();
+    if (share > 2) join<1>();
+    if (share > 4) join<2>();
+    if (share > 8) join<3>();
+  }
+  __device__ __forceinline__ T worth(int group_top) const {
+    return group_top > 1 && b != -(T)__builtin_inff() ? a + b : a;
+  }
+};
+
+// The top_groups best of Q groups per lane, group lead + q * step worth[q] (-inf:
+// all masked), as a mask.  certain: no other f32 rounding would have kept
+// others (slack < 0: the values are exact).
+template <int LANES, int Q, typename T>
+__device__ __forceinline__ uint64_t pick_groups(const T (&worth)[Q], int lead, int step, const RouterArgs& r, double slack,
                                                 bool& certain) {
-  const int per = r.E / r.n_groups;
-  // worth of groups i, i + 1, ... per lane; ids in the key's upper part for f64
-  T worth[4];
-  int share = 1;
-  while (2 * share * r.n_groups <= LANES) share *= 2;
-  const int sub = g & (share - 1), lead = g / share;  // lead: the group, LANES / share apart
-  const int step = LANES / share;
   const T none = -(T)__builtin_inff();
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const int gr = lead + q * step;
-    T a = none, b = none;
-    if (gr < r.n_groups) {
-      // four at a time, so that their reads are in flight together
-      for (int i = sub; i < per; i += 4 * share) {
-        T x[4];
-#pragma unroll
-        for (int z = 0; z < 4; ++z) x[z] = val[gr * per + min(i + z * share, per - 1)];
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          x[z] = i + z * share < per ? x[z] : none;
-          b = x[z] > a ? a : (x[z] > b ? x[z] : b);
-          a = x[z] > a ? x[z] : a;
-        }
-      }
-    }
-    if (share > 1) {
-      // the lanes of a group join their two best (share is a power of two, at most LANES / 2)
-#define JOIN(STEP)                                            \
-  {                                                           \
-    const T oa = partner<STEP>(a), ob = partner<STEP>(b);     \
-    const T lo = oa > a ? a : oa, hi = oa > a ? oa : a;       \
-    const T nb = ob > b ? ob : b;                             \
-    a = hi;                                                   \
-    b = lo > nb ? lo : nb;                                    \
-  }
-      JOIN(0)
-      if (share > 2) JOIN(1)
-      if (share > 4) JOIN(2)
-      if (share > 8) JOIN(3)
-#undef JOIN
-    }
-    worth[q] = r.group_top > 1 && b != none ? a + b : a;
-    if (step * (q + 1) >= r.n_groups) {
-#pragma unroll
-      for (int z = q + 1; z < 4; ++z) worth[z] = none;
-      break;
-    }
-  }
   uint64_t kept = 0;
   certain = true;
   if constexpr (sizeof(T) == 4) {
-    double key[4], last = 0.0;
+    double key[Q], last = 0.0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
+    for (int q = 0; q < Q; ++q) {
       const int gr = lead + q * step;
       key[q] = gr >= r.n_groups ? never_key() : worth[q] == none ? masked_key(gr) : make_key(worth[q], gr);
     }
     for (int j = 0; j <= r.top_groups; ++j) {
-      double k = max64(max64(key[0], key[1]), max64(key[2], key[3]));
+      double k = key[0];
+#pragma unroll
+      for (int q = 1; q < Q; ++q) k = max64(k, key[q]);
       k = reduce_max<LANES>(k);
       if (j == r.top_groups) {
         certain = slack < 0.0 || apart(last, k, slack);
@@ -284,14 +302,14 @@ __device__ __forceinline__ uint64_t pick_groups(const T* __restrict__ val, const
       last = k;
       kept |= 1ull << key_id(k);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) key[q] = key[q] == k ? never_key() : key[q];
+      for (int q = 0; q < Q; ++q) key[q] = key[q] == k ? never_key() : key[q];
     }
   } else {
     for (int j = 0; j < r.top_groups; ++j) {
       double v = none;
       int id = INT_MAX;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < Q; ++q) {
         const int gr = lead + q * step;
         if (gr < r.n_groups && !((kept >> gr) & 1)) better(v, id, (double)worth[q], gr);
       }
@@ -302,49 +320,136 @@ __device__ __forceinline__ uint64_t pick_groups(const T* __restrict__ val, const
   return kept;
 }
 
+// The same from the experts' values in LDS; the lanes share the groups, 1 << shift
+// lanes each where groups are few.
+template <int LANES, typename T>
+__device__ __forceinline__ uint64_t pick_groups_lds(const T* __restrict__ val, const RouterArgs& r, int g, double slack,
+                                                    bool& certain) {
+  const int per = r.per, shift = LANES == 32 ? r.share32 : r.share16, share = 1 << shift;
+  const int sub = g & (share - 1), lead = g >> shift, step = LANES >> shift;
+  const T none = -(T)__builtin_inff();
+  T worth[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int gr = lead + q * step;
+    Two<T> two{none, none};
+    if (gr < r.n_groups) {
+      // four at a time, so that their reads are in flight together
+      for (int i = sub; i < per; i += 4 * share) {
+        T x[4];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) x[z] = val[gr * per + min(i + z * share, per - 1)];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) two.add(i + z * share < per ? x[z] : none);
+      }
+    }
+    two.join_lanes(share);
+    worth[q] = two.worth(r.group_top);
+    if (step * (q + 1) >= r.n_groups) {
+#pragma unroll
+      for (int z = q + 1; z < 4; ++z) worth[z] = none;
+      break;
+    }
+  }
+  return pick_groups<LANES, 4>(worth, lead, step, r, slack, certain);
+}
+
+// The experts of lane g: id(i), i < EPL, if has(i).
+template <int LANES, int GM>
+struct Held {
+  int first, n, E;
+  __device__ __forceinline__ Held(int g, int E) : first(GM == kGroupLanes ? g * (E / LANES) : g), n(E / LANES), E(E) {}
+  __device__ __forceinline__ int id(int i) const { return GM == kGroupLanes ? first + i : first + i * LANES; }
+  __device__ __forceinline__ bool has(int i) const { return GM == kGroupLanes ? i < n : id(i) < E; }
+};
+
+// This lane's values of a row (anything where there is none).  Runs are read in
+// 16 bytes where their alignment allows (r.vec4): a load of lanes that are apart
+// takes a cycle per lane.
+template <int EPL, int LANES, int GM>
+__device__ __forceinline__ void held_values(float (&v)[EPL], const float* __restrict__ row, const Held<LANES, GM>& held,
+                                            const RouterArgs& r) {
+  if (GM == kGroupLanes && r.vec4) {
+#pragma unroll
+    for (int i = 0; i < EPL; i += 4) {
+      const float4 q = *reinterpret_cast<const float4*>(row + min(held.id(i), r.E - 4));
+      v[i] = q.x;
+      v[i + 1] = q.y;
+      v[i + 2] = q.z;
+      v[i + 3] = q.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) v[i] = row[min(held.id(i), r.E - 1)];
+  }
+}
+
+// The groups that stay, where LANES / n_groups lanes hold a group each, from the
+// two largest of each lane's values (-inf: masked or none), which become the
+// group's.
+template <int EPL, typename T>
+__device__ __forceinline__ Two<T> two_of(const T (&c)[EPL]) {
+  Two<T> two{-(T)__builtin_inff(), -(T)__builtin_inff()};
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) two.add(c[i]);
+  return two;
+}
+template <int LANES, typename T>
+__device__ __forceinline__ uint64_t pick_group_lanes(Two<T>& two, const RouterArgs& r, int g, double slack, bool& certain) {
+  const int shift = LANES == 32 ? r.share32 : r.share16;
+  two.join_lanes(1 << shift);
+  const T worth[1] = {two.worth(r.group_top)};
+  return pick_groups<LANES, 1>(worth, g >> shift, LANES, r, slack, certain);
+}
+
 // The whole selection in f64, for a token with more choices too close to each
 // other than it has lanes: lane j gets slot j's expert.  All of its lanes call it.
-template <int EPL, int LANES>
+template <int EPL, int LANES, int GM>
 __device__ __noinline__ int select_exact(const float* __restrict__ l, const float* __restrict__ bias, RouterArgs r, int g,
                                          double* __restrict__ val) {
   const double none = -__builtin_inf();
+  const Held<LANES, GM> held{g, r.E};
   double top = none, total = 0.0;
   if (!r.sigmoid) {
     for (int i = 0; i < EPL; ++i) {
-      const int e = i * LANES + g;
-      if (e < r.E && __builtin_isfinite(l[e])) top = max64(top, (double)l[e]);
+      const int e = held.id(i);
+      if (held.has(i) && __builtin_isfinite(l[e])) top = max64(top, (double)l[e]);
     }
     top = reduce_max<LANES>(top);
     for (int i = 0; i < EPL; ++i) {
-      const int e = i * LANES + g;
-      if (e < r.E && __builtin_isfinite(l[e])) total += exp((double)l[e] - top);
+      const int e = held.id(i);
+      if (held.has(i) && __builtin_isfinite(l[e])) total += exp((double)l[e] - top);
     }
     total = reduce<LANES>(total, [](double a, double b) { return a + b; });
   }
   double c[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
-    const int e = i * LANES + g;
+    const int e = held.id(i);
     c[i] = none;
-    if (e < r.E && __builtin_isfinite(l[e])) {
+    if (held.has(i) && __builtin_isfinite(l[e])) {
       const double x = (double)l[e];
       c[i] = r.sigmoid ? sigmoid64(x) : exp(x - top) / total;
       if (bias) c[i] += (double)bias[e];
       if (!__builtin_isfinite(c[i])) c[i] = none;
     }
-    if (r.n_groups > 1 && e < r.E) val[e] = c[i];
+    if (GM == kGroupsInLds && held.has(i)) val[e] = c[i];
   }
   uint64_t kept = ~0ull;
-  if (r.n_groups > 1) {
+  bool certain;
+  if constexpr (GM == kGroupsInLds) {
     wave_fence();
-    bool certain;
-    kept = pick_groups<LANES, double>(val, r, g, -1.0, certain);
+    kept = pick_groups_lds<LANES, double>(val, r, g, -1.0, certain);
+  }
+  if constexpr (GM == kGroupLanes) {
+    Two<double> two = two_of<EPL>(c);
+    kept = pick_group_lanes<LANES>(two, r, g, -1.0, certain);
   }
   unsigned avail = 0;
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
-    const int e = i * LANES + g;
-    if (e < r.E && ((kept >> (r.n_groups > 1 ? e / (r.E / r.n_groups) : 0)) & 1)) avail |= 1u << i;
+    const int e = held.id(i);
+    if (held.has(i) && ((kept >> (GM == kNoGroups ? 0 : e / r.per)) & 1)) avail |= 1u << i;
     // without a bias experts are picked by their logits
     if (!bias && c[i] != none) c[i] = (double)l[e];
   }
@@ -354,9 +459,11 @@ __device__ __noinline__ int select_exact(const float* __restrict__ l, const floa
     int id = INT_MAX;
 #pragma unroll
     for (int i = 0; i < EPL; ++i)
-      if ((avail >> i) & 1) better(v, id, c[i], i * LANES + g);
+      if ((avail >> i) & 1) better(v, id, c[i], held.id(i));
     best_of<LANES>(v, id);
-    if (id % LANES == g) avail &= ~(1u << (id / LANES));
+#pragma unroll
+    for (int i = 0; i < EPL; ++i)
+      if (held.id(i) == id) avail &= ~(1u << i);
     if (g == j) mine = id;
   }
   return mine;
@@ -369,18 +476,17 @@ enum { kByLogit = 0, kBySoftmax = 1, kBySigmoid = 2 };
 // Routes token t on its LANES lanes: lane j < k gets slot j's expert and weight.
 // val: the token's LDS row (of E values; unused without groups).  bad: a value
 // to be reported was seen by this lane.
-template <int EPL, int LANES, int BY>
+template <int EPL, int LANES, int BY, int GM>
 __device__ __forceinline__ void route_scored(const float* __restrict__ logits, int64_t ld,
                                              const float* __restrict__ bias, const RouterArgs& r, int64_t t, int g,
                                              double* __restrict__ val, int& my_e, float& my_w, bool& bad) {
   const float* __restrict__ l = logits + t * ld;
   const float none = -__builtin_inff();
+  const Held<LANES, GM> held{g, r.E};
   float x[EPL], b[EPL];
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) x[i] = l[min(i * LANES + g, r.E - 1)];
+  held_values<EPL>(x, l, held, r);
   if (BY != kByLogit && bias) {
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) b[i] = bias[min(i * LANES + g, r.E - 1)];
+    held_values<EPL>(b, bias, held, r);
   } else {
 #pragma unroll
     for (int i = 0; i < EPL; ++i) b[i] = 0.f;
@@ -391,8 +497,8 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
   for (int i = 0; i < EPL; ++i) {
     // a difference of a finite value with itself is 0, of any other NaN
     const bool live = x[i] - x[i] == 0.f;
-    bad |= !live && x[i] != none;
-    x[i] = live && i * LANES + g < r.E ? x[i] : none;
+    bad |= !live && x[i] != none && held.has(i);
+    x[i] = live && held.has(i) ? x[i] : none;
     top = fmaxf(top, x[i]);
   }
   float total = 1.f;
@@ -410,20 +516,24 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
   const float inv = BY == kBySoftmax ? __builtin_amdgcn_rcpf(total) : 1.f;
   float* __restrict__ val32 = reinterpret_cast<float*>(val);
   double key[EPL];
+  float val_of[EPL];
 #pragma unroll
   for (int i = 0; i < EPL; ++i) {
-    const int e = i * LANES + g;
+    const int e = held.id(i);
     float c = x[i];
     if constexpr (BY == kBySoftmax) c = exp_neg(x[i] - top) * inv + b[i];
     if constexpr (BY == kBySigmoid) c = sigmoid32(x[i]) + b[i];
     const bool off = BY != kByLogit && c - c != 0.f && x[i] != none;  // a bias that is not finite
     bad |= off;
     c = x[i] == none || off ? none : c;
-    if (r.n_groups > 1 && e < r.E) val32[e] = c;
+    val_of[i] = c;
+    if (GM == kGroupsInLds && held.has(i)) val32[e] = c;
     const float by = BY == kByLogit || bias ? c : x[i];
-    key[i] = e >= r.E ? never_key() : c == none ? masked_key(e) : make_key(by, e);
+    key[i] = !held.has(i) ? never_key() : c == none ? masked_key(e) : make_key(by, e);
   }
-  constexpr double slack = BY == kByLogit ? -1.0 : BY == kBySoftmax ? kSlackSoftmax : kSlackSigmoid;
+  // (the largest softmax score is inv; the sum of a group's two may be 1)
+  const double slack = BY == kBySoftmax ? 0x1p-18 * (double)inv : 0x1p-21;
+  const double group_slack = BY == kByLogit ? -1.0 : BY == kBySoftmax ? 0x1p-18 : 0x1p-20;
   // softmax in f64, where it is needed
   auto total64 = [&] {
     double z = 0.0;
@@ -431,32 +541,54 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
     for (int i = 0; i < EPL; ++i) z += x[i] == none ? 0.0 : exp((double)x[i] - (double)top);
     return reduce<LANES>(z, [](double a, double b) { return a + b; });
   };
-  if (r.n_groups > 1) {
-    wave_fence();
+  auto choice64 = [&](float v, float bv, double z) {
+    return (BY == kBySigmoid ? sigmoid64((double)v) : exp((double)v - (double)top) / z) + (double)bv;
+  };
+  uint64_t kept = ~0ull;
+  if constexpr (GM != kNoGroups) {
     bool certain;
-    uint64_t kept = pick_groups<LANES, float>(val32, r, g, slack, certain);
-    if (BY != kByLogit && !certain) {
-      const double z = BY == kBySoftmax ? total64() : 1.0;
+    if constexpr (GM == kGroupsInLds) {
       wave_fence();
+      kept = pick_groups_lds<LANES, float>(val32, r, g, group_slack, certain);
+      if (BY != kByLogit && !certain) {
+        const double z = BY == kBySoftmax ? total64() : 1.0;
+        wave_fence();
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) {
-        const int e = i * LANES + g;
-        double c = BY == kBySigmoid ? sigmoid64((double)x[i]) : exp((double)x[i] - (double)top) / z;
-        c += (double)b[i];
-        if (e < r.E) val[e] = is_live(key[i]) ? c : -__builtin_inf();
+        for (int i = 0; i < EPL; ++i)
+          if (held.has(i)) val[held.id(i)] = is_live(key[i]) ? choice64(x[i], b[i], z) : -__builtin_inf();
+        wave_fence();
+        kept = pick_groups_lds<LANES, double>(val, r, g, -1.0, certain);
       }
-      wave_fence();
-      kept = pick_groups<LANES, double>(val, r, g, -1.0, certain);
-    }
+    } else {
+      Two<float> two = two_of<EPL>(val_of);
+      kept = pick_group_lanes<LANES>(two, r, g, group_slack, certain);
+      if (BY != kByLogit && !certain) {
+        // in f64, the experts that may be among their group's best: about one per lane
+        const double z = BY == kBySoftmax ? total64() : 1.0;
+        const float least = r.group_top > 1 && two.b != none ? two.b : two.a;
+        const float limit = least - ((float)group_slack + 0x1p-22f * fabsf(least));
+        unsigned may = 0;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      const int e = i * LANES + g;
-      if (!((kept >> ((e * r.inv_per) >> 20)) & 1)) key[i] = never_key();
+        for (int i = 0; i < EPL; ++i) may |= val_of[i] != none && val_of[i] >= limit ? 1u << i : 0u;
+        Two<double> best{-__builtin_inf(), -__builtin_inf()};
+        for (; may; may &= may - 1) {
+          const int e = held.id(__ffs(may) - 1);
+          best.add(choice64(l[e], bias ? bias[e] : 0.f, z));
+        }
+        kept = pick_group_lanes<LANES>(best, r, g, -1.0, certain);
+      }
+    }
+    if constexpr (GM == kGroupsInLds) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i)
+        if (!((kept >> ((held.id(i) * r.inv_per) >> 20)) & 1)) key[i] = never_key();
     }
   }
   constexpr int L = EPL > 8 ? 8 : EPL;
   double list[L];
   best_keys<EPL, L>(key, list);
+  // a lane whose head is never taken never moves up
+  if (GM == kGroupLanes && !((kept >> (g >> (LANES == 32 ? r.share32 : r.share16))) & 1)) list[0] = never_key();
   const double end = L < EPL ? unknown_key() : never_key();
   my_e = 0;
   bool close = false, lost = false;  // choices too close to each other; more of them than were kept at hand
@@ -491,23 +623,18 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
       int id = INT_MAX;
       if (g < n) {
         id = my_e;
-        const double v = (double)l[id], bv = (double)bias[id];
-        if (v - v == 0.0 && bv - bv == 0.0) c = (BY == kBySigmoid ? sigmoid64(v) : exp(v - (double)top) / z) + bv;
+        const float v = l[id], bv = bias[id];
+        if (v - v == 0.f && bv - bv == 0.f) c = choice64(v, bv, z);
       }
       int rank = 0;
-      for (int d = 1; d < LANES; ++d) {
-        const int from = (g + d) & (LANES - 1);
-        const double oc = __shfl(c, from, LANES);
-        const int oid = __shfl(id, from, LANES);
-        rank += oid != INT_MAX && (oc > c || (oc == c && oid < id));
-      }
+      others<LANES>(c, id, [&](double oc, int oid) { rank += oid != INT_MAX && (oc > c || (oc == c && oid < id)); });
       // lanes without a candidate keep to their own places behind
       rank = g < n ? rank : g;
       const int at = ((threadIdx.x & 63 & ~(LANES - 1)) + rank) * 4;
       my_e = __builtin_amdgcn_ds_permute(at, my_e);
     }
   }
-  if (lost) my_e = select_exact<EPL, LANES>(l, bias, r, g, val);
+  if (lost) my_e = select_exact<EPL, LANES, GM>(l, bias, r, g, val);
 
   // weights, from the chosen ones' scores in f64
   double s = 0.0;
@@ -526,7 +653,7 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
 }
 
 // Tokens without queues.
-template <int EPL, int LANES, int BY>
+template <int EPL, int LANES, int BY, int GM>
 __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restrict__ logits, int64_t ld,
                                                            const float* __restrict__ bias, int T, RouterArgs r,
                                                            int32_t* __restrict__ idx, float* __restrict__ w,
@@ -538,7 +665,7 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restri
   float v;
   bool bad;
   // (the last tokens' lanes repeat the last one: a wave has no idle rows)
-  route_scored<EPL, LANES, BY>(logits, ld, bias, r, t < T ? t : T - 1, g, vals + tb * r.row, e, v, bad);
+  route_scored<EPL, LANES, BY, GM>(logits, ld, bias, r, t < T ? t : T - 1, g, vals + tb * r.row, e, v, bad);
   if (t < T && g < r.k) {
     idx[t * r.k + g] = e;
     w[t * r.k + g] = v;
@@ -551,7 +678,7 @@ __global__ __launch_bounds__(256) void route_scored_kernel(const float* __restri
 // tokens that picked an expert are a mask).  A fragment of one workgroup gets
 // its queue entries and depths written here; else blockcnt [E][workgroups] gets
 // the workgroup's rows per expert.
-template <int EPL, int LANES, int BY>
+template <int EPL, int LANES, int BY, int GM>
 __global__ __launch_bounds__(32 * LANES) void route_queue_kernel(
     const float* __restrict__ logits, const float* __restrict__ bias, int T, RouterArgs r, int32_t* __restrict__ r_idx,
     float* __restrict__ r_w, int32_t* __restrict__ r_rank, int32_t* __restrict__ blockcnt,
@@ -565,7 +692,7 @@ __global__ __launch_bounds__(32 * LANES) void route_queue_kernel(
   int e;
   float w;
   bool bad;
-  route_scored<EPL, LANES, BY>(logits, r.E, bias, r, t < T ? t : T - 1, g, vals + tb * r.row, e, w, bad);
+  route_scored<EPL, LANES, BY, GM>(logits, r.E, bias, r, t < T ? t : T - 1, g, vals + tb * r.row, e, w, bad);
   const bool on = t < T && g < r.k;
   if (on) atomicOr(&tok_mask[e], 1u << tb);
   __syncthreads();
@@ -638,6 +765,7 @@ __global__ __launch_bounds__(kRouteThreads) void append_scored_kernel(const int3
     int v = c[blockIdx.x];
     if (direct) {
       int sum = a.depth_cur[e];
+#pragma unroll 8
       for (int b = 0; b < (int)blockIdx.x; ++b) sum += c[b];
       if ((int)blockIdx.x == nb - 1) a.depth_nxt[e] = sum + v;
       v = sum;
@@ -662,46 +790,66 @@ __global__ __launch_bounds__(kRouteThreads) void append_scored_kernel(const int3
   if (g == 0) a.tok_row[tok] = row;
 }
 
-// Calls f(EPL, LANES, BY) as constants.
+// Calls f(EPL, LANES, BY, GM) as constants.
 template <typename F>
 static void by_rule(const RouterArgs& r, bool bias, F f) {
-  auto sized = [&](auto by) {
+  using std::integral_constant;
+  auto sized = [&](auto by, auto gm) {
     if (r.E <= 64)
-      f(std::integral_constant<int, 4>{}, std::integral_constant<int, 16>{}, by);
+      f(integral_constant<int, 4>{}, integral_constant<int, 16>{}, by, gm);
     else if (r.E <= 128)
-      f(std::integral_constant<int, 8>{}, std::integral_constant<int, 16>{}, by);
+      f(integral_constant<int, 8>{}, integral_constant<int, 16>{}, by, gm);
     else if (r.E <= 256)
-      f(std::integral_constant<int, 16>{}, std::integral_constant<int, 16>{}, by);
+      f(integral_constant<int, 16>{}, integral_constant<int, 16>{}, by, gm);
     else
-      f(std::integral_constant<int, 16>{}, std::integral_constant<int, 32>{}, by);
+      f(integral_constant<int, 16>{}, integral_constant<int, 32>{}, by, gm);
+  };
+  auto grouped = [&](auto by) {
+    const int lanes = r.E <= 256 ? 16 : 32;
+    if (r.n_groups == 1)
+      sized(by, integral_constant<int, kNoGroups>{});
+    else if (lanes % r.n_groups == 0 && r.E % lanes == 0)
+      sized(by, integral_constant<int, kGroupLanes>{});
+    else
+      sized(by, integral_constant<int, kGroupsInLds>{});
   };
   if (!bias && !(r.n_groups > 1 && r.group_top > 1))
-    sized(std::integral_constant<int, kByLogit>{});
+    grouped(integral_constant<int, kByLogit>{});
   else if (r.sigmoid)
-    sized(std::integral_constant<int, kBySigmoid>{});
+    grouped(integral_constant<int, kBySigmoid>{});
   else
-    sized(std::integral_constant<int, kBySoftmax>{});
+    grouped(integral_constant<int, kBySoftmax>{});
 }
 
-hipError_t launch_route_scored(const float* logits, int64_t ld, const float* bias, int T, const RouterArgs& r,
+// Runs of experts per lane start and end at 16 bytes, in every row.
+static int runs_aligned(const float* logits, int64_t ld, const float* bias, const RouterArgs& r) {
+  const int lanes = r.E <= 256 ? 16 : 32;
+  return (((uintptr_t)logits | (uintptr_t)bias) & 15) == 0 && ld % 4 == 0 && r.E % (4 * lanes) == 0;
+}
+
+hipError_t launch_route_scored(const float* logits, int64_t ld, const float* bias, int T, const RouterArgs& rule,
                                int32_t* idx, float* w, int32_t* flag, hipStream_t s) {
-  by_rule(r, bias != nullptr, [&](auto epl, auto lanes, auto by) {
+  RouterArgs r = rule;
+  r.vec4 = runs_aligned(logits, ld, bias, r);
+  by_rule(r, bias != nullptr, [&](auto epl, auto lanes, auto by, auto gm) {
     // few tokens: a wave per workgroup, so that they spread over the CUs
     const int threads = T <= 4096 ? 64 : 256, tokens = threads / lanes();
-    const size_t lds = r.n_groups > 1 ? (size_t)tokens * r.row * 8 : 0;
-    route_scored_kernel<epl(), lanes(), by()><<<(T + (int64_t)tokens - 1) / tokens, threads, lds, s>>>(logits, ld, bias, T, r, idx,
+    const size_t lds = gm() == kGroupsInLds ? (size_t)tokens * r.row * 8 : 0;
+    route_scored_kernel<epl(), lanes(), by(), gm()><<<(T + (int64_t)tokens - 1) / tokens, threads, lds, s>>>(logits, ld, bias, T, r, idx,
                                                                                                w, flag);
   });
   return hipGetLastError();
 }
 
-hipError_t launch_route_queue(const float* logits, const float* bias, int T, const RouterArgs& r, int32_t* r_idx,
+hipError_t launch_route_queue(const float* logits, const float* bias, int T, const RouterArgs& rule, int32_t* r_idx,
                               float* r_w, int32_t* r_rank, int32_t* blockcnt, int32_t* idx_out, float* w_out,
                               const AppendArgs& a, hipStream_t s) {
+  RouterArgs r = rule;
+  r.vec4 = runs_aligned(logits, r.E, bias, r);
   const int nb = (T + 31) / 32;
-  by_rule(r, bias != nullptr, [&](auto epl, auto lanes, auto by) {
-    const size_t lds = r.n_groups > 1 ? (size_t)32 * r.row * 8 : 0;
-    route_queue_kernel<epl(), lanes(), by()><<<nb, 32 * lanes(), lds, s>>>(logits, bias, T, r, r_idx, r_w, r_rank, blockcnt,
+  by_rule(r, bias != nullptr, [&](auto epl, auto lanes, auto by, auto gm) {
+    const size_t lds = gm() == kGroupsInLds ? (size_t)32 * r.row * 8 : 0;
+    route_queue_kernel<epl(), lanes(), by(), gm()><<<nb, 32 * lanes(), lds, s>>>(logits, bias, T, r, r_idx, r_w, r_rank, blockcnt,
                                                                          idx_out, w_out, a);
   });
   hipError_t e = hipGetLastError();

@@ -27,9 +27,21 @@ aep_status check_router(const aep_router* r) {
 }
 
 RouterArgs router_args(const aep_router& r) {
-  const int per = r.n_experts / r.n_groups;
-  return RouterArgs{r.n_experts, r.top_k,  r.score == AEP_SCORE_SIGMOID, r.n_groups,       r.top_groups, r.group_top,
-                    r.renorm,    r.scale, ((1 << 20) + per - 1) / per,  r.n_experts | 1};
+  RouterArgs a{};
+  a.E = r.n_experts;
+  a.k = r.top_k;
+  a.sigmoid = r.score == AEP_SCORE_SIGMOID;
+  a.n_groups = r.n_groups;
+  a.top_groups = r.top_groups;
+  a.group_top = r.group_top;
+  a.renorm = r.renorm;
+  a.scale = r.scale;
+  a.per = r.n_experts / r.n_groups;
+  a.inv_per = ((1 << 20) + a.per - 1) / a.per;
+  while ((r.n_groups << (a.share16 + 1)) <= 16) ++a.share16;
+  while ((r.n_groups << (a.share32 + 1)) <= 32) ++a.share32;
+  a.row = r.n_experts | 1;  // (odd: tokens start in different banks)
+  return a;
 }
 
 }  // namespace aep

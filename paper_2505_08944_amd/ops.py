@@ -46,12 +46,6 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-# The raw current stream of a device: torch builds a Stream object around it
-# otherwise, which takes longer than everything else here but the launch.
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
-    (lambda index: torch.cuda.current_stream(index).cuda_stream)
-
-
 class Linear:
     """y = f(scale * (x W^T) + bias) + residual (``aep_linear``).
 
@@ -116,12 +110,13 @@ class Linear:
             key = (m, x.stride(0), out.stride(0), residual.stride(0), residual.dtype)
         call = self._calls.get(key) or self._describe(key, x, residual, out)
         need = call[1]
-        ws = torch.empty(need, dtype=torch.uint8, device=dev).data_ptr() if need else None
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None  # held until the launch is in the stream
         scale, bias = self.scale, self.bias
         st = self._lib.aep_linear(call[0], x.data_ptr(), self.weight.data_ptr(),
                                   None if scale is None else scale.data_ptr(),
                                   None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(),
-                                  out.data_ptr(), ws, need, _raw_stream(dev.index))
+                                  out.data_ptr(), None if ws is None else ws.data_ptr(), need,
+                                  L.raw_stream(dev.index))
         if st:
             L.check(st, "aep_linear")
         return out
@@ -200,7 +195,7 @@ def route(router: Router, logits: torch.Tensor, bias: Optional[torch.Tensor] = N
         weights = torch.empty((T, k), dtype=torch.float32, device=dev)
     st = router._lib.aep_route_topk(
         router._at, logits.data_ptr(), _ld(logits), None if bias is None else bias.data_ptr(), T, idx.data_ptr(),
-        weights.data_ptr(), None if flag is None else flag.data_ptr(), _raw_stream(dev.index))
+        weights.data_ptr(), None if flag is None else flag.data_ptr(), L.raw_stream(dev.index))
     if st:
         L.check(st, "aep_route_topk")
     return idx, weights

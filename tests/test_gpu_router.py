@@ -52,6 +52,8 @@ def inputs(c, T, seed, mode="plain"):
             l[1, E // 2] = 1.0
     elif mode == "close":  # neighbours that 32 bits do not tell apart once the bias is added
         l = 8.0 + torch.randn(T, E, generator=g) * 1e-2
+    elif mode == "offset":  # a bias so large that f32 sums keep little of the scores
+        b = None if b is None else b + 50.0
     elif mode == "wide":
         l = l * 200.0
     return l, b
@@ -68,7 +70,7 @@ def check(c, l, b, idx, w):
 
 
 @pytest.mark.parametrize("c", RULES, ids=lambda c: "-".join(f"{k}{v}" for k, v in c.items()))
-@pytest.mark.parametrize("mode", ["plain", "ties", "masked", "close", "wide"])
+@pytest.mark.parametrize("mode", ["plain", "ties", "masked", "close", "offset", "wide"])
 def test_rules(c, mode):
     r = aep.Router(c["E"], c["k"], **rule(c))
     for T in (1, 2, 33, 130):
