@@ -82,19 +82,21 @@ __device__ __forceinline__ int key_id(double k) {
 __device__ __forceinline__ double masked_key(int id) { return __hiloint2double((int)0xFE000000u, id); }
 __device__ __forceinline__ double never_key() { return -DBL_MAX; }
 __device__ __forceinline__ bool is_live(double k) { return k > -1e100; }
+// A key's value (its id is below half a step); -inf for those two.
+__device__ __forceinline__ float key_value(double k) { return (float)k; }
 static_assert(kMaxScoredExperts <= kIdMask + 1, "an id in kIdMask");
 
 // Neighbours a >= b that are further apart than both errors: slack for the
 // scores' part of them, and 2^-23 of the values for the additions, which are off
 // by half a step, 2^-24, of each result.  A sigmoid is off by less than 2^-22 (the
 // reciprocal 2^-23 and 1 + e^-x 2^-24 of it; e^-x 2^-23, and 2^-24 |x| for its
-// argument, of s (1 - s)), a softmax score by 2^-19.5 of the largest one (e^x
-// 2^-22, up to 20 additions of 2^-24, the reciprocal 2^-23); two scores twice
+// argument, of s (1 - s)), a softmax score by 2^-20 of the largest one (e^x and
+// their sum 2^-22 each, the reciprocal 2^-23); two scores twice
 // that, two sums of two four times (of softmax scores, whose sum is at most 1,
 // twice).
-__device__ __forceinline__ bool apart(double a, double b, double slack) {
-  if (!is_live(a) || !is_live(b)) return true;
-  return a - b > slack + 0x1p-23 * (fabs(a) + fabs(b));
+__device__ __forceinline__ bool apart(float a, float b, float slack) {
+  // (-inf, a masked one, is apart from every other)
+  return b == -__builtin_inff() || a - b > slack + 0x1p-23f * (fabsf(a) + fabsf(b));
 }
 
 // e^x for x <= 0 to 2^-22: the hardware's 2^x on the rounded x log2(e),
@@ -278,13 +280,14 @@ struct Two {
 // all masked), as a mask.  certain: no other f32 rounding would have kept
 // others (slack < 0: the values are exact).
 template <int LANES, int Q, typename T>
-__device__ __forceinline__ uint64_t pick_groups(const T (&worth)[Q], int lead, int step, const RouterArgs& r, double slack,
+__device__ __forceinline__ uint64_t pick_groups(const T (&worth)[Q], int lead, int step, const RouterArgs& r, float slack,
                                                 bool& certain) {
   const T none = -(T)__builtin_inff();
   uint64_t kept = 0;
   certain = true;
   if constexpr (sizeof(T) == 4) {
-    double key[Q], last = 0.0;
+    double key[Q];
+    float last = 0.f;
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
       const int gr = lead + q * step;
@@ -296,10 +299,10 @@ __device__ __forceinline__ uint64_t pick_groups(const T (&worth)[Q], int lead, i
       for (int q = 1; q < Q; ++q) k = max64(k, key[q]);
       k = reduce_max<LANES>(k);
       if (j == r.top_groups) {
-        certain = slack < 0.0 || apart(last, k, slack);
+        certain = slack < 0.f || apart(last, key_value(k), slack);
         break;
       }
-      last = k;
+      last = key_value(k);
       kept |= 1ull << key_id(k);
 #pragma unroll
       for (int q = 0; q < Q; ++q) key[q] = key[q] == k ? never_key() : key[q];
@@ -323,7 +326,7 @@ __device__ __forceinline__ uint64_t pick_groups(const T (&worth)[Q], int lead, i
 // The same from the experts' values in LDS; the lanes share the groups, 1 << shift
 // lanes each where groups are few.
 template <int LANES, typename T>
-__device__ __forceinline__ uint64_t pick_groups_lds(const T* __restrict__ val, const RouterArgs& r, int g, double slack,
+__device__ __forceinline__ uint64_t pick_groups_lds(const T* __restrict__ val, const RouterArgs& r, int g, float slack,
                                                     bool& certain) {
   const int per = r.per, shift = LANES == 32 ? r.share32 : r.share16, share = 1 << shift;
   const int sub = g & (share - 1), lead = g >> shift, step = LANES >> shift;
@@ -395,7 +398,7 @@ __device__ __forceinline__ Two<T> two_of(const T (&c)[EPL]) {
   return two;
 }
 template <int LANES, typename T>
-__device__ __forceinline__ uint64_t pick_group_lanes(Two<T>& two, const RouterArgs& r, int g, double slack, bool& certain) {
+__device__ __forceinline__ uint64_t pick_group_lanes(Two<T>& two, const RouterArgs& r, int g, float slack, bool& certain) {
   const int shift = LANES == 32 ? r.share32 : r.share16;
   two.join_lanes(1 << shift);
   const T worth[1] = {two.worth(r.group_top)};
@@ -439,11 +442,11 @@ __device__ __noinline__ int select_exact(const float* __restrict__ l, const floa
   bool certain;
   if constexpr (GM == kGroupsInLds) {
     wave_fence();
-    kept = pick_groups_lds<LANES, double>(val, r, g, -1.0, certain);
+    kept = pick_groups_lds<LANES, double>(val, r, g, -1.f, certain);
   }
   if constexpr (GM == kGroupLanes) {
     Two<double> two = two_of<EPL>(c);
-    kept = pick_group_lanes<LANES>(two, r, g, -1.0, certain);
+    kept = pick_group_lanes<LANES>(two, r, g, -1.f, certain);
   }
   unsigned avail = 0;
 #pragma unroll
@@ -499,17 +502,22 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
     const bool live = x[i] - x[i] == 0.f;
     bad |= !live && x[i] != none && held.has(i);
     x[i] = live && held.has(i) ? x[i] : none;
-    top = fmaxf(top, x[i]);
   }
+  const bool softmax = BY == kBySoftmax || (BY == kByLogit && !r.sigmoid);
   float total = 1.f;
-  if (!r.sigmoid) {
+  double sum_exp = 1.0;
+  if (softmax) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) top = fmaxf(top, x[i]);
     top = reduce<LANES>(top, [](float a, float b) { return fmaxf(a, b); });
     top = top == none ? 0.f : top;  // every expert masked
     if (BY == kBySoftmax || !r.renorm) {
-      total = 0.f;
+      // (added up in f64: weights that are not renormalised are divided by it)
+      double z = 0.0;
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) total += exp_neg(x[i] - top);
-      total = reduce<LANES>(total, [](float a, float b) { return a + b; });
+      for (int i = 0; i < EPL; ++i) z += (double)exp_neg(x[i] - top);
+      sum_exp = reduce<LANES>(z, [](double a, double b) { return a + b; });
+      total = (float)sum_exp;
     }
   }
   // choices, or logits; with groups, what an expert is worth to its group
@@ -529,11 +537,13 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
     val_of[i] = c;
     if (GM == kGroupsInLds && held.has(i)) val32[e] = c;
     const float by = BY == kByLogit || bias ? c : x[i];
-    key[i] = !held.has(i) ? never_key() : c == none ? masked_key(e) : make_key(by, e);
+    // (without runs, ids past E come behind every expert: none is picked)
+    const double off_key = GM != kGroupLanes || held.has(i) ? masked_key(e) : never_key();
+    key[i] = c == none ? off_key : make_key(by, e);
   }
   // (the largest softmax score is inv; the sum of a group's two may be 1)
-  const double slack = BY == kBySoftmax ? 0x1p-18 * (double)inv : 0x1p-21;
-  const double group_slack = BY == kByLogit ? -1.0 : BY == kBySoftmax ? 0x1p-18 : 0x1p-20;
+  const float slack = BY == kBySoftmax ? 0x1p-18f * inv : 0x1p-21f;
+  const float group_slack = BY == kByLogit ? -1.f : BY == kBySoftmax ? 0x1p-18f : 0x1p-20f;
   // softmax in f64, where it is needed
   auto total64 = [&] {
     double z = 0.0;
@@ -557,7 +567,7 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
         for (int i = 0; i < EPL; ++i)
           if (held.has(i)) val[held.id(i)] = is_live(key[i]) ? choice64(x[i], b[i], z) : -__builtin_inf();
         wave_fence();
-        kept = pick_groups_lds<LANES, double>(val, r, g, -1.0, certain);
+        kept = pick_groups_lds<LANES, double>(val, r, g, -1.f, certain);
       }
     } else {
       Two<float> two = two_of<EPL>(val_of);
@@ -566,7 +576,7 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
         // in f64, the experts that may be among their group's best: about one per lane
         const double z = BY == kBySoftmax ? total64() : 1.0;
         const float least = r.group_top > 1 && two.b != none ? two.b : two.a;
-        const float limit = least - ((float)group_slack + 0x1p-22f * fabsf(least));
+        const float limit = least - (group_slack + 0x1p-22f * fabsf(least));
         unsigned may = 0;
 #pragma unroll
         for (int i = 0; i < EPL; ++i) may |= val_of[i] != none && val_of[i] >= limit ? 1u << i : 0u;
@@ -575,7 +585,7 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
           const int e = held.id(__ffs(may) - 1);
           best.add(choice64(l[e], bias ? bias[e] : 0.f, z));
         }
-        kept = pick_group_lanes<LANES>(best, r, g, -1.0, certain);
+        kept = pick_group_lanes<LANES>(best, r, g, -1.f, certain);
       }
     }
     if constexpr (GM == kGroupsInLds) {
@@ -592,12 +602,14 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
   const double end = L < EPL ? unknown_key() : never_key();
   my_e = 0;
   bool close = false, lost = false;  // choices too close to each other; more of them than were kept at hand
-  double last = 0.0;
+  float last = 0.f;
   for (int j = 0; j < r.k; ++j) {
     const double w = take_best<LANES, L>(list, end);
     lost |= w == unknown_key();
-    if (BY != kByLogit && bias) close |= j > 0 && !apart(last, w, slack);
-    last = w;
+    if (BY != kByLogit && bias) {
+      close |= j > 0 && !apart(last, key_value(w), slack);
+      last = key_value(w);
+    }
     if (g == j) my_e = key_id(w);
   }
   if (BY != kByLogit && bias) {
@@ -606,13 +618,13 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
     for (;; ++n) {
       const double w = take_best<LANES, L>(list, end);
       lost |= w == unknown_key();
-      if (lost || apart(last, w, slack)) break;
+      if (lost || apart(last, key_value(w), slack)) break;
       close = true;
       if (n == LANES) {
         lost = true;
         break;
       }
-      last = w;
+      last = key_value(w);
       if (g == n) my_e = key_id(w);
     }
     if (close && !lost) {
@@ -641,13 +653,13 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
   if (g < r.k) {
     const float v = l[my_e];
     const bool live = __builtin_isfinite(v) && (!bias || __builtin_isfinite(bias[my_e]));
-    if (live) s = r.sigmoid ? sigmoid64((double)v) : exp((double)v - (double)top);
+    if (live) s = softmax ? exp((double)v - (double)top) : sigmoid64((double)v);
   }
   if (r.renorm) {
     const double sum = reduce<LANES>(s, [](double a, double b) { return a + b; });
     s = sum > 0.0 ? s / sum : 0.0;
-  } else if (!r.sigmoid) {
-    s = total > 0.f ? s / (double)total : 0.0;  // 0: every expert masked
+  } else if (softmax) {
+    s = sum_exp > 0.0 ? s / sum_exp : 0.0;  // 0: every expert masked
   }
   my_w = (float)(s * (double)r.scale);
 }
