@@ -212,7 +212,8 @@ typedef struct {
  * other GPUs).  Device pointers: logits f32, row t at logits + t * ld_logits
  * (ld_logits >= E), bias [E] f32 or NULL, idx [T][top_k] int32, w [T][top_k]
  * f32, flag one int32 or NULL, set to 1 (and never cleared) where a value is
- * reported as above.  Needs no context.  T == 0 is a no-op.
+ * reported as above.  Needs no context; runs on the current HIP device, which
+ * the pointers and the stream belong to.  T == 0 is a no-op.
  * AEP_ERR_UNSUPPORTED for more than 512 experts or a top_k above 16. */
 aep_status aep_route_topk(const aep_router* r, const float* logits, int64_t ld_logits, const float* bias, int32_t T,
                           int32_t* idx, float* w, int32_t* flag, void* stream);
@@ -486,8 +487,10 @@ aep_status aep_linear_workspace(const aep_linear_desc* l, size_t* bytes);
  * not overlap any input.  d_ws: 16-byte aligned scratch of ws_bytes, or NULL:
  * the product then runs without it where less than aep_linear_workspace is
  * given.  Nothing in d_ws is kept from call to call, and calls that may
- * overlap on the GPU need one each.  Needs no context.  Results do not depend
- * on other calls, and equal calls give equal bits.  m == 0 is a no-op. */
+ * overlap on the GPU need one each.  Needs no context; runs on the current HIP
+ * device, which the pointers and the stream belong to.  Results do not depend
+ * on other calls, and equal calls (sizes, strides, alignments and scratch given)
+ * give equal bits.  m == 0 is a no-op. */
 aep_status aep_linear(const aep_linear_desc* l, const void* x, const void* w, const void* scale, const void* bias,
                       const void* residual, void* y, void* d_ws, size_t ws_bytes, void* stream);
 

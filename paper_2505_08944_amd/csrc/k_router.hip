@@ -19,9 +19,10 @@
 //
 // What bounds it: 8192 tokens of 256 experts in 8 groups, sigmoid and bias, 13.3
 // us (8.9 MB: 1.7 us at the rate of a large copy): 1600 vector instructions per
-// wave of four tokens, two waves per SIMD, so that half the time is their
-// dependences'.  (A wave per token, all of it in f64: 34 us.)  64 tokens: 7.7 us,
-// one wave's chain of loads, sort, rounds and f64 weights.
+// wave of four tokens, two waves per SIMD; a further 8192 tokens take 5.4.  (A
+// wave per token, all of it in f64: 34 us.)  64 tokens: 7.4 us, one wave's chain
+// of loads, sort, rounds and f64 weights; 1.8 more where a token's choices have
+// to be compared in f64.
 #include <float.h>
 #include <limits.h>
 
@@ -666,7 +667,7 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
 
 // Tokens without queues.
 template <int EPL, int LANES, int BY, int GM>
-__global__ __launch_bounds__(256) void route_scored_kernel(const float* __restrict__ logits, int64_t ld,
+__global__ __launch_bounds__(64) void route_scored_kernel(const float* __restrict__ logits, int64_t ld,
                                                            const float* __restrict__ bias, int T, RouterArgs r,
                                                            int32_t* __restrict__ idx, float* __restrict__ w,
                                                            int32_t* __restrict__ flag) {
@@ -844,8 +845,9 @@ hipError_t launch_route_scored(const float* logits, int64_t ld, const float* bia
   RouterArgs r = rule;
   r.vec4 = runs_aligned(logits, ld, bias, r);
   by_rule(r, bias != nullptr, [&](auto epl, auto lanes, auto by, auto gm) {
-    // few tokens: a wave per workgroup, so that they spread over the CUs
-    const int threads = T <= 4096 ? 64 : 256, tokens = threads / lanes();
+    // a wave per workgroup: tokens spread over the CUs (256 threads: 64 tokens
+    // 9.2 us instead of 7.4, 8192 and more within 1%)
+    const int threads = 64, tokens = threads / lanes();
     const size_t lds = gm() == kGroupsInLds ? (size_t)tokens * r.row * 8 : 0;
     route_scored_kernel<epl(), lanes(), by(), gm()><<<(T + (int64_t)tokens - 1) / tokens, threads, lds, s>>>(logits, ld, bias, T, r, idx,
                                                                                                w, flag);
