@@ -8,8 +8,6 @@
 // and (in brackets) in HBM: 32 x 4096 x 4096 7.9 (11.9; its bytes at the rate of
 // a large copy 6.6), 1 x 14336 x 4096 fp8 11.5 (15.1; 11.3), 8192 x 64 x 2048 8.9
 // (9.1; 6.9), an empty launch 1.5.
-#include <limits.h>
-
 #include <algorithm>
 
 #include "linear_epilogue.h"
@@ -73,7 +71,7 @@ __global__ __launch_bounds__(WAVES * 64) void linear_rows_kernel(const LinearArg
   const int rr = lane & 15, hh = lane >> 4;
   // an XCD gets a contiguous run of tiles, row tiles of a column band adjacent
   const int64_t per = gridDim.x >> 3;
-  const int64_t tile = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  const int64_t tile = (int64_t)blockIdx.y * gridDim.x + (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
   const int tm = (p.m + TM - 1) / TM;
   if (tile >= (int64_t)tm * ((p.n + TN - 1) / TN)) return;
   const int ti = (int)(tile % tm), tj = (int)(tile / tm);
@@ -229,9 +227,10 @@ __global__ __launch_bounds__(WAVES * 64) void linear_rows_kernel(const LinearArg
 template <typename XT, typename WT, int RF, int CF, int WAVES, int D, bool ALIGNED>
 static hipError_t rows_launch(const LinearArgs& p, hipStream_t s) {
   const int64_t tiles = (int64_t)((p.m + RF * 16 - 1) / (RF * 16)) * ((p.n + CF * 16 - 1) / (CF * 16));
-  const int64_t grid = ((tiles + 7) / 8) * 8;
-  if (grid > INT_MAX) return hipErrorInvalidValue;
-  linear_rows_kernel<XT, WT, RF, CF, WAVES, D, ALIGNED><<<(unsigned)grid, WAVES * 64, 0, s>>>(p);
+  // (at most 2^30 tiles; a grid's side has fewer than 2^32 threads)
+  const int64_t gx = std::min<int64_t>((tiles + 7) / 8 * 8, 1 << 22);
+  const dim3 grid((unsigned)gx, (unsigned)((tiles + gx - 1) / gx));
+  linear_rows_kernel<XT, WT, RF, CF, WAVES, D, ALIGNED><<<grid, WAVES * 64, 0, s>>>(p);
   return hipGetLastError();
 }
 

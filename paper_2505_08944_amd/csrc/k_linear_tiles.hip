@@ -310,7 +310,7 @@ __device__ __forceinline__ void finish_wide(const LinearItem& it, int wm, int wn
           for (int e = 0; e < 4; ++e) {
             float v = acc[u][b][i][j][e];
             if constexpr (FP8) v *= s4[b][j][e];
-            o[j][e] = linear_fn_bf16<fn()>(v + b4[b][j][e]);
+            o[j][e] = linear_fn_tile<fn()>(v + b4[b][j][e]);
           }
         if (p.res) {
           const u32x4_t v = res[q & 1][i];
@@ -373,7 +373,7 @@ __device__ __forceinline__ void finish_any(const LinearItem& it, int wm, int wn,
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[i][j][e] = linear_fn_bf16<fn()>(v[i][j][e] + b4[j][e]);
+          for (int e = 0; e < 4; ++e) v[i][j][e] = linear_fn_tile<fn()>(v[i][j][e] + b4[j][e]);
     });
     if (p.res) {
 #pragma unroll

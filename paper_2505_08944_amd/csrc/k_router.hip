@@ -668,12 +668,12 @@ __device__ __forceinline__ void route_scored(const float* __restrict__ logits, i
 // Tokens without queues.
 template <int EPL, int LANES, int BY, int GM>
 __global__ __launch_bounds__(64) void route_scored_kernel(const float* __restrict__ logits, int64_t ld,
-                                                           const float* __restrict__ bias, int T, RouterArgs r,
-                                                           int32_t* __restrict__ idx, float* __restrict__ w,
-                                                           int32_t* __restrict__ flag) {
+                                                          const float* __restrict__ bias, int T, RouterArgs r,
+                                                          int32_t* __restrict__ idx, float* __restrict__ w,
+                                                          int32_t* __restrict__ flag) {
   extern __shared__ double vals[];
   const int g = threadIdx.x & (LANES - 1), tb = threadIdx.x / LANES;
-  const int64_t t = (int64_t)blockIdx.x * (blockDim.x / LANES) + tb;
+  const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (64 / LANES) + tb;
   int e;
   float v;
   bool bad;
@@ -847,10 +847,12 @@ hipError_t launch_route_scored(const float* logits, int64_t ld, const float* bia
   by_rule(r, bias != nullptr, [&](auto epl, auto lanes, auto by, auto gm) {
     // a wave per workgroup: tokens spread over the CUs (256 threads: 64 tokens
     // 9.2 us instead of 7.4, 8192 and more within 1%)
-    const int threads = 64, tokens = threads / lanes();
+    const int tokens = 64 / lanes();
     const size_t lds = gm() == kGroupsInLds ? (size_t)tokens * r.row * 8 : 0;
-    route_scored_kernel<epl(), lanes(), by(), gm()><<<(T + (int64_t)tokens - 1) / tokens, threads, lds, s>>>(logits, ld, bias, T, r, idx,
-                                                                                               w, flag);
+    const int64_t nb = (T + (int64_t)tokens - 1) / tokens, gx = nb < 1 << 24 ? nb : 1 << 24;
+    // (a grid's side has fewer than 2^32 threads)
+    route_scored_kernel<epl(), lanes(), by(), gm()>
+        <<<dim3((unsigned)gx, (unsigned)((nb + gx - 1) / gx)), 64, lds, s>>>(logits, ld, bias, T, r, idx, w, flag);
   });
   return hipGetLastError();
 }

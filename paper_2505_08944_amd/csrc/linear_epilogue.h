@@ -80,12 +80,15 @@ __device__ __forceinline__ float linear_fn(int fn, float v) {
   }
 }
 
-// The activation for bf16 results, short enough to be laid out for every value
-// of a tile: SILU and GELU_TANH as v / (1 + e^-u), with the hardware's exponential and reciprocal (2^-20 at |u| < 20; beyond, one of 1
-// and e^-u is lost); GELU with erf from Abramowitz and Stegun 7.1.26, whose
-// error is at most 1.5e-7 (half of it here, times |v|).
+// The activation for whole tiles, short enough to be laid out for every value of
+// one: SILU and GELU_TANH as v / (1 + e^-u), with the hardware's exponential and
+// reciprocal (2^-20 at |u| < 20; beyond, one of 1 and e^-u is lost); GELU with erf
+// from Abramowitz and Stegun 7.1.26, whose error is at most 1.5e-7, here half of
+// it times |v|.  Made for bf16 results (half a step: 2^-9 .. 2^-8 of them); an f32
+// result keeps that relative error of 2^-20 (GELU: that absolute one, below what
+// the sum's own roundings leave of v's size).
 template <int FN>
-__device__ __forceinline__ float linear_fn_bf16(float v) {
+__device__ __forceinline__ float linear_fn_tile(float v) {
   if constexpr (FN == kFnNone) return v;
   if constexpr (FN == kFnRelu) return v > 0.f ? v : v == v ? 0.f : v;
   if constexpr (FN == kFnSilu) return v * __builtin_amdgcn_rcpf(1.f + __expf(-v));

@@ -46,14 +46,30 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
-class Linear:
+def _int32(n: int, most: int, what: str, call: str) -> None:
+    # (ctypes cuts larger values off)
+    if n > most:
+        raise L.AEPError(L.AEP_ERR_UNSUPPORTED, f"{call}: {n} {what}")
+
+
+class _Fixed:
+    """Attributes are set once: what is kept for calls goes with them."""
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__:
+            raise AttributeError(f"{type(self).__name__}.{name} is fixed: make a new {type(self).__name__}")
+        self.__dict__[name] = value
+
+
+class Linear(_Fixed):
     """y = f(scale * (x W^T) + bias) + residual (``aep_linear``).
 
     weight [n, k]: float32 (x float32), bfloat16 or float8_e4m3fn / uint8 codes
     (x bfloat16), the latter with scale [n] bfloat16; rows may be strided.
     bias [n] float32 or bfloat16.  activation: none, relu, silu, gelu or
     gelu_tanh.  out_dtype: x's type (the default) or float32.  The tensors are
-    kept, not copied: values written to them later are used by later calls.
+    kept, not copied: values written to them later are used by later calls;
+    their shapes, strides and types stay as they are.
     """
 
     def __init__(self, weight: torch.Tensor, *, scale: Optional[torch.Tensor] = None,
@@ -66,6 +82,7 @@ class Linear:
         n, k = weight.shape
         if n < 1 or k < 1:
             raise ValueError(f"weight has shape {tuple(weight.shape)}")
+        _int32(max(n, k), 1 << 30, "channels", "aep_linear")
         fp8 = _CODE[weight.dtype] == L.AEP_FP8_E4M3
         if fp8 != (scale is not None):
             raise ValueError("scale goes with fp8 weights, and only with them")
@@ -123,6 +140,7 @@ class Linear:
 
     def _describe(self, key, x, residual, out):
         """(description, bytes of scratch) of a call, kept for the next ones like it."""
+        _int32(key[0], 1 << 30, "rows", "aep_linear")
         n, k, x_dtype, w_dtype, y_dtype, bias_dtype = self._fixed
         d = L.LinearDesc(key[0], n, k, x_dtype, w_dtype, y_dtype, bias_dtype,
                          L.AEP_F32 if residual is None else _CODE[residual.dtype], self._fn, _ld(x), self._ldw,
@@ -142,7 +160,7 @@ def linear(x: torch.Tensor, weight: torch.Tensor, *, scale: Optional[torch.Tenso
     return Linear(weight, scale=scale, bias=bias, activation=activation, out_dtype=out_dtype)(x, residual, out)
 
 
-class Router:
+class Router(_Fixed):
     """How a layer picks its experts (``aep_router``): softmax or sigmoid
     scores; experts in n_groups groups of consecutive ids, of which the
     top_groups best stay, each worth the sum of its group_top (1 or 2) best
@@ -180,6 +198,7 @@ def route(router: Router, logits: torch.Tensor, bias: Optional[torch.Tensor] = N
             return route(router, logits, bias, idx=idx, weights=weights, flag=flag)
     _rows(logits, "logits", (torch.float32,), (None, router.n_experts), dev)
     T, k = logits.shape[0], router.top_k
+    _int32(T, (1 << 31) - 1, "tokens", "aep_route_topk")
     if bias is not None:
         _rows(bias, "bias", (torch.float32,), (router.n_experts,), dev)
     if idx is not None or weights is not None or flag is not None:

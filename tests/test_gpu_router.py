@@ -29,6 +29,7 @@ RULES = [
     dict(E=36, k=4, n_groups=4, top_groups=4, group_top=1, bias=True), dict(E=511, k=9, bias=True),
     dict(E=512, k=16, n_groups=4, top_groups=2, group_top=2, score="sigmoid", bias=True, renorm=False),
     dict(E=384, k=8, score="sigmoid", bias=True),
+    dict(E=512, k=8, n_groups=64, top_groups=6, group_top=2, bias=True),
 ]
 
 
@@ -171,7 +172,8 @@ def queue_ref(idx, w, x, E):
 
 
 @pytest.mark.parametrize("i,frags", [(1, (5,)), (4, (1, 31, 40)), (7, (777,)), (8, (64, 33, 3)), (8, (2500, 1, 40)),
-                                     (12, (4100,)), (13, (32, 32)), (14, (70, 1))])
+                                     (12, (4100,)), (13, (32, 32)), (14, (70, 1)),
+                                     (17, (32, 45))])
 @pytest.mark.parametrize("S", [0, 1])
 def test_queues(i, frags, S):
     c = RULES[i]
