@@ -142,6 +142,9 @@ def lib() -> ctypes.CDLL:
 # otherwise (2.8 us a call, of the 4 us that a launch through ctypes takes).
 raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
+# (half the time of torch.cuda.current_device(), which sees to torch's
+# initialisation first: whoever has a tensor of a device has that behind)
+current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def check(status: int, call: str) -> None:

@@ -104,52 +104,55 @@ class Linear(_Fixed):
                        L.AEP_F32 if bias is None else _CODE[bias.dtype])
         self._fn = _FN[activation]
         self._ldw = _ld(weight)
-        self._calls = {}  # by sizes, strides and types: the description of such a call and its bytes of scratch
+        self._calls = {}  # by what is checked of the tensors: what _describe makes of such a call
 
     def __call__(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None,
                  out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x [m, k] -> [m, n].  residual [m, n] float32 or bfloat16; out may be
         the residual itself, and must not overlap anything else."""
-        dev, n = self.device, self.n
-        if dev.index != torch.cuda.current_device():
+        dev = self.device
+        if dev.index != L.current_device():
             with torch.cuda.device(dev):
                 return self(x, residual, out)
-        _rows(x, "x", (self.x_dtype,), (None, self.k), dev)
-        m = x.shape[0]
+        # a call like one before, in all that is checked, needs no checks
+        try:
+            key = (x.shape, x.stride(), x.dtype, x.device,
+                   residual is None or (residual.shape, residual.stride(), residual.dtype, residual.device),
+                   out is None or (out.shape, out.stride(), out.dtype, out.device))
+        except AttributeError:
+            raise ValueError("x, residual and out must be tensors") from None
+        desc, need, shape = self._calls.get(key) or self._describe(key, x, residual, out)
         if out is None:
-            out = torch.empty((m, n), dtype=self.out_dtype, device=dev)
-        else:
-            _rows(out, "out", (self.out_dtype,), (m, n), dev)
-        if residual is None:
-            key = (m, x.stride(0), out.stride(0))
-        else:
-            _rows(residual, "residual", (torch.float32, torch.bfloat16), (m, n), dev)
-            key = (m, x.stride(0), out.stride(0), residual.stride(0), residual.dtype)
-        call = self._calls.get(key) or self._describe(key, x, residual, out)
-        need = call[1]
+            out = torch.empty(shape, dtype=self.out_dtype, device=dev)
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None  # held until the launch is in the stream
         scale, bias = self.scale, self.bias
-        st = self._lib.aep_linear(call[0], x.data_ptr(), self.weight.data_ptr(),
-                                  None if scale is None else scale.data_ptr(),
-                                  None if bias is None else bias.data_ptr(), None if residual is None else residual.data_ptr(),
-                                  out.data_ptr(), None if ws is None else ws.data_ptr(), need,
-                                  L.raw_stream(dev.index))
+        st = self._lib.aep_linear(desc, x.data_ptr(), self.weight.data_ptr(), None if scale is None else scale.data_ptr(),
+                                  None if bias is None else bias.data_ptr(),
+                                  None if residual is None else residual.data_ptr(), out.data_ptr(),
+                                  None if ws is None else ws.data_ptr(), need, L.raw_stream(dev.index))
         if st:
             L.check(st, "aep_linear")
         return out
 
     def _describe(self, key, x, residual, out):
-        """(description, bytes of scratch) of a call, kept for the next ones like it."""
-        _int32(key[0], 1 << 30, "rows", "aep_linear")
+        """(description, bytes of scratch, shape of the result) of a checked call, kept for the next ones like it."""
         n, k, x_dtype, w_dtype, y_dtype, bias_dtype = self._fixed
-        d = L.LinearDesc(key[0], n, k, x_dtype, w_dtype, y_dtype, bias_dtype,
+        dev = self.device
+        _rows(x, "x", (self.x_dtype,), (None, k), dev)
+        m = x.shape[0]
+        _int32(m, 1 << 30, "rows", "aep_linear")
+        if residual is not None:
+            _rows(residual, "residual", (torch.float32, torch.bfloat16), (m, n), dev)
+        if out is not None:
+            _rows(out, "out", (self.out_dtype,), (m, n), dev)
+        d = L.LinearDesc(m, n, k, x_dtype, w_dtype, y_dtype, bias_dtype,
                          L.AEP_F32 if residual is None else _CODE[residual.dtype], self._fn, _ld(x), self._ldw,
-                         _ld(out), n if residual is None else _ld(residual))
+                         n if out is None else _ld(out), n if residual is None else _ld(residual))
         b = ctypes.c_size_t()
         L.check(self._lib.aep_linear_workspace(ctypes.byref(d), ctypes.byref(b)), "aep_linear_workspace")
         if len(self._calls) >= 1024:
             self._calls.clear()
-        call = self._calls[key] = (ctypes.byref(d), b.value)
+        call = self._calls[key] = (ctypes.byref(d), b.value, (m, n))
         return call
 
 
@@ -178,6 +181,7 @@ class Router(_Fixed):
                                  self.scale)
         self._at = ctypes.byref(self.desc)
         self._lib = L.lib()
+        self._seen = set()  # what was checked of logits and biases
         # the library checks the values; routing no tokens does nothing else
         L.check(self._lib.aep_route_topk(self._at, None, max(n_experts, 0), None, 0, None, None, None, None),
                 "aep_route_topk")
@@ -190,17 +194,27 @@ def route(router: Router, logits: torch.Tensor, bias: Optional[torch.Tensor] = N
     float32 (``aep_route_topk``).  bias [E] float32 is added to the scores for
     the choice only.  flag: int32 [1], set to 1 where a logit is NaN or +inf
     (-inf masks an expert) or a bias is not finite."""
-    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+    try:
+        dev = logits.device
+        key = (logits.shape, logits.stride(), logits.dtype, dev,
+               bias is None or (bias.shape, bias.stride(), bias.dtype, bias.device))
+    except AttributeError:
+        raise ValueError("logits and bias must be tensors") from None
+    if not logits.is_cuda:
         raise ValueError("logits must be a CUDA (HIP) tensor")
-    dev = logits.device
-    if dev.index != torch.cuda.current_device():
+    if dev.index != L.current_device():
         with torch.cuda.device(dev):
             return route(router, logits, bias, idx=idx, weights=weights, flag=flag)
-    _rows(logits, "logits", (torch.float32,), (None, router.n_experts), dev)
-    T, k = logits.shape[0], router.top_k
-    _int32(T, (1 << 31) - 1, "tokens", "aep_route_topk")
-    if bias is not None:
-        _rows(bias, "bias", (torch.float32,), (router.n_experts,), dev)
+    # logits and bias like ones before, in all that is checked, need no checks
+    if key not in router._seen:
+        _rows(logits, "logits", (torch.float32,), (None, router.n_experts), dev)
+        _int32(logits.shape[0], (1 << 31) - 1, "tokens", "aep_route_topk")
+        if bias is not None:
+            _rows(bias, "bias", (torch.float32,), (router.n_experts,), dev)
+        if len(router._seen) >= 1024:
+            router._seen.clear()
+        router._seen.add(key)
+    T, k = key[0][0], router.top_k
     if idx is not None or weights is not None or flag is not None:
         for t, name, dtype, shape in ((idx, "idx", torch.int32, (T, k)), (weights, "weights", torch.float32, (T, k)),
                                       (flag, "flag", torch.int32, (1,))):
@@ -211,7 +225,7 @@ def route(router: Router, logits: torch.Tensor, bias: Optional[torch.Tensor] = N
     if idx is None:
         idx = torch.empty((T, k), dtype=torch.int32, device=dev)
     if weights is None:
-        weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+        weights = torch.empty_like(idx, dtype=torch.float32)  # (quicker than empty())
     st = router._lib.aep_route_topk(
         router._at, logits.data_ptr(), _ld(logits), None if bias is None else bias.data_ptr(), T, idx.data_ptr(),
         weights.data_ptr(), None if flag is None else flag.data_ptr(), L.raw_stream(dev.index))

@@ -119,3 +119,17 @@ def test_linear_refuses_arguments():
     # no rows: nothing to do
     assert lib.aep_linear(ctypes.byref(_linear(m=0)), None, None, None, None, None, None, None, 0, None) == L.AEP_OK
     assert lib.aep_linear_workspace(ctypes.byref(d), None) == L.AEP_ERR_INVALID_ARG
+
+
+def test_calls_refuse_what_is_no_device_tensor():
+    import numpy as np
+    import torch
+
+    import paper_2505_08944_amd as aep
+    _lib()
+    r = aep.Router(8, 2)
+    for bad in (np.zeros((4, 8), np.float32), None, [[0.0] * 8], torch.zeros(4, 8)):
+        with pytest.raises(ValueError):
+            aep.route(r, bad)
+        with pytest.raises(ValueError):
+            aep.Linear(bad)
