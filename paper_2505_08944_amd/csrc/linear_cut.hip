@@ -104,13 +104,20 @@ const LinearPlan& linear_plan(int m, int n, int k, bool fp8, int nwg, int64_t ma
 // 64 x 4096 x 4096 2x2 9.2, 1x4 10.5, 4x1 11.1, 4x2 12.6; 512 x 256 x 7168 1x2
 // 12.0, 2x1 12.3, 2x2 13.5, 1x1 15.9; 128 x 4096 x 4096 2x4 12.9, 4x2 13.0, 2x2
 // 14.9; 32 x 256 x 2048 1x1 4.6, 2x1 5.0, 2x2 5.4.
+// f32: the same bytes at 120 GB/s and the MFMAs beside them, 0.9 us per fragment and
+// 1024 of K (150 TFLOP/s on 256 CUs), 0.3 us per tile.  294 x 845 x 960 1x1 11.8, 2x1 13.2, 2x2
+// 13.7, 2x4 (the choice by bytes alone) 14.2; 400 x 1500 x 1488 2x2 27.7, 2x1
+// 31.2, 2x4 35.6; 512 x 2048 x 2048 2x2 48.1, 2x4 48.7, 1x1 63.3; 128 x 1024 x
+// 1024 2x1 6.2, 1x1 6.3, 2x2 8.1, 2x4 13.0.
 RowsPlan rows_plan(int m, int n, int k, int x_bytes, int w_bytes, int ncu) {
   constexpr int kShapes[][2] = {{2, 4}, {4, 2}, {2, 2}, {2, 1}, {1, 2}, {1, 1}};
   RowsPlan best{0, 0, 1e300};
   for (auto& q : kShapes) {
     const int rf = q[0], cf = q[1];
     const int64_t tiles = ((int64_t)(m + rf * 16 - 1) / (rf * 16)) * ((n + cf * 16 - 1) / (cf * 16));
-    const double us = 3.0 + (double)((tiles + ncu - 1) / ncu) * 16.0 * (rf * x_bytes + cf * w_bytes) * (double)k / 76e3;
+    const double bytes = 16.0 * (rf * x_bytes + cf * w_bytes) * (double)k;
+    const double tile = x_bytes == 4 ? 0.3 + bytes / 120e3 + 0.88e-3 * rf * cf * (double)k : bytes / 76e3;
+    const double us = 3.0 + (double)((tiles + ncu - 1) / ncu) * tile;
     if (us < best.us) best = RowsPlan{rf, cf, us};
   }
   return best;
