@@ -230,17 +230,19 @@ constexpr int kF32 = 0, kBF16 = 1, kFP8 = 2;
 constexpr int kFnNone = 0, kFnRelu = 1, kFnSilu = 2, kFnGelu = 3, kFnGeluTanh = 4;
 
 // A checked dense product.  aligned: rows of x and w start at 16 bytes and
-// end there (k a multiple of what 16 bytes hold), vec_*: four
-// consecutive columns of a row, from a multiple of four on, may be read or
-// written at once.
+// end there (k a multiple of what 16 bytes hold).
+// wide: kWideBf16: bf16 y, and the residual if any, eight columns from a multiple of
+// eight on at once, n a multiple of 8; kWideF32: f32 y, n a multiple of 4, rows of a
+// residual at least dword-aligned.
+constexpr int kWideBf16 = 1, kWideF32 = 2;
 struct LinearArgs {
   int m, n, k;
   int x_dtype, w_dtype, y_dtype, bias_dtype, res_dtype, fn;
   int64_t ldx, ldw, ldy, ldr;
   const void *x, *w, *scale, *bias, *res;
   void* y;
-  int aligned, vec_scale, vec_bias, vec_res, vec_y;  // 0 or 1 (words: read through the scalar cache)
-  int wide;  // bf16 y, and the residual if any: eight columns from a multiple of eight on at once, n a multiple of 8
+  int aligned;  // 0 or 1 (words: read through the scalar cache)
+  int wide;     // how results may go out in 16 bytes
 };
 // nwg: workgroups of a persistent launch; scratch may be null with 0 floats.
 hipError_t launch_linear(const LinearArgs& p, int nwg, float* scratch, int64_t scratch_floats, hipStream_t s);

@@ -335,67 +335,172 @@ __device__ __forceinline__ void finish_wide(const LinearItem& it, int wm, int wn
   });
 }
 
-// The same for any other result: f32, rows of any alignment and length.
+// The same for f32 results of a multiple of 4 columns, which go out as a lane
+// holds them.  The residual may be f32, or bf16 of dword-aligned rows.  (4096 x
+// 4096 x 1024 with bias, SiLU and f32 residual 48 us, 26 of them its bytes; by
+// finish_any 61.)
+template <bool FP8, int FAM, int NB>
+__device__ __forceinline__ void finish_f32(const LinearItem& it, int wm, int wn, int rr, int hh,
+                                           f32x4_t (&acc)[Shape<FP8, FAM, NB>::kUnits][Shape<FP8, FAM, NB>::NP][Shape<FP8, FAM, NB>::RF][2]) {
+  using S = Shape<FP8, FAM, NB>;
+  constexpr int RF = S::RF, NU = S::kUnits, NP = S::NP;
+  const LinearArgs p = the_args();
+  const int rows = min(p.m - it.m0, S::kRows), cols = p.n - it.n0;
+  if (cols <= 0) return;
+  __amdgpu_buffer_rsrc_t ry = __builtin_amdgcn_make_buffer_rsrc(
+      reinterpret_cast<float*>(p.y) + (int64_t)it.m0 * p.ldy + it.n0, 0,
+      (int)(((uint32_t)(rows - 1) * (uint32_t)p.ldy + (uint32_t)cols) * 4u), 0x00020000);
+  const uint32_t rs = p.res_dtype == kF32 ? 4u : 2u;
+  __amdgpu_buffer_rsrc_t rr_ = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<char*>(reinterpret_cast<const char*>(p.res)) + (p.res ? ((int64_t)it.m0 * p.ldr + it.n0) * rs : 0), 0,
+      p.res ? (int)(((uint32_t)(rows - 1) * (uint32_t)p.ldr + (uint32_t)cols) * rs) : 0, 0x00020000);
+  const uint32_t ystep = (uint32_t)p.ldy * 4u, rstep = (uint32_t)p.ldr * rs;
+  by_fn(p.fn, [&](auto fn) {
+#pragma unroll
+    for (int q = 0; q < NU * NP; ++q) {
+      const int u = q / NP, b = q % NP;
+      int row = S::row0(wm) + rr, c0 = hh * 4;
+      asm volatile("" : "+v"(row), "+v"(c0));  // offsets are made here, not kept for all pairs
+      uint32_t yo[2], ro[2];
+      f32x4_t b4[2], s4[FP8 ? 2 : 1];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int c = S::col0(wn, b) + j * 16 + c0;
+        yo[j] = c < cols ? (uint32_t)(row + u * 128) * ystep + (uint32_t)c * 4u : 0x80000000u;
+        ro[j] = c < cols ? (uint32_t)(row + u * 128) * rstep + (uint32_t)c * rs : 0x80000000u;
+        b4[j] = p.bias ? columns4(p.bias, p.bias_dtype, it.n0 + c, p.n) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if constexpr (FP8) s4[j] = columns4(p.scale, kBF16, it.n0 + c, p.n);
+      }
+      u32x4_t res[RF][2];
+      if (p.res) {
+#pragma unroll
+        for (int i = 0; i < RF; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t at = ro[j] + (uint32_t)(i * 16) * rstep;
+            if (rs == 4u) {
+              res[i][j] = __builtin_amdgcn_raw_buffer_load_b128(rr_, at, 0, 0);
+            } else {
+              const auto h = __builtin_amdgcn_raw_buffer_load_b64(rr_, at, 0, 0);
+              res[i][j] = u32x4_t{h[0], h[1], 0u, 0u};
+            }
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < RF; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          f32x4_t v = acc[u][b][i][j];
+          if constexpr (FP8) v *= s4[j];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = linear_fn_tile<fn()>(v[e] + b4[j][e]);
+          if (p.res) {
+            const u32x4_t t = res[i][j];
+            v += rs == 4u ? __builtin_bit_cast(f32x4_t, t) : f32x4_t{bf16_lo(t[0]), bf16_hi(t[0]), bf16_lo(t[1]), bf16_hi(t[1])};
+          }
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), ry, yo[j] + (uint32_t)(i * 16) * ystep, 0, 0);
+        }
+      __builtin_amdgcn_sched_barrier(0);  // the next pair's values would not fit beside these
+    }
+  });
+}
+
+// The same for any other result: rows of any alignment and length, by unaligned
+// accesses of four values.  (bf16 rows of 4097 elements, otherwise as above: 62 us;
+// value by value 79; wide rows 39.)
 template <bool FP8, int FAM, int NB>
 __device__ __forceinline__ void finish_any(const LinearItem& it, int wm, int wn, int rr, int hh,
                                            f32x4_t (&acc)[Shape<FP8, FAM, NB>::kUnits][Shape<FP8, FAM, NB>::NP][Shape<FP8, FAM, NB>::RF][2]) {
   using S = Shape<FP8, FAM, NB>;
   constexpr int RF = S::RF, NU = S::kUnits, NP = S::NP;
-  // one x unit and pair of columns at a time: the code is long
+  // two fragments of one x unit and pair of columns at a time: the code is long, and
+  // more values would not fit beside the sums
+  constexpr int RH = 2, NH = RF / RH;
 #pragma unroll 1
-  for (int q = 0; q < NU * NP; ++q) {
-    f32x4_t v[RF][2];
+  for (int h = 0; h < NU * NP * NH; ++h) {
+    const int q = h / NH;
+    f32x4_t v[RH][2];
 #pragma unroll
-    for (int a = 0; a < NU * NP; ++a)
-      if (q == a) {
+    for (int a = 0; a < NU * NP * NH; ++a)
+      if (h == a) {
 #pragma unroll
-        for (int i = 0; i < RF; ++i)
+        for (int i = 0; i < RH; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j) v[i][j] = acc[a / NP][a % NP][i][j];
+          for (int j = 0; j < 2; ++j) v[i][j] = acc[a / NH / NP][a / NH % NP][a % NH * RH + i][j];
       }
     const LinearArgs p = the_args();
-    const int m = it.m0 + (q / NP) * 128 + S::row0(wm) + rr;
-    f32x4_t b4[2];
+    const int m = it.m0 + (q / NP) * 128 + S::row0(wm) + h % NH * (RH * 16) + rr, n0 = it.n0 + S::col0(wn, q % NP) + hh * 4;
+    // all columns of the pair lie in the matrix (or some do not)
+    const bool full = it.n0 + S::col0(wn, q % NP) + 32 <= p.n;
+    f32x4_t res[RH][2], b4[2];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int c = it.n0 + S::col0(wn, q % NP) + j * 16 + hh * 4;
-      const float4 t = p.bias ? load4(p.bias, p.bias_dtype, c, p.n - c, p.vec_bias) : make_float4(0.f, 0.f, 0.f, 0.f);
-      b4[j] = f32x4_t{t.x, t.y, t.z, t.w};
-      if constexpr (FP8) {
-        const float4 s = load4(p.scale, kBF16, c, p.n - c, p.vec_scale);
+    for (int i = 0; i < RH; ++i)
 #pragma unroll
-        for (int i = 0; i < RF; ++i) v[i][j] *= f32x4_t{s.x, s.y, s.z, s.w};
-      }
-    }
-    by_fn(p.fn, [&](auto fn) {
+      for (int j = 0; j < 2; ++j) res[i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if (p.res && full) {
+      // (rows past the matrix: its last one)
+      auto load = [&](auto dtype) {
 #pragma unroll
-      for (int i = 0; i < RF; ++i)
+        for (int i = 0; i < RH; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+          for (int j = 0; j < 2; ++j) {
+            const float4 t = load4(p.res, dtype(), (int64_t)min(m + 16 * i, p.m - 1) * p.ldr + n0 + j * 16, 4);
+            res[i][j] = f32x4_t{t.x, t.y, t.z, t.w};
+          }
+      };
+      if (p.res_dtype == kF32)
+        load(std::integral_constant<int, kF32>{});
+      else
+        load(std::integral_constant<int, kBF16>{});
+    } else if (p.res) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[i][j][e] = linear_fn_tile<fn()>(v[i][j][e] + b4[j][e]);
-    });
-    if (p.res) {
-#pragma unroll
-      for (int i = 0; i < RF; ++i)
+      for (int i = 0; i < RH; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int c = it.n0 + S::col0(wn, q % NP) + j * 16 + hh * 4;
+          const int c = n0 + j * 16;
           if (m + 16 * i < p.m && c < p.n) {
-            const float4 t = load4(p.res, p.res_dtype, (int64_t)(m + 16 * i) * p.ldr + c, p.n - c, p.vec_res);
-            v[i][j] += f32x4_t{t.x, t.y, t.z, t.w};
+            const float4 t = load4(p.res, p.res_dtype, (int64_t)(m + 16 * i) * p.ldr + c, p.n - c);
+            res[i][j] = f32x4_t{t.x, t.y, t.z, t.w};
           }
         }
     }
 #pragma unroll
-    for (int i = 0; i < RF; ++i)
+    for (int j = 0; j < 2; ++j) {
+      const int c = n0 + j * 16;
+      const float4 t = p.bias ? load4(p.bias, p.bias_dtype, c, p.n - c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      b4[j] = f32x4_t{t.x, t.y, t.z, t.w};
+      if constexpr (FP8) {
+        const float4 s = load4(p.scale, kBF16, c, p.n - c);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int c = it.n0 + S::col0(wn, q % NP) + j * 16 + hh * 4;
-        if (m + 16 * i < p.m && c < p.n)
-          store4(p.y, p.y_dtype, (int64_t)(m + 16 * i) * p.ldy + c, p.n - c, p.vec_y,
-                 make_float4(v[i][j][0], v[i][j][1], v[i][j][2], v[i][j][3]));
+        for (int i = 0; i < RH; ++i) v[i][j] *= f32x4_t{s.x, s.y, s.z, s.w};
       }
+    }
+    by_fn(p.fn, [&](auto fn) {
+#pragma unroll
+      for (int i = 0; i < RH; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[i][j][e] = linear_fn_tile<fn()>(v[i][j][e] + b4[j][e]) + res[i][j][e];
+    });
+    auto store = [&](auto dtype, auto all) {
+#pragma unroll
+      for (int i = 0; i < RH; ++i)
+        if (m + 16 * i < p.m) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int c = n0 + j * 16;
+            if (all() || c < p.n)
+              store4(p.y, dtype(), (int64_t)(m + 16 * i) * p.ldy + c, all() ? 4 : p.n - c,
+                     make_float4(v[i][j][0], v[i][j][1], v[i][j][2], v[i][j][3]));
+          }
+        }
+    };
+    using std::integral_constant;
+    if (p.y_dtype == kF32)
+      full ? store(integral_constant<int, kF32>{}, std::true_type{}) : store(integral_constant<int, kF32>{}, std::false_type{});
+    else
+      full ? store(integral_constant<int, kBF16>{}, std::true_type{}) : store(integral_constant<int, kBF16>{}, std::false_type{});
   }
 }
 
@@ -643,8 +748,10 @@ __device__ __forceinline__ void run_shape(unsigned char* smem, uint32_t lds_base
               const int row = u * 128 + S::row0(wm) + i * 16 + rr, col = S::col0(wn, b) + j * 16 + hh * 4;
               *reinterpret_cast<f32x4_t*>(part + row * S::kCols + col) = acc[u][b][i][j];
             }
-    } else if (read_again<int>(&launch_params()->a.wide)) {
+    } else if (const int wide = read_again<int>(&launch_params()->a.wide); wide == kWideBf16) {
       finish_wide<FP8, FAM, NB>(cur, wm, wn, rr, hh, acc);
+    } else if (wide == kWideF32) {
+      finish_f32<FP8, FAM, NB>(cur, wm, wn, rr, hh, acc);
     } else {
       finish_any<FP8, FAM, NB>(cur, wm, wn, rr, hh, acc);
     }

@@ -16,10 +16,14 @@ constexpr int64_t kMaxScratchFloats = (int64_t)24 << 20;
 // was more than 5% behind the best for two): a K step of a tile shape (256 x 256, 256 x 128, 128 x 128, 64 x 128), what
 // an item takes besides, and the launch that adds the pieces' sums with its
 // bytes.
+// Results that do not go out as wide bf16 ones take an item longer (1024 of K, with
+// bias, SiLU and residual in their type: 256 x 256 39 us, f32 48, others 62; 128 x
+// 128 15, 18 and 21).
 struct Costs {
   double step[4], item[4], part[4], sums, sums_float;
 };
 constexpr Costs kBf16 = {{1.25, 0.69, 0.47, 0.40}, {6.0, 5.4, 4.0, 3.6}, {4.0, 2.5, 1.5, 1.0}, 2.5, 1.0e-6};
+constexpr double kResults[3][4] = {{16.0, 8.0, 4.0, 1.5}, {0.0, 0.0, 0.0, 0.0}, {6.0, 3.0, 2.0, 1.0}};  // by `wide`
 constexpr Costs kFp8 = {{1.40, 0.75, 0.55, 0.45}, {6.0, 5.4, 4.0, 3.6}, {4.0, 2.5, 1.5, 1.0}, 2.5, 1.0e-6};
 
 // The busiest workgroup's time in the rounds that hold a items of time ta and
@@ -43,8 +47,9 @@ double rounds_time(int64_t a, double ta, int64_t b, double tb, int nwg) {
   return worst;
 }
 
-LinearPlan choose(int m, int n, int k, bool fp8, int nwg, int64_t max_floats) {
+LinearPlan choose(int m, int n, int k, bool fp8, int wide, int nwg, int64_t max_floats) {
   const Costs& q = fp8 ? kFp8 : kBf16;
+  const double* const result = kResults[wide];
   const int KT = (k + 63) / 64, rem = m % 256;
   const int max_p = std::max(1, std::min(kMaxPieces, KT / kMinPieceSteps));
   LinearPlan best{{}, 1e300};
@@ -70,9 +75,9 @@ LinearPlan choose(int m, int n, int k, bool fp8, int nwg, int64_t max_floats) {
           const int64_t fl = t.floats(n);
           if (fl > max_floats) continue;
           const int s0 = halves - 1, sr = 1 + t.fam;
-          const double t0 = q.item[s0] + (double)KT / p0 * q.step[s0] + (p0 > 1 ? q.part[s0] : 0.0);
-          const double tr = t.fam ? q.item[sr] + (double)KT / pr * q.step[sr] + (pr > 1 ? q.part[sr] : 0.0) : 0.0;
-          double us = c.whole / nwg * (q.item[0] + KT * q.step[0]) + rounds_time(t.rest_items(), t0, last * pr, tr, nwg);
+          const double t0 = q.item[s0] + (double)KT / p0 * q.step[s0] + (p0 > 1 ? q.part[s0] : result[s0]);
+          const double tr = t.fam ? q.item[sr] + (double)KT / pr * q.step[sr] + (pr > 1 ? q.part[sr] : result[sr]) : 0.0;
+          double us = c.whole / nwg * (q.item[0] + KT * q.step[0] + result[0]) + rounds_time(t.rest_items(), t0, last * pr, tr, nwg);
           if (fl) us += q.sums + q.sums_float * (double)fl;
           if (us < best.us) best = LinearPlan{t, us};
         }
@@ -82,10 +87,10 @@ LinearPlan choose(int m, int n, int k, bool fp8, int nwg, int64_t max_floats) {
 
 }  // namespace
 
-const LinearPlan& linear_plan(int m, int n, int k, bool fp8, int nwg, int64_t max_floats) {
+const LinearPlan& linear_plan(int m, int n, int k, bool fp8, int wide, int nwg, int64_t max_floats) {
   // a few sizes come again and again: the last choices of this thread
   struct Seen {
-    int m, n, k, fp8, nwg;
+    int m, n, k, fp8, wide, nwg;
     int64_t max_floats;
     LinearPlan plan;
   };
@@ -93,8 +98,8 @@ const LinearPlan& linear_plan(int m, int n, int k, bool fp8, int nwg, int64_t ma
   max_floats = std::min(max_floats, kMaxScratchFloats);
   const uint32_t h = ((uint32_t)m * 2654435761u ^ (uint32_t)n * 2246822519u ^ (uint32_t)k * 3266489917u) >> 26;
   Seen& s = seen[h];
-  if (s.m != m || s.n != n || s.k != k || s.fp8 != (int)fp8 || s.nwg != nwg || s.max_floats != max_floats)
-    s = Seen{m, n, k, (int)fp8, nwg, max_floats, choose(m, n, k, fp8, nwg, max_floats)};
+  if (s.m != m || s.n != n || s.k != k || s.fp8 != (int)fp8 || s.wide != wide || s.nwg != nwg || s.max_floats != max_floats)
+    s = Seen{m, n, k, (int)fp8, wide, nwg, max_floats, choose(m, n, k, fp8, wide, nwg, max_floats)};
   return s.plan;
 }
 
@@ -133,10 +138,8 @@ const LinearPlan* linear_tiles_plan(const LinearArgs& p, int nwg, int64_t max_fl
   if (std::max({p.ldx, p.ldw, p.ldy, p.res ? p.ldr : 0}) >= 1 << 22) return nullptr;
   const RowsPlan rows = rows_plan(p.m, p.n, p.k, 2, p.w_dtype == kFP8 ? 1 : 2, nwg);
   if (rows.us < 16.0) return nullptr;  // less than any tiled product takes
-  const LinearPlan& t = linear_plan(p.m, p.n, p.k, p.w_dtype == kFP8, nwg, max_floats);
-  // results that do not go out in 16 bytes take a tile some 15 us more
-  const double slow = p.wide ? 0.0 : 15.0 * ((t.cut.items + nwg - 1) / nwg);
-  return t.us + slow < rows.us ? &t : nullptr;
+  const LinearPlan& t = linear_plan(p.m, p.n, p.k, p.w_dtype == kFP8, p.wide, nwg, max_floats);
+  return t.us < rows.us ? &t : nullptr;
 }
 
 }  // namespace aep

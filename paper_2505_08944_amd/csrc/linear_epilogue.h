@@ -8,24 +8,28 @@
 
 namespace aep {
 
-// Four consecutive values of a bf16 or f32 row from column c on; vec: they may
-// be read at once (16 or 8 byte aligned), else only the first n of them are.
-__device__ __forceinline__ float4 load4(const void* p, int dtype, int64_t at, int n, bool vec) {
+// Four consecutive values of a bf16 or f32 row from `at` on, of which n exist.
+// At once whatever their alignment: the load path takes unaligned addresses.
+__device__ __forceinline__ float4 load4(const void* p, int dtype, int64_t at, int n) {
   float v[4] = {0.f, 0.f, 0.f, 0.f};
   if (dtype == kF32) {
     const float* q = reinterpret_cast<const float*>(p) + at;
-    if (vec && n >= 4) return *reinterpret_cast<const float4*>(q);
+    if (n >= 4) {
+      __builtin_memcpy(v, q, 16);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) v[i] = q[i];
+      for (int i = 0; i < 3; ++i)
+        if (i < n) v[i] = q[i];
+    }
   } else {
     const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + at;
-    if (vec && n >= 4) {
-      const uint2 w = *reinterpret_cast<const uint2*>(q);
+    if (n >= 4) {
+      uint2 w;
+      __builtin_memcpy(&w, q, 8);
       return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 3; ++i)
       if (i < n) v[i] = bf16_lo(q[i]);
   }
   return make_float4(v[0], v[1], v[2], v[3]);
@@ -41,26 +45,27 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-__device__ __forceinline__ void store4(void* p, int dtype, int64_t at, int n, bool vec, const float4 v) {
+__device__ __forceinline__ void store4(void* p, int dtype, int64_t at, int n, const float4 v) {
   const float a[4] = {v.x, v.y, v.z, v.w};
   if (dtype == kF32) {
     float* q = reinterpret_cast<float*>(p) + at;
-    if (vec && n >= 4) {
-      *reinterpret_cast<float4*>(q) = v;
-      return;
-    }
+    if (n >= 4) {
+      __builtin_memcpy(q, a, 16);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) q[i] = a[i];
+      for (int i = 0; i < 3; ++i)
+        if (i < n) q[i] = a[i];
+    }
   } else {
     uint16_t* q = reinterpret_cast<uint16_t*>(p) + at;
-    if (vec && n >= 4) {
-      *reinterpret_cast<uint2*>(q) = make_uint2(bf16_pair(a[0], a[1]), bf16_pair(a[2], a[3]));
-      return;
-    }
+    if (n >= 4) {
+      const uint2 w = make_uint2(bf16_pair(a[0], a[1]), bf16_pair(a[2], a[3]));
+      __builtin_memcpy(q, &w, 8);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < n) q[i] = (uint16_t)bf16_bits(a[i]);
+      for (int i = 0; i < 3; ++i)
+        if (i < n) q[i] = (uint16_t)bf16_bits(a[i]);
+    }
   }
 }
 
@@ -123,14 +128,14 @@ __device__ __forceinline__ void linear_out4(const LinearArgs& p, int64_t m, int 
   const int64_t at = m * p.ldr + c;
   float4 b = make_float4(0.f, 0.f, 0.f, 0.f), r = b;
   if (p.scale) {
-    const float4 q = load4(p.scale, kBF16, c, left, p.vec_scale);
+    const float4 q = load4(p.scale, kBF16, c, left);
     s = make_float4(s.x * q.x, s.y * q.y, s.z * q.z, s.w * q.w);
   }
-  if (p.bias) b = load4(p.bias, p.bias_dtype, c, left, p.vec_bias);
-  if (p.res) r = load4(p.res, p.res_dtype, at, left, p.vec_res);
+  if (p.bias) b = load4(p.bias, p.bias_dtype, c, left);
+  if (p.res) r = load4(p.res, p.res_dtype, at, left);
   s = make_float4(linear_fn(p.fn, s.x + b.x) + r.x, linear_fn(p.fn, s.y + b.y) + r.y, linear_fn(p.fn, s.z + b.z) + r.z,
                   linear_fn(p.fn, s.w + b.w) + r.w);
-  store4(p.y, p.y_dtype, m * p.ldy + c, left, p.vec_y, s);
+  store4(p.y, p.y_dtype, m * p.ldy + c, left, s);
 }
 
 }  // namespace aep

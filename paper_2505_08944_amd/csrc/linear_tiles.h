@@ -34,13 +34,14 @@ struct LinearCut {
   }
 };
 
-// The cheapest cut of a product of these sizes on nwg workgroups whose pieces'
-// sums take at most max_floats of scratch, and its time.
+// The cheapest cut of a product of these sizes, its results going out as `wide`
+// says, on nwg workgroups whose pieces' sums take at most max_floats of scratch,
+// and its time.
 struct LinearPlan {
   LinearCut cut;
   double us;
 };
-const LinearPlan& linear_plan(int m, int n, int k, bool fp8, int nwg, int64_t max_floats);
+const LinearPlan& linear_plan(int m, int n, int k, bool fp8, int wide, int nwg, int64_t max_floats);
 // The row kernel's tile (fragments of rows and columns) and its time.
 struct RowsPlan {
   int rf, cf;

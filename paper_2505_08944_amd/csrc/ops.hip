@@ -83,8 +83,7 @@ int persistent_workgroups() {
 
 LinearArgs linear_args(const aep_linear_desc& l, const void* x, const void* w, const void* scale, const void* bias,
                        const void* residual, void* y) {
-  const int xs = esize(l.x_dtype), ws = esize(l.w_dtype), ys = esize(l.y_dtype), bs = esize(l.bias_dtype),
-            rs = esize(l.res_dtype);
+  const int xs = esize(l.x_dtype), ws = esize(l.w_dtype);
   LinearArgs p{};
   p.m = l.m;
   p.n = l.n;
@@ -107,12 +106,14 @@ LinearArgs linear_args(const aep_linear_desc& l, const void* x, const void* w, c
   p.y = y;
   p.aligned = !off(x, 16) && !off(w, 16) && (l.ldx * xs) % 16 == 0 && (l.ldw * ws) % 16 == 0 &&
               ((int64_t)l.k * xs) % 16 == 0 && ((int64_t)l.k * ws) % 16 == 0;
-  p.vec_scale = !off(scale, 8);
-  p.vec_bias = !off(bias, 4 * bs);
-  p.vec_res = !off(residual, 4 * rs) && l.ldr % 4 == 0;
-  p.vec_y = !off(y, 4 * ys) && l.ldy % 4 == 0;
-  p.wide = l.y_dtype == AEP_BF16 && l.n % 8 == 0 && !off(y, 16) && l.ldy % 8 == 0 &&
-           (!residual || (l.res_dtype == AEP_BF16 && !off(residual, 16) && l.ldr % 8 == 0));
+  const bool f32_res = l.res_dtype == AEP_F32;
+  if (l.y_dtype == AEP_BF16 && l.n % 8 == 0 && !off(y, 16) && l.ldy % 8 == 0 &&
+      (!residual || (!f32_res && !off(residual, 16) && l.ldr % 8 == 0)))
+    p.wide = kWideBf16;
+  // (a tile's offsets fit 31 bits)
+  if (l.y_dtype == AEP_F32 && l.n % 4 == 0 && l.ldy < 1 << 21 &&
+      (!residual || (f32_res ? l.ldr < 1 << 21 : !off(residual, 4) && l.ldr % 2 == 0)))
+    p.wide = kWideF32;
   return p;
 }
 
@@ -140,10 +141,13 @@ aep_status aep_linear_workspace(const aep_linear_desc* l, size_t* bytes) {
   if (!bytes) return AEP_ERR_INVALID_ARG;
   *bytes = 0;
   if (l->m == 0) return AEP_OK;
-  // as for aligned pointers
-  const LinearArgs p = linear_args(*l, nullptr, nullptr, nullptr, nullptr, nullptr, nullptr);
-  if (const LinearPlan* t = linear_tiles_plan(p, persistent_workgroups(), INT64_MAX))
-    *bytes = (size_t)t->cut.floats(p.n) * 4;
+  // as for aligned pointers, with a residual or without
+  const void* const some = reinterpret_cast<const void*>(16);
+  for (const void* residual : {(const void*)nullptr, some}) {
+    const LinearArgs p = linear_args(*l, some, some, some, some, residual, nullptr);
+    if (const LinearPlan* t = linear_tiles_plan(p, persistent_workgroups(), INT64_MAX))
+      *bytes = std::max(*bytes, (size_t)t->cut.floats(p.n) * 4);
+  }
   return AEP_OK;
 }
 

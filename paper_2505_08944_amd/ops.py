@@ -146,7 +146,7 @@ class Linear(_Fixed):
         if out is not None:
             _rows(out, "out", (self.out_dtype,), (m, n), dev)
         d = L.LinearDesc(m, n, k, x_dtype, w_dtype, y_dtype, bias_dtype,
-                         L.AEP_F32 if residual is None else _CODE[residual.dtype], self._fn, _ld(x), self._ldw,
+                         y_dtype if residual is None else _CODE[residual.dtype], self._fn, _ld(x), self._ldw,
                          n if out is None else _ld(out), n if residual is None else _ld(residual))
         b = ctypes.c_size_t()
         L.check(self._lib.aep_linear_workspace(ctypes.byref(d), ctypes.byref(b)), "aep_linear_workspace")

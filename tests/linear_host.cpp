@@ -6,6 +6,10 @@
 static const void* kernarg;
 #define __builtin_amdgcn_kernarg_segment_ptr() (kernarg)
 #define __builtin_amdgcn_exp2f(x) exp2f(x)
+struct TwoWords {
+  unsigned operator[](int) const { return 0; }
+};
+#define __builtin_amdgcn_raw_buffer_load_b64(...) (TwoWords{})
 
 #include "linear_device.inc"
 
@@ -48,7 +52,7 @@ static long violations(int k, int whole, int rest, int halves, int p0, int fam, 
   p.k = k;
   p.ldx = p.ldw = (k + 15) / 16 * 16;
   p.ldy = p.n;
-  p.wide = 1;
+  p.wide = kWideBf16;
   static uint16_t scale[2048];
   p.scale = FP8 ? scale : nullptr;
   p.w_dtype = FP8 ? kFP8 : kBF16;

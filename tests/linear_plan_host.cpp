@@ -23,7 +23,7 @@ extern "C" void plan(int m, int n, int k, int fp8, int wide, int nwg, long long 
   p.aligned = 1;
   p.wide = wide;
   const LinearPlan* t = linear_tiles_plan(p, nwg, max_floats);
-  const LinearPlan& any = linear_plan(m, n, k, fp8, nwg, max_floats);
+  const LinearPlan& any = linear_plan(m, n, k, fp8, wide, nwg, max_floats);
   const LinearCut& c = any.cut;
   const RowsPlan r = rows_plan(m, n, k, 2, fp8 ? 1 : 2, nwg);
   const int v[] = {t != nullptr, c.whole, c.rest, c.halves, c.p0, c.fam, c.pr, c.lrow, c.items, c.nrow, c.ncol, r.rf, r.cf};

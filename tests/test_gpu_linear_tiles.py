@@ -164,3 +164,28 @@ def test_graphs_on_two_streams_and_equal_bits(M, N, K, wdt):
         mine = lin(x, r)
         torch.cuda.synchronize()
         assert all(torch.equal(o, ref) for o in outs) and torch.equal(mine, ref), i
+
+
+@pytest.mark.parametrize("M,N,K", [(1100, 4103, 1024), (2050, 2049, 1032), (640, 4099, 4096), (1100, 4108, 1024)])
+@pytest.mark.parametrize("out,res", [("bf16", None), ("bf16", "bf16"), ("bf16", "f32"), ("f32", None), ("f32", "bf16"),
+                                     ("f32", "f32")])
+def test_results_of_any_alignment(M, N, K, out, res):
+    """Odd numbers of columns; results and residuals whose rows start anywhere; what lies around them stays."""
+    x, w, s, b, _ = gpu_make(M, N, K, "bf16", None, seed=17)
+    for i, (off, pad) in enumerate(((0, 0), (1, 3), (2, 2), (4, 1), (0, (-N) % 8))):
+        fn = FNS[(i + N) % 5]
+        log(f"tiles {M}x{N}x{K} {out} residual {res} offset {off} padding {pad} {fn}")
+
+        def at(dtype):
+            buf = torch.full((off + (M + 2) * (N + pad),), 77.0, dtype=TYPES[dtype], device="cuda")
+            return buf, buf[off:].view(M + 2, N + pad)[1:M + 1, :N]
+
+        buf, y = at(out)
+        r = None
+        if res:
+            r = at(res)[1]
+            r.copy_(torch.randn(M, N, device="cuda"))
+        aep.linear(x, w, bias=b, activation=fn, residual=r, out=y, out_dtype=TYPES[out])
+        gpu_check(y, x, w, s, b, r, fn, (M, N, K, out, res, off, pad))
+        y.fill_(77.0)
+        assert (buf == 77.0).all()
