@@ -15,7 +15,7 @@
 // (main loop of a 256 x 256 tile 1.46 .. 1.56 PFLOP/s), and below that size a CU's
 // way to L2 (76 GB/s: a 128 x 128 tile moves twice the bytes per operation, so
 // that shape is for what is left over).  Measured: 4096 x 14336 x 4096 with bias
-// and SiLU 348 .. 380 us (1.27 .. 1.38 PFLOP/s), 2048 x 4096 x 14336 fp8 200 (1.2;
+// and SiLU 348 .. 380 us (1.27 .. 1.38 PFLOP/s), 2048 x 4096 x 14336 fp8 189 (1.27;
 // one round of 128 tiles cut in halves), 777 x 4096 x 4096 38 (0.68; 3.04 row
 // tiles).  256 x 128 tiles have four waves along their rows (two: 5% longer).
 //
@@ -722,11 +722,15 @@ __device__ __forceinline__ void run_shape(unsigned char* smem, uint32_t lds_base
         next_k();
         wait_loads<kFlight>();
         wait_lds();
-#pragma unroll
-        for (int q = 0; q < NP; ++q) widen(q, false);
         slot_end();
+        // fp8 W is widened between the MFMAs: the other slot, of reads, is the longer one
+        // (2048 x 4096 x 14336 in halves 224 -> 203 us, 1024 rows of 128 144 -> 132;
+        // with four phases per step it makes no difference)
 #pragma unroll
-        for (int q = 0; q < NP; ++q) mma(0, q);
+        for (int q = 0; q < NP; ++q) {
+          widen(q, false);
+          mma(0, q);
+        }
         slot_end();
       }
       stage = ns;

@@ -24,7 +24,7 @@ struct Costs {
 };
 constexpr Costs kBf16 = {{1.25, 0.69, 0.47, 0.40}, {6.0, 5.4, 4.0, 3.6}, {4.0, 2.5, 1.5, 1.0}, 2.5, 1.0e-6};
 constexpr double kResults[3][4] = {{16.0, 8.0, 4.0, 1.5}, {0.0, 0.0, 0.0, 0.0}, {6.0, 3.0, 2.0, 1.0}};  // by `wide`
-constexpr Costs kFp8 = {{1.40, 0.75, 0.55, 0.45}, {6.0, 5.4, 4.0, 3.6}, {4.0, 2.5, 1.5, 1.0}, 2.5, 1.0e-6};
+constexpr Costs kFp8 = {{1.40, 0.70, 0.50, 0.43}, {6.0, 5.4, 4.0, 3.6}, {4.0, 2.5, 1.5, 1.0}, 2.5, 1.0e-6};
 
 // The busiest workgroup's time in the rounds that hold a items of time ta and
 // then b of time tb: these are dealt in turn, odd rounds in reverse, so a load
