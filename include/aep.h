@@ -482,7 +482,8 @@ aep_status aep_linear_workspace(const aep_linear_desc* l, size_t* bytes);
 
 /* Run it.  Device pointers: x, w, y as described, aligned to their elements
  * (rows of 16-byte aligned x and w, as rows of a multiple of 8 elements, 16
- * for FP8, in an aligned matrix are, take the fast loads); scale [n] bf16 for
+ * for FP8, in an aligned matrix are, take the fast loads; others of large products
+ * are copied to such rows in d_ws first, if it is given); scale [n] bf16 for
  * FP8 weights and NULL for others; bias [n] or NULL; residual or NULL.  y may
  * be the residual itself (same type and row stride); apart from that it must
  * not overlap any input.  d_ws: 16-byte aligned scratch of ws_bytes, or NULL:

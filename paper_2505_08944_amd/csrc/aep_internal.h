@@ -229,8 +229,8 @@ hipError_t launch_route_queue(const float* logits, const float* bias, int T, con
 constexpr int kF32 = 0, kBF16 = 1, kFP8 = 2;
 constexpr int kFnNone = 0, kFnRelu = 1, kFnSilu = 2, kFnGelu = 3, kFnGeluTanh = 4;
 
-// A checked dense product.  aligned: rows of x and w start at 16 bytes and
-// end there (k a multiple of what 16 bytes hold).
+// A checked dense product.  x_aligned, w_aligned: its rows start at 16 bytes;
+// aligned: both do, and end there (k a multiple of what 16 bytes hold).
 // wide: kWideBf16: bf16 y, and the residual if any, eight columns from a multiple of
 // eight on at once, n a multiple of 8; kWideF32: f32 y, n a multiple of 4, rows of a
 // residual at least dword-aligned.
@@ -241,7 +241,7 @@ struct LinearArgs {
   int64_t ldx, ldw, ldy, ldr;
   const void *x, *w, *scale, *bias, *res;
   void* y;
-  int aligned;  // 0 or 1 (words: read through the scalar cache)
+  int x_aligned, w_aligned, aligned;  // 0 or 1 (words: read through the scalar cache)
   int wide;     // how results may go out in 16 bytes
 };
 // nwg: workgroups of a persistent launch; scratch may be null with 0 floats.

@@ -2,9 +2,9 @@
 //
 // Row kernel (linear_rows_kernel): output tiles of up to 64 x 32, the waves of a
 // workgroup split K and add their sums in LDS, in wave order.  It is for
-// products that one operand's stream bounds (few rows, or few channels), for f32
-// and for rows of any alignment; the tile kernel (k_linear_tiles.hip) takes the
-// others (linear_cut.hip).  Measured, us, with the operands in the Infinity Cache
+// products that one operand's stream bounds (few rows, or few channels) and for
+// f32; the tile kernel (k_linear_tiles.hip) takes the others (linear_cut.hip), rows
+// of other alignments than 16 bytes through aligned copies.  Measured, us, with the operands in the Infinity Cache
 // and (in brackets) in HBM: 32 x 4096 x 4096 7.9 (11.9; its bytes at the rate of
 // a large copy 6.6), 1 x 14336 x 4096 fp8 11.5 (15.1; 11.3), 8192 x 64 x 2048 8.9
 // (9.1; 6.9), an empty launch 1.5.
@@ -256,9 +256,45 @@ static hipError_t rows_align(const LinearArgs& p, int ncu, hipStream_t s) {
   return p.aligned ? rows_tile<XT, WT, true>(p, ncu, s) : rows_tile<XT, WT, false>(p, ncu, s);
 }
 
+// Rows of k values of any alignment to rows of `per_row` times 16 bytes, zeros
+// behind the values: 16 bytes per thread.
+template <typename T>
+__global__ __launch_bounds__(256) void linear_align_kernel(const T* __restrict__ src, int64_t ld, int rows, int k,
+                                                           int per_row, uint4* __restrict__ dst) {
+  constexpr int PER = 16 / (int)sizeof(T);
+  const int i = blockIdx.x * 256 + threadIdx.x, row = i / per_row, c = (i - row * per_row) * PER;
+  if (row >= rows) return;
+  const T* at = src + row * ld + c;
+  dst[i] = k - c >= PER ? load16<false>(at) : load16_end<false>(at, k - c);
+}
+template <typename T>
+static hipError_t align_rows(const void* src, int64_t ld, int rows, int k, int64_t bytes, void* dst, hipStream_t s) {
+  const int64_t chunks = bytes / 16;  // (of at most 512 MiB)
+  linear_align_kernel<<<(unsigned)((chunks + 255) / 256), 256, 0, s>>>(reinterpret_cast<const T*>(src), ld, rows, k,
+                                                                       (int)(chunks / rows), reinterpret_cast<uint4*>(dst));
+  return hipGetLastError();
+}
+
 hipError_t launch_linear(const LinearArgs& p, int nwg, float* scratch, int64_t scratch_floats, hipStream_t s) {
-  if (const LinearPlan* t = linear_tiles_plan(p, nwg, scratch_floats))
-    return launch_linear_tiles(p, t->cut, nwg, scratch, s);
+  if (const TilesPlan t = linear_tiles_plan(p, nwg, scratch_floats); t.use) {
+    LinearArgs q = p;
+    char* copy = reinterpret_cast<char*>(scratch + t.cut.floats(p.n));
+    q.k = t.k;
+    hipError_t e = hipSuccess;
+    if (t.x_bytes) {
+      e = align_rows<uint16_t>(p.x, p.ldx, p.m, p.k, t.x_bytes, copy, s);
+      q.x = copy;
+      q.ldx = t.k;
+      copy += t.x_bytes;
+    }
+    if (t.w_bytes && e == hipSuccess) {
+      e = p.w_dtype == kFP8 ? align_rows<uint8_t>(p.w, p.ldw, p.n, p.k, t.w_bytes, copy, s)
+                            : align_rows<uint16_t>(p.w, p.ldw, p.n, p.k, t.w_bytes, copy, s);
+      q.w = copy;
+      q.ldw = t.k;
+    }
+    return e == hipSuccess ? launch_linear_tiles(q, t.cut, nwg, scratch, s) : e;
+  }
   if (p.w_dtype == kF32) return rows_align<float, float>(p, nwg, s);
   if (p.w_dtype == kBF16) return rows_align<uint16_t, uint16_t>(p, nwg, s);
   return rows_align<uint16_t, uint8_t>(p, nwg, s);

@@ -10,6 +10,7 @@ namespace {
 constexpr int kMaxPieces = 8;
 constexpr int kMinPieceSteps = 4;  // K steps of a piece
 constexpr int64_t kMaxScratchFloats = (int64_t)24 << 20;
+constexpr int64_t kMaxCopiedBytes = (int64_t)512 << 20;  // of operands with unaligned rows
 
 // us, fitted to launches of 65 .. 4096 rows with their operands in the Infinity
 // Cache, each timed under all cuts worth trying (of 34 products, the chosen cut
@@ -132,14 +133,28 @@ RowsPlan rows_plan(int m, int n, int k, int x_bytes, int w_bytes, int ncu) {
 // of 48 .. 2048 rows, 64 .. 14336 columns and K = 1024 .. 14336: 384 x 4096 x
 // 4096 rows 30, tiles 27 us; 256 x 4096 x 4096 22 and 25; 2048 x 1024 x 1024 15
 // and 17; 96 x 14336 x 4096 32 and 29; 2048 x 4096 x 4096 160 and 47).  They need
-// aligned rows, and offsets within a tile that fit 31 bits.
-const LinearPlan* linear_tiles_plan(const LinearArgs& p, int nwg, int64_t max_floats) {
-  if (p.w_dtype == kF32 || !p.aligned || p.n < 8) return nullptr;
-  if (std::max({p.ldx, p.ldw, p.ldy, p.res ? p.ldr : 0}) >= 1 << 22) return nullptr;
-  const RowsPlan rows = rows_plan(p.m, p.n, p.k, 2, p.w_dtype == kFP8 ? 1 : 2, nwg);
-  if (rows.us < 16.0) return nullptr;  // less than any tiled product takes
-  const LinearPlan& t = linear_plan(p.m, p.n, p.k, p.w_dtype == kFP8, p.wide, nwg, max_floats);
-  return t.us < rows.us ? &t : nullptr;
+// offsets within a tile that fit 31 bits.  With rows that have to be copied first:
+// 777 x 2000 x 2001 rows 41, tiles 32; 1000 x 5000 x 2731 149 and 57; 2048 x 4096 x
+// 4095 325 and 81, fp8 288 and 79; 4096 x 4096 x 1001 235 and 48.
+TilesPlan linear_tiles_plan(const LinearArgs& p, int nwg, int64_t max_floats) {
+  TilesPlan r{};
+  if (p.w_dtype == kF32 || p.n < 8) return r;
+  const int es = p.w_dtype == kFP8 ? 1 : 2, per = 16 / es;
+  if (p.k >= 1 << 22 || std::max(p.ldy, p.res ? p.ldr : 0) >= 1 << 22) return r;
+  r.k = (p.k + per - 1) / per * per;
+  if (r.k != p.k || !p.x_aligned) r.x_bytes = (int64_t)p.m * r.k * 2;
+  if (r.k != p.k || !p.w_aligned) r.w_bytes = (int64_t)p.n * r.k * es;
+  if ((!r.x_bytes && p.ldx >= 1 << 22) || (!r.w_bytes && p.ldw >= 1 << 22)) return r;
+  const int64_t copied = r.x_bytes + r.w_bytes;
+  if (copied > kMaxCopiedBytes || copied / 4 > max_floats) return r;
+  // (rows of any alignment take the row kernel half as long again)
+  const double rows = rows_plan(p.m, p.n, p.k, 2, es, nwg).us * (p.aligned ? 1.0 : 1.5);
+  if (rows < 16.0) return r;  // less than any tiled product takes
+  const LinearPlan& t = linear_plan(p.m, p.n, r.k, es == 1, p.wide, nwg, max_floats - copied / 4);
+  const double copies = (r.x_bytes ? 2.5 : 0.0) + (r.w_bytes ? 2.5 : 0.0) + (double)copied / 1.5e6;
+  r.cut = t.cut;
+  r.use = t.us + copies < rows;
+  return r;
 }
 
 }  // namespace aep

@@ -48,8 +48,17 @@ struct RowsPlan {
   double us;
 };
 RowsPlan rows_plan(int m, int n, int k, int x_bytes, int w_bytes, int ncu);
-// Whether the tile kernel takes the product, and then how (null: the row kernel).
-const LinearPlan* linear_tiles_plan(const LinearArgs& p, int nwg, int64_t max_floats);
+// Whether the tile kernel takes the product (or the row kernel), and then how.
+// Operands whose rows are not 16-byte aligned are copied to rows of k values first,
+// zeros behind their own, into the scratch behind the pieces' sums.
+struct TilesPlan {
+  bool use;
+  LinearCut cut;
+  int k;
+  int64_t x_bytes, w_bytes;  // of the copies (0: none)
+  int64_t bytes(int n) const { return cut.floats(n) * 4 + x_bytes + w_bytes; }
+};
+TilesPlan linear_tiles_plan(const LinearArgs& p, int nwg, int64_t max_floats);
 hipError_t launch_linear_tiles(const LinearArgs& p, const LinearCut& c, int nwg, float* scratch, hipStream_t s);
 
 }  // namespace aep

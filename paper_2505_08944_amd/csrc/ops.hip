@@ -104,8 +104,9 @@ LinearArgs linear_args(const aep_linear_desc& l, const void* x, const void* w, c
   p.bias = bias;
   p.res = residual;
   p.y = y;
-  p.aligned = !off(x, 16) && !off(w, 16) && (l.ldx * xs) % 16 == 0 && (l.ldw * ws) % 16 == 0 &&
-              ((int64_t)l.k * xs) % 16 == 0 && ((int64_t)l.k * ws) % 16 == 0;
+  p.x_aligned = !off(x, 16) && (l.ldx * xs) % 16 == 0;
+  p.w_aligned = !off(w, 16) && (l.ldw * ws) % 16 == 0;
+  p.aligned = p.x_aligned && p.w_aligned && ((int64_t)l.k * xs) % 16 == 0 && ((int64_t)l.k * ws) % 16 == 0;
   const bool f32_res = l.res_dtype == AEP_F32;
   if (l.y_dtype == AEP_BF16 && l.n % 8 == 0 && !off(y, 16) && l.ldy % 8 == 0 &&
       (!residual || (!f32_res && !off(residual, 16) && l.ldr % 8 == 0)))
@@ -145,8 +146,8 @@ aep_status aep_linear_workspace(const aep_linear_desc* l, size_t* bytes) {
   const void* const some = reinterpret_cast<const void*>(16);
   for (const void* residual : {(const void*)nullptr, some}) {
     const LinearArgs p = linear_args(*l, some, some, some, some, residual, nullptr);
-    if (const LinearPlan* t = linear_tiles_plan(p, persistent_workgroups(), INT64_MAX))
-      *bytes = std::max(*bytes, (size_t)t->cut.floats(p.n) * 4);
+    if (const TilesPlan t = linear_tiles_plan(p, persistent_workgroups(), INT64_MAX); t.use)
+      *bytes = std::max(*bytes, (size_t)t.bytes(p.n));
   }
   return AEP_OK;
 }

@@ -20,13 +20,14 @@ extern "C" void plan(int m, int n, int k, int fp8, int wide, int nwg, long long 
   p.x_dtype = kBF16;
   p.ldx = p.ldw = k;
   p.ldy = p.ldr = n;
-  p.aligned = 1;
+  p.x_aligned = p.w_aligned = 1;
+  p.aligned = k % (fp8 ? 16 : 8) == 0;
   p.wide = wide;
-  const LinearPlan* t = linear_tiles_plan(p, nwg, max_floats);
+  const TilesPlan t = linear_tiles_plan(p, nwg, max_floats);
   const LinearPlan& any = linear_plan(m, n, k, fp8, wide, nwg, max_floats);
   const LinearCut& c = any.cut;
   const RowsPlan r = rows_plan(m, n, k, 2, fp8 ? 1 : 2, nwg);
-  const int v[] = {t != nullptr, c.whole, c.rest, c.halves, c.p0, c.fam, c.pr, c.lrow, c.items, c.nrow, c.ncol, r.rf, r.cf};
+  const int v[] = {t.use, c.whole, c.rest, c.halves, c.p0, c.fam, c.pr, c.lrow, c.items, c.nrow, c.ncol, r.rf, r.cf};
   for (int i = 0; i < 13; ++i) out[i] = v[i];
   us[0] = any.us;
   us[1] = r.us;

@@ -189,3 +189,65 @@ def test_results_of_any_alignment(M, N, K, out, res):
         gpu_check(y, x, w, s, b, r, fn, (M, N, K, out, res, off, pad))
         y.fill_(77.0)
         assert (buf == 77.0).all()
+
+
+@pytest.mark.parametrize("M,N,K,wdt", [(1000, 5000, 2731, "bf16"), (777, 2003, 2001, "bf16"), (2048, 4096, 1000, "fp8"),
+                                       (1000, 5000, 2731, "fp8"), (1100, 4104, 1024, "bf16"), (1100, 4104, 2048, "fp8")])
+def test_operands_of_any_alignment(M, N, K, wdt):
+    """Rows that start anywhere are copied into the scratch: x's, W's, or both; with too little of it the product
+    runs without.  What lies between the rows (NaN) and behind the scratch is not used."""
+    b = torch.randn(N, device="cuda")
+    lib, need = L.lib(), ctypes.c_size_t()
+    taken = 0
+    for xo, xp, wo, wp in ((0, 0, 0, 0), (1, 0, 0, 0), (0, 3, 0, 0), (0, 0, 1, 0), (0, 0, 0, 5), (3, 1, 2, 7)):
+        def at(r, c, off, pad, dtype, scale):
+            t = torch.full((off + r * (c + pad),), float("nan"), device="cuda")
+            t[off:].view(r, c + pad)[:, :c] = torch.randn(r, c, device="cuda") * scale
+            return t.to(dtype)[off:].view(r, c + pad)[:, :c]
+
+        x = at(M, K, xo, xp, torch.bfloat16, 1.0)
+        w = at(N, K, wo, wp, TYPES[wdt], 50.0 if wdt == "fp8" else 0.5)
+        s = (torch.rand(N, device="cuda") * 0.02 + 0.001).to(torch.bfloat16) if wdt == "fp8" else None
+        log(f"operands {M}x{N}x{K} {wdt} offsets {xo} {wo} padding {xp} {wp}")
+        y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+        d = L.LinearDesc(M, N, K, L.AEP_BF16, L.AEP_FP8_E4M3 if wdt == "fp8" else L.AEP_BF16, L.AEP_BF16, L.AEP_F32,
+                         L.AEP_BF16, L.AEP_FN_GELU, K + xp, K + wp, N, N)
+        L.check(lib.aep_linear_workspace(ctypes.byref(d), ctypes.byref(need)), "workspace")
+        full = M * (K + 16) * 2 + N * (K + 16) * 2 + need.value  # enough for copies of misaligned pointers as well
+        for n in (0, need.value, need.value // 2, full // 16 * 16):
+            ws = torch.full((n + 64,), 255, dtype=torch.uint8, device="cuda")
+            y.fill_(0)
+            L.check(lib.aep_linear(ctypes.byref(d), x.data_ptr(), w.data_ptr(), None if s is None else s.data_ptr(),
+                                   b.data_ptr(), None, y.data_ptr(), ws.data_ptr() if n else None, n,
+                                   torch.cuda.current_stream().cuda_stream), "aep_linear")
+            gpu_check(y, x, w, s, b, None, "gelu", (M, N, K, wdt, xo, xp, wo, wp, n))
+            assert (ws[n:] == 255).all()
+            taken += int(n > 0 and not bool((ws[:n] == 255).all()))
+        lin = aep.linear(x, w, scale=s, bias=b, activation="gelu")
+        gpu_check(lin, x, w, s, b, None, "gelu", (M, N, K, wdt, xo, xp, wo, wp, "binding"))
+    assert taken  # copies were made
+
+
+def test_copied_operands_in_graphs():
+    x, w, s, b, r = gpu_make(1000, 5000, 2731, "bf16", "bf16", seed=21)
+    lin = aep.Linear(w, bias=b, activation="silu")
+    ref = lin(x, r)
+    gpu_check(ref, x, w, s, b, r, "silu", "eager")
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for _ in range(2):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            outs.append(lin(x, r))
+        graphs.append(gr)
+    torch.cuda.synchronize()
+    for i in range(3):
+        for o in outs:
+            o.fill_(0)
+        torch.cuda.synchronize()
+        for gr in graphs:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                gr.replay()
+        mine = lin(x, r)
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, ref) for o in outs) and torch.equal(mine, ref), i
