@@ -413,8 +413,10 @@ __device__ __noinline__ int select_exact(const float* __restrict__ l, const floa
                                          double* __restrict__ val) {
   const double none = -__builtin_inf();
   const Held<LANES, GM> held{g, r.E};
+  // without a bias experts are picked by their logits, and so are groups by their best one
+  const bool by_logit = !bias && r.group_top == 1;
   double top = none, total = 0.0;
-  if (!r.sigmoid) {
+  if (!r.sigmoid && !by_logit) {
     for (int i = 0; i < EPL; ++i) {
       const int e = held.id(i);
       if (held.has(i) && __builtin_isfinite(l[e])) top = max64(top, (double)l[e]);
@@ -433,7 +435,7 @@ __device__ __noinline__ int select_exact(const float* __restrict__ l, const floa
     c[i] = none;
     if (held.has(i) && __builtin_isfinite(l[e])) {
       const double x = (double)l[e];
-      c[i] = r.sigmoid ? sigmoid64(x) : exp(x - top) / total;
+      c[i] = by_logit ? x : r.sigmoid ? sigmoid64(x) : exp(x - top) / total;
       if (bias) c[i] += (double)bias[e];
       if (!__builtin_isfinite(c[i])) c[i] = none;
     }
@@ -454,7 +456,6 @@ __device__ __noinline__ int select_exact(const float* __restrict__ l, const floa
   for (int i = 0; i < EPL; ++i) {
     const int e = held.id(i);
     if (held.has(i) && ((kept >> (GM == kNoGroups ? 0 : e / r.per)) & 1)) avail |= 1u << i;
-    // without a bias experts are picked by their logits
     if (!bias && c[i] != none) c[i] = (double)l[e];
   }
   int mine = 0;
