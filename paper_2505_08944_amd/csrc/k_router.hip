@@ -272,8 +272,13 @@ struct Two {
     if (share > 4) join<2>();
     if (share > 8) join<3>();
   }
+  // (f32: a sum past its range is its largest value, which is apart() from smaller
+  // ones and never from another such sum; an infinity would be a masked group's
+  // worth or, with an id in its bits, no number)
   __device__ __forceinline__ T worth(int group_top) const {
-    return group_top > 1 && b != -(T)__builtin_inff() ? a + b : a;
+    T sum = a + b;
+    if constexpr (sizeof(T) == 4) sum = fminf(fmaxf(sum, -FLT_MAX), FLT_MAX);
+    return group_top > 1 && b != -(T)__builtin_inff() ? sum : a;
   }
 };
 
