@@ -16,7 +16,7 @@ import numpy as np
 import torch
 
 from . import _lib as L
-from .ops import Router
+from .ops import Router, arg32
 
 _ACT = {"f32": (L.AEP_F32, torch.float32), "bf16": (L.AEP_BF16, torch.bfloat16)}
 _WDT = {"f32": L.AEP_F32, "bf16": L.AEP_BF16, "fp8": L.AEP_FP8_E4M3}
@@ -163,6 +163,7 @@ class Context:
             _need(bias, "bias", torch.float32, (self.n_experts,))
             if bias.device != self.device:
                 raise ValueError(f"bias must be on {self.device}")
+        layer = arg32(layer, "layer", "aep_set_router")
         L.check(self.lib.aep_set_router(self.h, layer, None if router is None else ctypes.byref(router.desc),
                                         _ptr(bias)), "aep_set_router")
         self._bias_refs[layer] = bias

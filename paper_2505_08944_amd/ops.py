@@ -11,6 +11,7 @@ not take part in autograd.
 from __future__ import annotations
 
 import ctypes
+import operator
 from typing import Optional, Tuple
 
 import torch
@@ -50,6 +51,14 @@ def _int32(n: int, most: int, what: str, call: str) -> None:
     # (ctypes cuts larger values off)
     if n > most:
         raise L.AEPError(L.AEP_ERR_UNSUPPORTED, f"{call}: {n} {what}")
+
+
+def arg32(n, what: str, call: str) -> int:
+    """n, a whole number that an int32 argument holds."""
+    n = operator.index(n)
+    if not -(1 << 31) <= n < 1 << 31:
+        raise L.AEPError(L.AEP_ERR_INVALID_ARG, f"{call}: {what} {n}")
+    return n
 
 
 class _Fixed:
@@ -174,6 +183,10 @@ class Router(_Fixed):
                  group_top: int = 1, renorm: bool = True, scale: float = 1.0):
         if score not in _SCORE:
             raise ValueError(f"score {score!r}, expected one of {', '.join(_SCORE)}")
+        n_experts, top_k, n_groups, top_groups, group_top = (
+            arg32(n, what, "aep_route_topk") for n, what in
+            ((n_experts, "n_experts"), (top_k, "top_k"), (n_groups, "n_groups"), (top_groups, "top_groups"),
+             (group_top, "group_top")))
         self.n_experts, self.top_k, self.score = n_experts, top_k, score
         self.n_groups, self.top_groups, self.group_top = n_groups, top_groups, group_top
         self.renorm, self.scale = bool(renorm), float(scale)
