@@ -477,8 +477,14 @@ typedef struct {
 } aep_linear_desc;
 
 /* Bytes of device scratch with which aep_linear is fastest for this product
- * (host only; 0 for many). */
+ * (host only; 0 for many), its matrices all starting at 16-byte aligned
+ * addresses, with a residual or without. */
 aep_status aep_linear_workspace(const aep_linear_desc* l, size_t* bytes);
+/* The same for the call with these addresses (device pointers, of which only
+ * the alignment counts; residual NULL: none): x or W that starts elsewhere may
+ * need room for its copy. */
+aep_status aep_linear_workspace_at(const aep_linear_desc* l, const void* x, const void* w, const void* residual,
+                                   const void* y, size_t* bytes);
 
 /* Run it.  Device pointers: x, w, y as described, aligned to their elements
  * (rows of 16-byte aligned x and w, as rows of a multiple of 8 elements, 16
@@ -487,8 +493,8 @@ aep_status aep_linear_workspace(const aep_linear_desc* l, size_t* bytes);
  * FP8 weights and NULL for others; bias [n] or NULL; residual or NULL.  y may
  * be the residual itself (same type and row stride); apart from that it must
  * not overlap any input.  d_ws: 16-byte aligned scratch of ws_bytes, or NULL:
- * the product then runs without it where less than aep_linear_workspace is
- * given.  Nothing in d_ws is kept from call to call, and calls that may
+ * the product then runs without it where less than aep_linear_workspace_at
+ * says is given.  Nothing in d_ws is kept from call to call, and calls that may
  * overlap on the GPU need one each.  Needs no context; runs on the current HIP
  * device, which the pointers and the stream belong to.  Results do not depend
  * on other calls, and equal calls (sizes, strides, alignments and scratch given)

@@ -113,6 +113,7 @@ _SIG = {
     "aep_route_topk": (ctypes.c_int, [_P, _P, _I64, _P, _I32, _P, _P, _P, _P]),
     "aep_set_router": (ctypes.c_int, [_P, _I32, _P, _P]),
     "aep_linear_workspace": (ctypes.c_int, [_P, _P]),
+    "aep_linear_workspace_at": (ctypes.c_int, [_P, _P, _P, _P, _P, _P]),
     "aep_linear": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "aep_sched_pick": (ctypes.c_int, [_P, _I32, _I32, _I32, ctypes.c_double, _I32, ctypes.POINTER(_I32),
                                       ctypes.POINTER(_I32)]),

@@ -118,6 +118,14 @@ LinearArgs linear_args(const aep_linear_desc& l, const void* x, const void* w, c
   return p;
 }
 
+// Bytes of scratch of the cut that is taken where there is enough.
+size_t linear_scratch(const aep_linear_desc& l, const void* x, const void* w, const void* residual, const void* y) {
+  if (l.m == 0) return 0;
+  const LinearArgs p = linear_args(l, x, w, nullptr, nullptr, residual, const_cast<void*>(y));
+  const TilesPlan t = linear_tiles_plan(p, persistent_workgroups(), INT64_MAX);
+  return t.use ? (size_t)t.bytes(p.n) : 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -140,15 +148,20 @@ aep_status aep_linear_workspace(const aep_linear_desc* l, size_t* bytes) {
   const aep_status st = check_linear(l);
   if (st != AEP_OK) return st;
   if (!bytes) return AEP_ERR_INVALID_ARG;
-  *bytes = 0;
-  if (l->m == 0) return AEP_OK;
-  // as for aligned pointers, with a residual or without
   const void* const some = reinterpret_cast<const void*>(16);
-  for (const void* residual : {(const void*)nullptr, some}) {
-    const LinearArgs p = linear_args(*l, some, some, some, some, residual, nullptr);
-    if (const TilesPlan t = linear_tiles_plan(p, persistent_workgroups(), INT64_MAX); t.use)
-      *bytes = std::max(*bytes, (size_t)t.bytes(p.n));
-  }
+  *bytes = std::max(linear_scratch(*l, some, some, nullptr, some), linear_scratch(*l, some, some, some, some));
+  return AEP_OK;
+}
+
+aep_status aep_linear_workspace_at(const aep_linear_desc* l, const void* x, const void* w, const void* residual,
+                                   const void* y, size_t* bytes) {
+  const aep_status st = check_linear(l);
+  if (st != AEP_OK) return st;
+  if (!bytes) return AEP_ERR_INVALID_ARG;
+  if (off(x, esize(l->x_dtype)) || off(w, esize(l->w_dtype)) || off(residual, esize(l->res_dtype)) ||
+      off(y, esize(l->y_dtype)))
+    return AEP_ERR_INVALID_ARG;
+  *bytes = linear_scratch(*l, x, w, residual, y);
   return AEP_OK;
 }
 

@@ -123,11 +123,14 @@ class Linear(_Fixed):
         if dev.index != L.current_device():
             with torch.cuda.device(dev):
                 return self(x, residual, out)
-        # a call like one before, in all that is checked, needs no checks
+        # a call like one before, in all that is checked and in its alignment, which the
+        # scratch goes by, needs no checks
         try:
-            key = (x.shape, x.stride(), x.dtype, x.device,
-                   residual is None or (residual.shape, residual.stride(), residual.dtype, residual.device),
-                   out is None or (out.shape, out.stride(), out.dtype, out.device))
+            at, w_at = x.data_ptr(), self.weight.data_ptr()
+            key = (x.shape, x.stride(), x.dtype, x.device, (at & 15) << 4 | w_at & 15,
+                   residual is None or (residual.shape, residual.stride(), residual.dtype, residual.device,
+                                        residual.data_ptr() & 15),
+                   out is None or (out.shape, out.stride(), out.dtype, out.device, out.data_ptr() & 15))
         except AttributeError:
             raise ValueError("x, residual and out must be tensors") from None
         desc, need, shape = self._calls.get(key) or self._describe(key, x, residual, out)
@@ -135,7 +138,7 @@ class Linear(_Fixed):
             out = torch.empty(shape, dtype=self.out_dtype, device=dev)
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None  # held until the launch is in the stream
         scale, bias = self.scale, self.bias
-        st = self._lib.aep_linear(desc, x.data_ptr(), self.weight.data_ptr(), None if scale is None else scale.data_ptr(),
+        st = self._lib.aep_linear(desc, at, w_at, None if scale is None else scale.data_ptr(),
                                   None if bias is None else bias.data_ptr(),
                                   None if residual is None else residual.data_ptr(), out.data_ptr(),
                                   None if ws is None else ws.data_ptr(), need, L.raw_stream(dev.index))
@@ -158,7 +161,11 @@ class Linear(_Fixed):
                          y_dtype if residual is None else _CODE[residual.dtype], self._fn, _ld(x), self._ldw,
                          n if out is None else _ld(out), n if residual is None else _ld(residual))
         b = ctypes.c_size_t()
-        L.check(self._lib.aep_linear_workspace(ctypes.byref(d), ctypes.byref(b)), "aep_linear_workspace")
+        # (an output that torch allocates is aligned)
+        L.check(self._lib.aep_linear_workspace_at(ctypes.byref(d), x.data_ptr(), self.weight.data_ptr(),
+                                                  None if residual is None else residual.data_ptr(),
+                                                  16 if out is None else out.data_ptr(), ctypes.byref(b)),
+                "aep_linear_workspace_at")
         if len(self._calls) >= 1024:
             self._calls.clear()
         call = self._calls[key] = (ctypes.byref(d), b.value, (m, n))
