@@ -459,8 +459,10 @@ aep_status aep_set_clock_probe(aep_ctx* ctx, uint64_t* d_buf, int32_t n_pairs);
  * residual, the projection that closes an attention block.
  * Activations: RELU max(v, 0); SILU v / (1 + e^-v); GELU v (1 + erf(v /
  * sqrt 2)) / 2; GELU_TANH v / (1 + e^-2u), u = sqrt(2 / pi) (v + 0.044715 v^3),
- * which is its usual form with tanh(u).  Beside the roundings of the sum they are
- * off by at most 2^-19 of their value, and GELU by 2^-23 |v| more. */
+ * which is its usual form with tanh(u).  Beside the roundings of the sum, f32
+ * results are off by at most 2^-20 of the activation's value and 2^-142; bf16
+ * results, before their rounding, by 2^-15 of it, GELU by 2^-23 |v| more, and may
+ * lose values below 2^-119. */
 typedef enum {
   AEP_FN_NONE = 0, AEP_FN_RELU = 1, AEP_FN_SILU = 2, AEP_FN_GELU = 3, AEP_FN_GELU_TANH = 4
 } aep_fn;

@@ -337,7 +337,8 @@ __device__ __forceinline__ void finish_wide(const LinearItem& it, int wm, int wn
 
 // The same for f32 results of a multiple of 4 columns, which go out as a lane
 // holds them.  The residual may be f32, or bf16 of dword-aligned rows.  (4096 x
-// 4096 x 1024 with bias, SiLU and f32 residual 48 us, 26 of them its bytes; by
+// 4096 x 1024 with bias, SiLU and f32 residual 56 us, 26 of them its bytes and 5 the
+// activation to f32's accuracy; with the short form of bf16 results 51, and that by
 // finish_any 61.)
 template <bool FP8, int FAM, int NB>
 __device__ __forceinline__ void finish_f32(const LinearItem& it, int wm, int wn, int rr, int hh,
@@ -393,7 +394,7 @@ __device__ __forceinline__ void finish_f32(const LinearItem& it, int wm, int wn,
           f32x4_t v = acc[u][b][i][j];
           if constexpr (FP8) v *= s4[j];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = linear_fn_tile<fn()>(v[e] + b4[j][e]);
+          for (int e = 0; e < 4; ++e) v[e] = linear_fn<fn()>(v[e] + b4[j][e]);
           if (p.res) {
             const u32x4_t t = res[i][j];
             v += rs == 4u ? __builtin_bit_cast(f32x4_t, t) : f32x4_t{bf16_lo(t[0]), bf16_hi(t[0]), bf16_lo(t[1]), bf16_hi(t[1])};
@@ -406,8 +407,8 @@ __device__ __forceinline__ void finish_f32(const LinearItem& it, int wm, int wn,
 }
 
 // The same for any other result: rows of any alignment and length, by unaligned
-// accesses of four values.  (bf16 rows of 4097 elements, otherwise as above: 62 us;
-// value by value 79; wide rows 39.)
+// accesses of four values.  (bf16 rows of 4097 elements, otherwise as above: 66 us,
+// wide rows 41; value by value a quarter longer.)
 template <bool FP8, int FAM, int NB>
 __device__ __forceinline__ void finish_any(const LinearItem& it, int wm, int wn, int rr, int hh,
                                            f32x4_t (&acc)[Shape<FP8, FAM, NB>::kUnits][Shape<FP8, FAM, NB>::NP][Shape<FP8, FAM, NB>::RF][2]) {
@@ -476,12 +477,21 @@ __device__ __forceinline__ void finish_any(const LinearItem& it, int wm, int wn,
       }
     }
     by_fn(p.fn, [&](auto fn) {
+      if (p.y_dtype == kF32) {
 #pragma unroll
-      for (int i = 0; i < RH; ++i)
+        for (int i = 0; i < RH; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[i][j][e] = linear_fn_tile<fn()>(v[i][j][e] + b4[j][e]) + res[i][j][e];
+            for (int e = 0; e < 4; ++e) v[i][j][e] = linear_fn<fn()>(v[i][j][e] + b4[j][e]) + res[i][j][e];
+      } else {
+#pragma unroll
+        for (int i = 0; i < RH; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i][j][e] = linear_fn_tile<fn()>(v[i][j][e] + b4[j][e]) + res[i][j][e];
+      }
     });
     auto store = [&](auto dtype, auto all) {
 #pragma unroll

@@ -69,29 +69,76 @@ __device__ __forceinline__ void store4(void* p, int dtype, int64_t at, int n, co
   }
 }
 
-// v / (1 + e^-u) for f32 results: to within a few units of 2^-24.
-__device__ __forceinline__ float gate(float v, float u) { return v / (1.f + expf(-u)); }
+// e^-(a + lost) as m 2^n with m in [2^-1/2, 2^1/2], for a from 0 to 1000 and a lost that is
+// small beside it: m is off by 2^-23 of its value, as the exponent's whole part leaves
+// exactly (rounded as one f32, the exponent would put e^-80 off by 2^-17).
+__device__ __forceinline__ float exp_parts(float a, float lost, int& n) {
+#pragma clang fp contract(off)
+  constexpr double kLog2E = 1.4426950408889634;
+  constexpr float L = (float)kLog2E, L_lost = (float)(kLog2E - (double)L);
+  const float whole = __builtin_rintf(a * L);
+  n = -(int)whole;
+  float f = __builtin_fmaf(a, L, -whole);
+  f = __builtin_fmaf(a, L_lost, f);
+  return __builtin_amdgcn_exp2f(-__builtin_fmaf(lost, L, f));
+}
+// v / (1 + e^-u) for u = +-(a + lost) of v's sign: as v e^u / (1 + e^u) below 0, so that
+// nothing overflows.
+__device__ __forceinline__ float gate(float v, float a, float lost) {
+#pragma clang fp contract(off)
+  int n;
+  const float m = exp_parts(a, lost, n), e = __builtin_ldexpf(m, n);
+  return v * (v < 0.f ? e : 1.f) * __builtin_amdgcn_rcpf(1.f + e);
+}
 
-// The activation, accurate enough for an f32 result.  GELU through erfc, which
-// keeps its relative accuracy where 1 + erf cancels; GELU_TANH as v / (1 +
-// e^-2u), which does the same.
+// The activation for f32 results, and wherever there are few values: off by at most
+// 2^-21 of its value (exponential and reciprocal 2^-23, 1 + e^u and the products 2^-24
+// each), GELU by 2^-20, and by 2^-142, as e^u has steps of 2^-149 at least.  Products are
+// not fused with what is added to them, here or to the result, so that equal values
+// have equal results wherever they lie.  GELU is v Phi(v) with Phi(-a) = e^(-a^2 / 2) R(a)
+// / 2, R(a) = erfcx(a / sqrt 2) a polynomial in 1 / (1 + 0.27 a) fitted to 2^-25 of
+// its value for a up to 20 (in f32: 2^-21.3).  Arguments are cut off where the
+// result is 0 or v.
+template <int FN>
+__device__ __forceinline__ float linear_fn(float v) {
+#pragma clang fp contract(off)
+  if constexpr (FN == kFnNone) return v;
+  if constexpr (FN == kFnRelu) return v > 0.f ? v : v == v ? 0.f : v;  // NaN stays NaN
+  if constexpr (FN == kFnSilu) return gate(v, fminf(fabsf(v), 360.f), 0.f);
+  if constexpr (FN == kFnGeluTanh) {  // 1 + tanh u = 2 / (1 + e^-2u)
+    const double a = fminf(fabsf(v), 20.f), u = 2.0 * 0.79788456080286536 * a * (1.0 + 0.044715 * a * a);
+    const float hi = (float)u;
+    return gate(v, hi, (float)(u - (double)hi));
+  }
+  constexpr float c[] = {0.215443328f, 0.215052918f, 0.203844741f, 0.143263772f, 0.217531502f, -0.141038328f, 0.341777891f,
+                         -0.254003763f, 0.0581279807f};
+  const float a = fminf(fabsf(v), 40.f), s = 0.5f * a * a;
+  int n;
+  const float m = exp_parts(s, __builtin_fmaf(0.5f * a, a, -s), n);
+  const float z = __builtin_amdgcn_rcpf(1.f + 0.27f * a);
+  float r = c[8];
+#pragma unroll
+  for (int i = 7; i >= 0; --i) r = __builtin_fmaf(r, z, c[i]);
+  const float half = 0.5f * (r * z) * m;  // Phi(-|v|) = half 2^n
+  const float tail = __builtin_ldexpf(half, n);
+  return v * (v > 0.f ? 1.f - tail : tail);
+}
 __device__ __forceinline__ float linear_fn(int fn, float v) {
   switch (fn) {
-    case kFnRelu: return v > 0.f ? v : v == v ? 0.f : v;  // NaN stays NaN
-    case kFnSilu: return gate(v, v);
-    case kFnGelu: return 0.5f * v * erfcf(v * -0.70710678118654752f);
-    case kFnGeluTanh: return gate(v, 2.f * 0.79788456080286536f * (v + 0.044715f * v * v * v));
+    case kFnRelu: return linear_fn<kFnRelu>(v);
+    case kFnSilu: return linear_fn<kFnSilu>(v);
+    case kFnGelu: return linear_fn<kFnGelu>(v);
+    case kFnGeluTanh: return linear_fn<kFnGeluTanh>(v);
     default: return v;
   }
 }
 
-// The activation for whole tiles, short enough to be laid out for every value of
+// The activation for bf16 results of whole tiles, short enough to be laid out for every value of
 // one: SILU and GELU_TANH as v / (1 + e^-u), with the hardware's exponential and
-// reciprocal (2^-20 at |u| < 20; beyond, one of 1 and e^-u is lost); GELU with erf
-// from Abramowitz and Stegun 7.1.26, whose error is at most 1.5e-7, here half of
-// it times |v|.  Made for bf16 results (half a step: 2^-9 .. 2^-8 of them); an f32
-// result keeps that relative error of 2^-20 (GELU: that absolute one, below what
-// the sum's own roundings leave of v's size).
+// reciprocal and u in f32: off by |u| 2^-22 of its value and a few steps of 2^-23 (below
+// 2^-15 where the result is not lost: below u = -87 it is, of a size of 2^-119), where
+// bf16's half step is 2^-9 .. 2^-8.  GELU with erf from Abramowitz and Stegun 7.1.26,
+// whose error is at most 1.5e-7, here half of it times |v|.
 template <int FN>
 __device__ __forceinline__ float linear_fn_tile(float v) {
   if constexpr (FN == kFnNone) return v;
