@@ -78,7 +78,7 @@ class Linear(_Fixed):
     bias [n] float32 or bfloat16.  activation: none, relu, silu, gelu or
     gelu_tanh.  out_dtype: x's type (the default) or float32.  The tensors are
     kept, not copied: values written to them later are used by later calls;
-    their shapes, strides and types stay as they are.
+    with another shape, stride, type or device than they had they are refused.
     """
 
     def __init__(self, weight: torch.Tensor, *, scale: Optional[torch.Tensor] = None,
@@ -113,6 +113,7 @@ class Linear(_Fixed):
                        L.AEP_F32 if bias is None else _CODE[bias.dtype])
         self._fn = _FN[activation]
         self._ldw = _ld(weight)
+        self._kept = tuple((t, t.shape, t.stride(), t.dtype) for t in (weight, scale, bias) if t is not None)
         self._calls = {}  # by what is checked of the tensors: what _describe makes of such a call
 
     def __call__(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None,
@@ -123,6 +124,11 @@ class Linear(_Fixed):
         if dev.index != L.current_device():
             with torch.cuda.device(dev):
                 return self(x, residual, out)
+        # (a module's conversions set the data of its parameters; 0.3 .. 0.4 us per tensor, of some 6)
+        for t, shape, stride, dtype in self._kept:
+            if t.dtype is not dtype or t.stride() != stride or t.shape != shape or t.get_device() != dev.index:
+                raise ValueError("the weight, its scale or the bias has another shape, stride, type or device than it "
+                                 "had: make a new Linear")
         # a call like one before, in all that is checked and in its alignment, which the
         # scratch goes by, needs no checks
         try:
