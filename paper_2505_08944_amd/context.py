@@ -157,8 +157,9 @@ class Context:
     # ------------------------------------------------------------- receptor
     def set_router(self, layer: int, router: Optional[Router], bias: Optional[torch.Tensor] = None) -> None:
         """Route this layer's fragments by ``router`` (an ``aep.Router``), its
-        choices with bias [E] float32 (kept, not copied); None: by the
-        context's own rule again."""
+        choices with bias [E] float32 (its memory is kept, not copied: values
+        written there are used by later calls); None: by the context's own rule
+        again."""
         if bias is not None:
             _need(bias, "bias", torch.float32, (self.n_experts,))
             if bias.device != self.device:
@@ -166,7 +167,8 @@ class Context:
         layer = arg32(layer, "layer", "aep_set_router")
         L.check(self.lib.aep_set_router(self.h, layer, None if router is None else ctypes.byref(router.desc),
                                         _ptr(bias)), "aep_set_router")
-        self._bias_refs[layer] = bias
+        # (a tensor of its own: the given one may be set to other memory)
+        self._bias_refs[layer] = None if bias is None else bias.detach()
 
     def route_enqueue(self, layer: int, x: torch.Tensor, logits: torch.Tensor,
                       routing_out: bool = False) -> Optional[Tuple[torch.Tensor, torch.Tensor]]:
