@@ -112,7 +112,14 @@ __global__ __launch_bounds__(WAVES * 64) void linear_rows_kernel(const LinearArg
   auto piece = [&](const unsigned char* frag, int q) {
     return *reinterpret_cast<const uint4*>(frag + (q >> 2) * 1024 + (rr * 4 + ((q & 3) ^ (rr >> 2))) * 16);
   };
+  // One wave's LDS accesses are carried out in the order in which they were issued: the
+  // compiler only has to keep it, across lanes that it does not know to share values.
+  auto wave_order = [&] {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
   auto mma = [&](int b) {
+    wave_order();
     unsigned char* at = mine;
 #pragma unroll
     for (int j = 0; j < CF; ++j)
@@ -122,6 +129,7 @@ __global__ __launch_bounds__(WAVES * 64) void linear_rows_kernel(const LinearArg
     for (int i = 0; i < RF; ++i)
 #pragma unroll
       for (int q = 0; q < XQ; ++q, at += 1024) *reinterpret_cast<uint4*>(at + lane * 16) = xa[b][i][q];
+    wave_order();
     const unsigned char* xs = mine + CF * WQ * 1024;
     uint4 x[RF][2], w[CF][2];
 #pragma unroll
