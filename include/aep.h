@@ -471,8 +471,8 @@ typedef struct {
   int32_t x_dtype;       /* aep_dtype: F32 or BF16                                 */
   int32_t w_dtype;       /* F32 (with F32 x), BF16 or FP8_E4M3 (with BF16 x)       */
   int32_t y_dtype;       /* F32, or BF16 (with BF16 x)                             */
-  int32_t bias_dtype;    /* F32 or BF16 (ignored without a bias)                   */
-  int32_t res_dtype;     /* F32 or BF16 (ignored without a residual)               */
+  int32_t bias_dtype;    /* F32 or BF16, also where there is no bias               */
+  int32_t res_dtype;     /* F32 or BF16, also where there is no residual           */
   int32_t fn;            /* aep_fn                                                 */
   int64_t ldx, ldw;      /* elements from one row to the next, >= k                */
   int64_t ldy, ldr;      /* >= n (ldr ignored without a residual)                  */
