@@ -4,10 +4,11 @@
 // workgroup split K and add their sums in LDS, in wave order.  It is for
 // products that one operand's stream bounds (few rows, or few channels) and for
 // f32; the tile kernel (k_linear_tiles.hip) takes the others (linear_cut.hip), rows
-// of other alignments than 16 bytes through aligned copies.  Measured, us, with the operands in the Infinity Cache
-// and (in brackets) in HBM: 32 x 4096 x 4096 7.9 (11.9; its bytes at the rate of
-// a large copy 6.6), 1 x 14336 x 4096 fp8 11.5 (15.1; 11.3), 8192 x 64 x 2048 8.9
-// (9.1; 6.9), an empty launch 1.5.
+// of other alignments than 16 bytes through aligned copies.  Measured, us per call
+// of a captured run of them, with the operands in the Infinity Cache and (in brackets)
+// in HBM: 32 x 4096 x 4096 8.3 (11.3; its bytes at the rate of a large copy 6.6), 1 x
+// 14336 x 4096 fp8 12.5 (16.7; 11.3), 8192 x 64 x 2048 9.0 (12.4; 6.9), an empty
+// launch 1.5.
 #include <algorithm>
 
 #include "linear_epilogue.h"
