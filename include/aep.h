@@ -504,6 +504,134 @@ aep_status aep_linear_workspace_at(const aep_linear_desc* l, const void* x, cons
 aep_status aep_linear(const aep_linear_desc* l, const void* x, const void* w, const void* scale, const void* bias,
                       const void* residual, void* y, void* d_ws, size_t ws_bytes, void* stream);
 
+/* ---- Values in 4 bits ----
+ * OCP MXFP4: blocks of 32 consecutive values of a row share a power of two,
+ * held as a byte (2^(byte - 127); 255: NaN); a value is a code of 4 bits, sign
+ * and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 .. 7; + 8: negative).  Two
+ * codes to a byte, the earlier value in its low half.  Every value is a bf16
+ * value.  Quantising: a block's power is the smallest, from 2^-126 to 2^125, at
+ * which its largest magnitude is at most 7 times it (2^0 for zeros); a value goes
+ * to the nearest code, in the middle to the even one, above 6 to 6.  A block with
+ * a NaN or an infinity gets the byte 255: all of it reads back as NaN.
+ *
+ * All calls below need no context and run on the current HIP device, which
+ * pointers and stream belong to. */
+
+/* x [rows][k] F32 or BF16, row r at x + r * ldx elements (ldx >= k), to codes
+ * [rows][(k + 1) / 2] and scale [rows][(k + 31) / 32] (device, bytes; contiguous;
+ * of an odd k the last half byte is 0).  rows == 0 is a no-op. */
+aep_status aep_mx4_quantize(const void* x, int32_t x_dtype, int64_t ldx, int64_t rows, int32_t k, void* codes,
+                            void* scale, void* stream);
+/* And back, exactly, to y [rows][k] F32 or BF16 of row stride ldy. */
+aep_status aep_mx4_dequantize(const void* codes, const void* scale, int64_t rows, int32_t k, void* y, int32_t y_dtype,
+                              int64_t ldy, void* stream);
+
+/* Dense product with 4-bit weights: y = f(x W^T + b) + r as aep_linear, x BF16,
+ * W [n][k] in 4 bits.  The codes go to the matrix cores as the bf16 values that
+ * they are; sums and the epilogue are f32, y is rounded once. */
+typedef struct {
+  int32_t m, n, k;       /* m >= 0; n, k >= 1; none above 2^30, m n at most 2^38, n k 2^40 */
+  int32_t y_dtype;       /* F32 or BF16                                            */
+  int32_t bias_dtype;    /* F32 or BF16, also where there is no bias               */
+  int32_t res_dtype;     /* F32 or BF16, also where there is no residual           */
+  int32_t fn;            /* aep_fn                                                 */
+  int64_t ldx;           /* elements from one row to the next, >= k                */
+  int64_t ldy, ldr;      /* >= n (ldr ignored without a residual)                  */
+} aep_linear4_desc;
+
+/* The weights are laid out once for the product: codes and scale as
+ * aep_mx4_quantize writes them, to packed (device, 16-byte aligned, so many
+ * bytes), which is all that aep_linear4 reads of them. */
+aep_status aep_linear4_packed_bytes(int32_t n, int32_t k, size_t* bytes);
+aep_status aep_linear4_pack(const void* codes, const void* scale, int32_t n, int32_t k, void* packed, void* stream);
+
+/* Bytes of device scratch with which aep_linear4 is fastest for this product
+ * and these addresses (of which only the alignment counts; residual NULL: none);
+ * for many rows the weights widened to bf16 are the most of it. */
+aep_status aep_linear4_workspace(const aep_linear4_desc* l, const void* x, const void* residual, const void* y,
+                                 size_t* bytes);
+/* Run it: pointers, scratch (less, or none, runs a slower way), overlap and
+ * reproducibility as for aep_linear. */
+aep_status aep_linear4(const aep_linear4_desc* l, const void* x, const void* packed, const void* bias,
+                       const void* residual, void* y, void* d_ws, size_t ws_bytes, void* stream);
+
+/* ---- A paged cache of keys and values in 4 bits, and the attention over it ----
+ * One allocation (device, 16-byte aligned, aep_cache4_bytes) holds n_pages pages
+ * of page_size tokens: keys and values of n_heads heads of head_dim values, in
+ * blocks of 32 along head_dim.  Its inner order is the library's own; a copy of
+ * the whole allocation is a copy of the cache. */
+typedef struct {
+  int32_t n_pages;       /* >= 1                                                   */
+  int32_t page_size;     /* tokens: a power of two, 32 .. 4096                     */
+  int32_t n_heads;       /* heads of keys and values, 1 .. 1024                    */
+  int32_t head_dim;      /* 64, 128 or 256                                         */
+} aep_cache4;
+
+/* The sequences of a call.  A call has `total` rows (of keys and values, or of
+ * queries); sequence b has the rows rows[b] .. rows[b + 1] - 1, or, where rows is
+ * NULL, total / batch rows each (total a multiple of batch).  Its rows are its
+ * newest tokens: row i of n is token lens[b] - n + i, lens[b] being all tokens
+ * of the sequence with these.  A row whose token would lie before the first
+ * (more rows than tokens) has none.  Token t lies in page pages[b][t / page_size].
+ * Rows that belong to no sequence are neither read nor written.  pages, lens,
+ * rows and flag are device pointers to int32.  What only the device sees is held
+ * to what there is, so that accesses stay in bounds, and sets *flag to 1 (flag may
+ * be NULL; it is never cleared): rows that descend or lie outside 0 .. total, and
+ * of what the call's rows need, a page outside the cache, or a length below 0 or
+ * beyond max_pages.  What such a sequence's rows get is not defined. */
+typedef struct {
+  const int32_t* pages;  /* [batch][max_pages], rows ld_pages apart                */
+  const int32_t* lens;   /* [batch]                                                */
+  const int32_t* rows;   /* [batch + 1], ascending, or NULL                        */
+  int32_t* flag;         /* [1] or NULL                                            */
+  int64_t ld_pages;      /* >= max_pages                                           */
+  int32_t max_pages;     /* max_pages page_size at most 2^30                       */
+  int32_t batch;         /* at most 2^24                                           */
+  int32_t total;         /* at most 2^30                                           */
+} aep_cache4_seqs;
+
+aep_status aep_cache4_bytes(const aep_cache4* c, size_t* bytes);
+
+/* Quantise rows of keys and values (BF16; head h of row t at k + t * k_row + h *
+ * k_head elements, its values contiguous) into their tokens' places.  Places of
+ * one token are nobody else's, so calls that write different tokens may overlap;
+ * the same token twice in one call is kept as either of the two, or parts of both.
+ * total == 0 is a no-op. */
+aep_status aep_cache4_append(const aep_cache4* c, void* mem, const aep_cache4_seqs* s, const void* k, int64_t k_row,
+                             int64_t k_head, const void* v, int64_t v_row, int64_t v_head, void* stream);
+
+/* Read rows back, exactly: k and v [total][n_heads][head_dim] BF16, 16-byte
+ * aligned; zeros for a row without a token. */
+aep_status aep_cache4_read(const aep_cache4* c, const void* mem, const aep_cache4_seqs* s, void* k, void* v, void* stream);
+
+/* Attention: for each row and head of queries
+ *   out = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q . k_t),
+ * over the tokens t of its sequence up to the row's own and, with a window, of
+ * these the last `window`.  Head j reads head j / (n_heads / the cache's
+ * n_heads) of the cache.  lse = log sum_t exp(scale q . k_t).  A row without a
+ * token has out = 0 and lse = -infinity.  Tokens that a row does not see do not
+ * count for it, whatever their places hold.  Sums are f32; the p_t of a sum are
+ * rounded to bf16 relative to one reference each, the same in both sums. */
+typedef struct {
+  int32_t n_heads;          /* of queries: a multiple of the cache's                */
+  int32_t window;           /* 0: none                                              */
+  float scale;              /* finite, > 0                                          */
+  int64_t q_row, q_head;    /* elements from one row, or head, to the next, >= 0    */
+  int64_t out_row, out_head; /* the same of out, whose heads must not overlap       */
+} aep_attend4_desc;
+
+/* Bytes of device scratch of a call (host only). */
+aep_status aep_cache4_attend_workspace(const aep_cache4* c, const aep_cache4_seqs* s, const aep_attend4_desc* a,
+                                       size_t* bytes);
+/* q and out BF16, lse [total][n_heads] f32 or NULL (rows of no sequence stay as
+ * they were).  d_ws: 16-byte aligned scratch (AEP_ERR_CAPACITY if less than
+ * aep_cache4_attend_workspace says); nothing in it is kept from call to call, and
+ * calls that may overlap on the GPU need one each.  out must not overlap q.  Equal
+ * calls give equal bits.  AEP_ERR_UNSUPPORTED for more work than 31 bits count:
+ * (total n_heads / 16 + batch) (max_pages page_size / 128), about. */
+aep_status aep_cache4_attend(const aep_cache4* c, const void* mem, const aep_cache4_seqs* s, const aep_attend4_desc* a,
+                             const void* q, void* out, float* lse, void* d_ws, size_t ws_bytes, void* stream);
+
 /* Utility: decode n OCP e4m3fn codes (device) to bf16 (device); exact. */
 aep_status aep_fp8_e4m3_to_bf16(const uint8_t* codes, uint16_t* out, int64_t n, void* stream);
 

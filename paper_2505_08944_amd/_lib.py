@@ -59,6 +59,25 @@ class LinearDesc(ctypes.Structure):
                [(n, ctypes.c_int64) for n in ("ldx", "ldw", "ldy", "ldr")]
 
 
+class Linear4Desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("m", "n", "k", "y_dtype", "bias_dtype", "res_dtype", "fn")] + \
+               [(n, ctypes.c_int64) for n in ("ldx", "ldy", "ldr")]
+
+
+class Cache4Desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "n_heads", "head_dim")]
+
+
+class Cache4Seqs(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("pages", "lens", "rows", "flag")] + [("ld_pages", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("max_pages", "batch", "total")]
+
+
+class Attend4Desc(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("q_row", "q_head", "out_row", "out_head")]
+
+
 class SimConfig(ctypes.Structure):
     _fields_ = [("n_blocks", ctypes.c_int32), ("n_experts", ctypes.c_int32), ("top_k", ctypes.c_int32),
                 ("n_frag", ctypes.c_int32), ("granularity", ctypes.c_int32), ("policy", ctypes.c_int32),
@@ -115,6 +134,17 @@ _SIG = {
     "aep_linear_workspace": (ctypes.c_int, [_P, _P]),
     "aep_linear_workspace_at": (ctypes.c_int, [_P, _P, _P, _P, _P, _P]),
     "aep_linear": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "aep_mx4_quantize": (ctypes.c_int, [_P, _I32, _I64, _I64, _I32, _P, _P, _P]),
+    "aep_mx4_dequantize": (ctypes.c_int, [_P, _P, _I64, _I32, _P, _I32, _I64, _P]),
+    "aep_linear4_packed_bytes": (ctypes.c_int, [_I32, _I32, _P]),
+    "aep_linear4_pack": (ctypes.c_int, [_P, _P, _I32, _I32, _P, _P]),
+    "aep_linear4_workspace": (ctypes.c_int, [_P, _P, _P, _P, _P]),
+    "aep_linear4": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
+    "aep_cache4_bytes": (ctypes.c_int, [_P, _P]),
+    "aep_cache4_append": (ctypes.c_int, [_P, _P, _P, _P, _I64, _I64, _P, _I64, _I64, _P]),
+    "aep_cache4_read": (ctypes.c_int, [_P, _P, _P, _P, _P, _P]),
+    "aep_cache4_attend_workspace": (ctypes.c_int, [_P, _P, _P, _P]),
+    "aep_cache4_attend": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, _P, _P, ctypes.c_size_t, _P]),
     "aep_sched_pick": (ctypes.c_int, [_P, _I32, _I32, _I32, ctypes.c_double, _I32, ctypes.POINTER(_I32),
                                       ctypes.POINTER(_I32)]),
     "aep_sim_run": (ctypes.c_int, [ctypes.POINTER(SimConfig), ctypes.POINTER(SimTrace),

@@ -1,0 +1,89 @@
+// The paged cache of keys and values in 4 bits (mx4.h): its layout, and what its
+// kernels share.
+//
+// A page holds P tokens (a power of two, 32 at least) of every head.  D values of a
+// head are D / 32 blocks.  In the order in which the attention's lanes take them:
+//   keys     [page][head][P / 16][block][16 tokens][16 bytes]: the codes in their order
+//   values   [page][head][P / 32][16 l][4 g][8 j][D / 32 bytes]: the D / 16 codes from
+//            D / 16 l on of token cache4_token(g, j) of the 32
+//   scales of keys    [page][head][P][block]
+//   scales of values  [page][head][P / 32][block][4 g][8 j]
+// one behind the other.  No byte belongs to two tokens.
+#pragma once
+
+#include "aep_internal.h"
+#include "mx4.h"
+
+namespace aep {
+
+struct Cache4 {
+  uint8_t *k, *v, *ks, *vs;
+  int n_pages, log_page, heads, d;
+};
+
+// Where sequences' rows and tokens are: row i of the n rows of sequence b is its
+// token len - n + i, which lies in page pages[b][token / P].  Sequence b has the rows
+// from rows[b] to rows[b + 1]; without rows, n rows each.
+struct Cache4Seqs {
+  const int32_t *pages, *lens, *rows;
+  int64_t ld_pages;
+  int max_pages, batch, total, n;
+  int32_t* flag;
+};
+
+// What the device reads is held to what the buffers have; what had to be is reported.
+struct SeqRows {
+  int row0, n, len;
+};
+__device__ __forceinline__ SeqRows seq_rows(const Cache4Seqs& q, int log_page, int b) {
+  SeqRows s;
+  if (q.rows) {
+    const int a = q.rows[b], e = q.rows[b + 1];
+    s.row0 = min(max(a, 0), q.total);
+    const int last = min(max(e, s.row0), q.total);
+    s.n = last - s.row0;
+    if (q.flag && (a != s.row0 || e != last)) *q.flag = 1;
+  } else {
+    s.row0 = b * q.n;
+    s.n = q.n;
+  }
+  const int l = q.lens[b];
+  s.len = (int)min((int64_t)max(l, 0), (int64_t)q.max_pages << log_page);
+  if (q.flag && l != s.len) *q.flag = 1;
+  return s;
+}
+__device__ __forceinline__ int seq_page(const Cache4Seqs& q, int n_pages, int b, int i) {
+  const int p = q.pages[b * q.ld_pages + i], in = min(max(p, 0), n_pages - 1);
+  if (q.flag && p != in) *q.flag = 1;
+  return in;
+}
+
+// Place (g, j) of token t of 32: the rows 4 g + i of an MFMA's result over tokens 0 ..
+// 15 are a lane's values j = i, those over 16 .. 31 its values j = 4 + i.
+__device__ __forceinline__ int cache4_place(int t) { return ((t & 15) >> 2) * 8 + (t & 3) + (t >> 4) * 4; }
+
+struct Attend4Args {
+  Cache4 c;
+  Cache4Seqs s;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  int64_t q_row, q_head, o_row, o_head;
+  int group;    // heads of queries per head of the cache
+  int window;
+  float scale;  // times log2 e
+  float* parts;
+  int workers;
+};
+// The attention's launch: columns of 16 per workgroup, workgroups, bytes of scratch.
+struct Attend4Plan {
+  int nc, workers;
+  int64_t bytes;
+};
+Attend4Plan attend4_plan(int batch, int total, int heads, int group, int d, int64_t max_len, int ncu);
+hipError_t launch_attend4(const Attend4Args& a, int nc, hipStream_t s);
+hipError_t launch_cache4_append(const Cache4& c, const Cache4Seqs& q, const uint16_t* k, const uint16_t* v, int64_t k_row,
+                                int64_t k_head, int64_t v_row, int64_t v_head, hipStream_t s);
+hipError_t launch_cache4_read(const Cache4& c, const Cache4Seqs& q, uint16_t* k, uint16_t* v, hipStream_t s);
+
+}  // namespace aep

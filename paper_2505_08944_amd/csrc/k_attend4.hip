@@ -1,0 +1,503 @@
+// Attention over a paged cache of keys and values in 4 bits (cache4.h): for each row
+// of queries o = sum_t p_t v_t / sum_t p_t, p_t = e^(scale q k_t), over the tokens that
+// it sees, in one pass with a running reference for the exponents.
+//
+// A tile of 16 NC columns (a column is a row of queries and one of the heads that share
+// a head of the cache) takes 32 tokens at a time in a wave: scores as K q^T on MFMAs
+// (rows: tokens, columns: queries), which leaves a lane 8 tokens of its column, in the
+// order in which it holds them as an operand of V^T p^T.  Codes become exact bf16 in
+// registers; p is rounded to bf16 once, and its sum is that of the rounded values (an
+// MFMA with ones), so that weights sum to 1.
+//
+// Bound by the cache's bytes for few columns, by VALU (conversions, exponentials) for many.
+// The work is divided evenly: all units of 128 tokens of all tiles in a row, an equal share
+// for each workgroup; its four waves take 32 of each unit and are joined in LDS.
+// Tiles that several workgroups share leave parts in the scratch, which a second launch joins
+// in the order of the tokens.
+#include <algorithm>
+#include <cmath>
+
+#include "cache4.h"
+#include "linear_epilogue.h"
+
+namespace aep {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+namespace {
+
+constexpr int kUnit = 128;  // tokens
+constexpr float kNegInf = -INFINITY;
+// A column's reference follows its largest score (in powers of two) only when that is this
+// much ahead: most blocks then change nothing, and p stays below 2^8.
+constexpr float kAhead = 8.f;
+
+// A sequence's units: tiles of columns for each head, units of tokens for each tile.
+struct SeqUnits {
+  SeqRows s;
+  int first, nb, ct;  // first unit, units of a tile, tiles of a head
+  __device__ int units(int heads) const { return heads * ct * nb; }
+};
+template <int COLS>
+__device__ __forceinline__ SeqUnits seq_units(const Attend4Args& a, int b) {
+  SeqUnits u;
+  u.s = seq_rows(a.s, a.c.log_page, b);
+  u.first = 0;
+  if (a.window) u.first = max(0, u.s.len - u.s.n - a.window + 1) / kUnit;
+  u.nb = max(1, (u.s.len + kUnit - 1) / kUnit - u.first);
+  u.ct = (int)(((int64_t)u.s.n * a.group + COLS - 1) / COLS);
+  return u;
+}
+
+__device__ __forceinline__ int wave_sum(int v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// Where a workgroup is among the units.
+struct Place {
+  int total;     // units of all sequences
+  int u0, u1;    // this workgroup's
+  int b, before; // sequence of u0, units before that sequence
+};
+__device__ __forceinline__ int share_start(int total, int workers, int w) { return (int)((int64_t)total * w / workers); }
+
+template <int COLS>
+__device__ __forceinline__ Place find_place(const Attend4Args& a, int w) {
+  const int lane = threadIdx.x & 63;
+  Place p;
+  int mine = 0, first = 0;
+  for (int b = lane; b < a.s.batch; b += 64) {
+    const int n = seq_units<COLS>(a, b).units(a.c.heads);
+    if (b == lane) first = n;
+    mine += n;
+  }
+  p.total = __builtin_amdgcn_readfirstlane(wave_sum(mine));
+  p.u0 = share_start(p.total, a.workers, w);
+  p.u1 = share_start(p.total, a.workers, w + 1);
+  p.b = a.s.batch;  // (found below, unless what is read changes meanwhile)
+  p.before = 0;
+  for (int base = 0; base < a.s.batch; base += 64) {
+    int n = first;
+    if (base) n = base + lane < a.s.batch ? seq_units<COLS>(a, base + lane).units(a.c.heads) : 0;
+    int upto = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
+    }
+    const int at = __popcll(__ballot(p.before + upto <= p.u0));  // sequences that end before u0
+    if (at < 64) {
+      p.b = base + at;
+      p.before += __builtin_amdgcn_readlane(upto - n, at);
+      break;
+    }
+    p.before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  p.b = __builtin_amdgcn_readfirstlane(p.b);
+  p.before = __builtin_amdgcn_readfirstlane(p.before);
+  return p;
+}
+
+__device__ __forceinline__ float max_of_columns(float v) {  // over the lanes l, l + 16, l + 32, l + 48
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
+}
+
+__device__ __forceinline__ uint32_t any_byte_255(uint32_t w) { return (~w - 0x01010101u) & w & 0x80808080u; }
+// The word with its bytes of 255 as 0.
+__device__ __forceinline__ uint32_t without_255(uint32_t w) {
+  uint32_t o = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t b = w >> (8 * i) & 255u;
+    o |= (b == 255u ? 0u : b) << (8 * i);
+  }
+  return o;
+}
+
+// A column's sums of one piece of the tokens, in powers of two of `m`.
+__device__ __forceinline__ float lse_of(float m, float l) { return (m + __log2f(l)) * 0.6931471805599453f; }
+
+template <int D>
+struct Block {  // 32 tokens in a lane
+  static constexpr int W = D / 32;  // words of keys per 16 tokens, and of values per 4
+  uint32_t k[2][W], v[2 * W], vs[2];
+  uint32_t ks[2];
+};
+
+template <int D>
+__device__ __forceinline__ void load_block(Block<D>& x, const Cache4& c, int64_t head, int at, int l, int g) {
+  // at: the block's first token in its page
+  constexpr int W = D / 32;
+  const int64_t tok = (head << c.log_page) + at;
+  const uint8_t* k = c.k + (tok * D >> 1);
+  const uint8_t* v = c.v + (tok * D >> 1) + (l * 4 + g) * (D / 4);
+  const uint8_t* ks = c.ks + tok * W;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const uint8_t* kt = k + t * (8 * D);
+    const uint8_t* st = ks + (t * 16 + l) * W;
+    if constexpr (D == 64) {
+      __builtin_memcpy(x.k[t], kt + (g >> 1) * 256 + l * 16 + (g & 1) * 8, 8);
+      x.ks[t] = st[g >> 1];
+    } else if constexpr (D == 128) {
+      __builtin_memcpy(x.k[t], kt + g * 256 + l * 16, 16);
+      x.ks[t] = st[g];
+    } else {
+      __builtin_memcpy(x.k[t], kt + g * 512 + l * 16, 16);
+      __builtin_memcpy(x.k[t] + 4, kt + g * 512 + 256 + l * 16, 16);
+      x.ks[t] = *reinterpret_cast<const uint16_t*>(st + 2 * g);
+    }
+  }
+  const uint4* v4 = reinterpret_cast<const uint4*>(v);
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const uint4 w = v4[i];
+    x.v[4 * i] = w.x;
+    x.v[4 * i + 1] = w.y;
+    x.v[4 * i + 2] = w.z;
+    x.v[4 * i + 3] = w.w;
+  }
+  __builtin_memcpy(x.vs, c.vs + tok * W + l * D / 512 * 32 + g * 8, 8);
+}
+
+// Eight tokens' codes of the values 2 P and 2 P + 1 of a lane, as two operands: token j's
+// are in byte P of its D / 32.
+template <int D, int P>
+__device__ __forceinline__ void values_pair(const uint32_t* v, const float* s, uint4& even, uint4& odd) {
+  uint32_t u[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if constexpr (D == 64)
+      u[j] = j & 1 ? mx4_pair<2 + (P & 1)>(v[j >> 1], s[j]) : mx4_pair<(P & 1)>(v[j >> 1], s[j]);
+    else
+      u[j] = mx4_pair<(P & 3)>(v[j * (D / 128) + P / 4], s[j]);
+  }
+  even = make_uint4(__builtin_amdgcn_perm(u[1], u[0], 0x05040100u), __builtin_amdgcn_perm(u[3], u[2], 0x05040100u),
+                    __builtin_amdgcn_perm(u[5], u[4], 0x05040100u), __builtin_amdgcn_perm(u[7], u[6], 0x05040100u));
+  odd = make_uint4(__builtin_amdgcn_perm(u[1], u[0], 0x07060302u), __builtin_amdgcn_perm(u[3], u[2], 0x07060302u),
+                   __builtin_amdgcn_perm(u[5], u[4], 0x07060302u), __builtin_amdgcn_perm(u[7], u[6], 0x07060302u));
+}
+
+template <int D, int NC, int P>
+__device__ __forceinline__ void add_values(f32x4_t (&o)[NC][D / 16], const uint32_t* v, const float* s, const bf16x8_t* p) {
+  if constexpr (P < D / 32) {
+    uint4 even, odd;
+    values_pair<D, P>(v, s, even, odd);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      o[c][2 * P] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, even), p[c], o[c][2 * P], 0, 0, 0);
+      o[c][2 * P + 1] =
+          __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, odd), p[c], o[c][2 * P + 1], 0, 0, 0);
+    }
+    add_values<D, NC, P + 1>(o, v, s, p);
+  }
+}
+
+}  // namespace
+
+template <int D, int NC>
+__global__ __launch_bounds__(256) void attend4_kernel(const Attend4Args a) {
+  constexpr int COLS = 16 * NC, STEPS = D / 32, NT = D / 16, PITCH = D + 4;
+  __shared__ __attribute__((aligned(16))) float part_o[4][16][PITCH];
+  __shared__ float part_m[4][16], part_l[4][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l = lane & 15, g = lane >> 4;
+  // an XCD's workgroups have neighbouring shares
+  const int w = (int)(blockIdx.x & 7) * (a.workers >> 3) + (int)(blockIdx.x >> 3);
+  const Place place = find_place<COLS>(a, w);
+  const uint4 ones4 = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+  const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, ones4);
+
+  int u = place.u0, b = place.b, before = place.before;
+  while (u < place.u1 && b < a.s.batch) {
+    const SeqUnits q = seq_units<COLS>(a, b);
+    const int seq_total = q.units(a.c.heads);
+    if (u - before >= seq_total) {
+      before += seq_total;
+      ++b;
+      continue;
+    }
+    // the tile of columns and the units of it that are this workgroup's
+    const int item = (u - before) / q.nb, start = u - before - item * q.nb;
+    const int end = min(q.nb, start + place.u1 - u);
+    const int h = item / q.ct, tile = item - h * q.ct;
+    u += end - start;
+
+    const int cols = (int)min((int64_t)COLS, (int64_t)q.s.n * a.group - (int64_t)tile * COLS);  // at least one
+    const int r0 = tile * COLS / a.group, r1 = (tile * COLS + cols - 1) / a.group;  // rows of the sequence
+    const int pos0 = q.s.len - q.s.n + r0, pos1 = q.s.len - q.s.n + r1;             // their tokens
+    // this lane's columns
+    bf16x8_t qv[NC][STEPS];
+    int pos[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int col = tile * COLS + min(c * 16 + l, cols - 1), r = col / a.group, head = col - r * a.group;
+      pos[c] = q.s.len - q.s.n + r;
+      const uint16_t* at = a.q + (int64_t)(q.s.row0 + r) * a.q_row + (int64_t)(h * a.group + head) * a.q_head + g * (D / 4);
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) __builtin_memcpy(&qv[c][s], at + s * 8, 16);
+    }
+    f32x4_t o[NC][NT], sum[NC];
+    float m[NC], off[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) o[c][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      sum[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      m[c] = kNegInf;
+      off[c] = 0.f;
+    }
+
+    // blocks of 32 tokens that any column of the tile sees
+    int blk = (q.first + start) * 4, blk_end = min((q.first + end) * 4, (pos1 + 32) >> 5);
+    if (a.window) blk = max(blk, max(0, pos0 - a.window + 1) >> 5);
+    blk += wave;
+    const int pages32 = a.c.log_page - 5;
+    Block<D> x[2];
+    auto load = [&](int i, int at) {
+      const int page = seq_page(a.s, a.c.n_pages, b, at >> pages32);
+      load_block<D>(x[i], a.c, (int64_t)page * a.c.heads + h, (at & ((1 << pages32) - 1)) * 32, l, g);
+    };
+    auto step = [&](int i, int at) {
+      f32x4_t sc[2][NC];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c) sc[t][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        float s0, s1;
+        if constexpr (D == 256) {
+          s0 = mx4_scale(x[i].ks[t] & 255u);
+          s1 = mx4_scale(x[i].ks[t] >> 8);
+        } else {
+          s0 = s1 = mx4_scale(x[i].ks[t]);
+        }
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+          const bf16x8_t kv = __builtin_bit_cast(bf16x8_t, mx4_bf16x8(x[i].k[t][s], s < 4 ? s0 : s1));
+#pragma unroll
+          for (int c = 0; c < NC; ++c) sc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, qv[c][s], sc[t][c], 0, 0, 0);
+        }
+      }
+      uint32_t vs[2] = {x[i].vs[0], x[i].vs[1]};
+      const int t0 = at * 32;
+      const bool edge = t0 + 31 > pos0 || (a.window && t0 <= pos1 - a.window);
+      bool lost = false;  // a block of values that is NaN where some column may not see it
+      if (edge) {
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int tok = t0 + t * 16 + g * 4 + j;
+              if (tok > pos[c] || (a.window && tok <= pos[c] - a.window)) sc[t][c][j] = kNegInf;
+            }
+        lost = __ballot((any_byte_255(vs[0]) | any_byte_255(vs[1])) != 0) != 0;
+        if (lost) {
+          vs[0] = without_255(vs[0]);
+          vs[1] = without_255(vs[1]);
+        }
+      }
+      bf16x8_t p[NC];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        float big = fmaxf(fmaxf(fmaxf(sc[0][c][0], sc[0][c][1]), fmaxf(sc[0][c][2], sc[0][c][3])),
+                          fmaxf(fmaxf(sc[1][c][0], sc[1][c][1]), fmaxf(sc[1][c][2], sc[1][c][3])));
+        big *= a.scale;
+        if (__ballot(big > m[c] + kAhead)) {
+          const float now = fmaxf(m[c], max_of_columns(big));
+          const float shrink = now == m[c] ? 1.f : __builtin_amdgcn_exp2f(m[c] - now);
+          m[c] = now;
+          off[c] = now == kNegInf ? 0.f : -now;
+          sum[c] *= shrink;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) o[c][n] *= shrink;
+        }
+        uint32_t pk[4];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int j = 0; j < 4; j += 2)
+            pk[t * 2 + (j >> 1)] = bf16_pair(__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][c][j], a.scale, off[c])),
+                                             __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][c][j + 1], a.scale, off[c])));
+        p[c] = __builtin_bit_cast(bf16x8_t, make_uint4(pk[0], pk[1], pk[2], pk[3]));
+        sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[c], sum[c], 0, 0, 0);
+      }
+      float fs[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) fs[j] = mx4_scale(vs[j >> 2] >> (8 * (j & 3)) & 255u);
+      add_values<D, NC, 0>(o, x[i].v, fs, p);
+      if (lost) {
+        // columns that see a token whose block is NaN: that token counts 1 for this lane's
+        // values, a token that a column sees 1 for it
+        uint32_t na[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t pair = x[i].vs[j >> 1] >> (16 * (j & 1));
+          na[j] = ((pair & 255u) == 255u ? 0x3f80u : 0u) | ((pair >> 8 & 255u) == 255u ? 0x3f800000u : 0u);
+        }
+        const bf16x8_t nan_at = __builtin_bit_cast(bf16x8_t, make_uint4(na[0], na[1], na[2], na[3]));
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          uint32_t se[4];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int tok = t0 + (j >> 2) * 16 + g * 4 + (j & 3);
+            const bool sees = tok <= pos[c] && (!a.window || tok > pos[c] - a.window);
+            const uint32_t one = sees ? 0x3f80u << (16 * (j & 1)) : 0u;
+            se[j >> 1] = j & 1 ? se[j >> 1] | one : one;
+          }
+          const f32x4_t hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              nan_at, __builtin_bit_cast(bf16x8_t, make_uint4(se[0], se[1], se[2], se[3])), f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (hit[j] > 0.f) o[c][n][j] = NAN;
+        }
+      }
+    };
+    if (blk < blk_end) {
+      load(0, blk);
+      for (;;) {
+        if (blk + 4 < blk_end) load(1, blk + 4);
+        step(0, blk);
+        blk += 4;
+        if (blk >= blk_end) break;
+        if (blk + 4 < blk_end) load(0, blk + 4);
+        step(1, blk);
+        blk += 4;
+        if (blk >= blk_end) break;
+      }
+    }
+
+    // The four waves' sums, 16 columns at a time.
+    const bool whole = start == 0 && end == q.nb;
+    float* slot = a.parts + (int64_t)(2 * w + (start == 0)) * (COLS * (D + 2));
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < NT; n += 4)
+          *reinterpret_cast<float4*>(&part_o[wave][l][(4 * g + j) * NT + n]) =
+              make_float4(o[c][n][j], o[c][n + 1][j], o[c][n + 2][j], o[c][n + 3][j]);
+      if (g == 0) {
+        part_m[wave][l] = m[c];
+        part_l[wave][l] = sum[c][0];
+      }
+      __syncthreads();
+      for (int e = tid; e < 16 * (D / 4); e += 256) {
+        const int col = e / (D / 4), d = (e % (D / 4)) * 4;
+        if (c * 16 + col >= cols) continue;
+        const float top = fmaxf(fmaxf(part_m[0][col], part_m[1][col]), fmaxf(part_m[2][col], part_m[3][col]));
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        float ls = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float f = part_m[i][col] == top ? 1.f : __builtin_amdgcn_exp2f(part_m[i][col] - top);
+          const float4 v = *reinterpret_cast<const float4*>(&part_o[i][col][d]);
+          s = make_float4(s.x + f * v.x, s.y + f * v.y, s.z + f * v.z, s.w + f * v.w);
+          ls += f * part_l[i][col];
+        }
+        if (!whole) {
+          *reinterpret_cast<float4*>(slot + (c * 16 + col) * D + d) = s;
+          if (d == 0) {
+            slot[COLS * D + c * 16 + col] = top;
+            slot[COLS * D + COLS + c * 16 + col] = ls;
+          }
+          continue;
+        }
+        const int at = tile * COLS + c * 16 + col, r = at / a.group, head = h * a.group + at - r * a.group;
+        const int64_t row = q.s.row0 + r;
+        const bool empty = q.s.len - q.s.n + r < 0;
+        const float inv = 1.f / ls;
+        store4(a.out, kBF16, row * a.o_row + head * a.o_head + d, 4,
+               empty ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv));
+        if (a.lse && d == 0) a.lse[row * ((int64_t)a.c.heads * a.group) + head] = empty ? kNegInf : lse_of(top, ls);
+      }
+    }
+  }
+}
+
+// The parts of a tile, joined by the workgroup that has its place of the last of them.
+template <int D, int NC>
+__global__ __launch_bounds__(256) void attend4_join_kernel(const Attend4Args a) {
+  constexpr int COLS = 16 * NC, SLOT = COLS * (D + 2);
+  const int w = blockIdx.x;
+  const Place place = find_place<COLS>(a, w);
+  if (place.u0 >= place.u1 || place.b >= a.s.batch) return;
+  const SeqUnits q = seq_units<COLS>(a, place.b);
+  const int item = (place.u0 - place.before) / q.nb, start = place.u0 - place.before - item * q.nb;
+  if (start == 0 || place.u1 - place.u0 < q.nb - start) return;  // begins here, or goes on behind
+  const int item_u = place.u0 - start;
+  // the first workgroup of the tile: the last one that starts at or before it
+  const int w0 = (int)((((int64_t)item_u + 1) * a.workers - 1) / place.total);
+  const int h = item / q.ct, tile = item - h * q.ct;
+  const int cols = (int)min((int64_t)COLS, (int64_t)q.s.n * a.group - (int64_t)tile * COLS);
+  for (int e = threadIdx.x; e < cols * (D / 4); e += 256) {
+    const int col = e / (D / 4), d = (e % (D / 4)) * 4;
+    float top = kNegInf, ls = 0.f;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = w0; i <= w; ++i) {
+      // (the tile starts inside w0's share, at its end or not; a share without units has no part)
+      const int from = share_start(place.total, a.workers, i), to = share_start(place.total, a.workers, i + 1);
+      if (from == to) continue;
+      const float* slot = a.parts + (int64_t)(2 * i + (from <= item_u)) * SLOT;
+      const float m = slot[COLS * D + col], pl = slot[COLS * D + COLS + col];
+      const float4 v = *reinterpret_cast<const float4*>(slot + col * D + d);
+      const float now = fmaxf(top, m);
+      const float f0 = top == now ? 1.f : __builtin_amdgcn_exp2f(top - now), f1 = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
+      s = make_float4(s.x * f0 + v.x * f1, s.y * f0 + v.y * f1, s.z * f0 + v.z * f1, s.w * f0 + v.w * f1);
+      ls = ls * f0 + pl * f1;
+      top = now;
+    }
+    const int at = tile * COLS + col, r = at / a.group, head = h * a.group + at - r * a.group;
+    const int64_t row = q.s.row0 + r;
+    const bool empty = q.s.len - q.s.n + r < 0;
+    const float inv = 1.f / ls;
+    store4(a.out, kBF16, row * a.o_row + head * a.o_head + d, 4,
+           empty ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv));
+    if (a.lse && d == 0) a.lse[row * ((int64_t)a.c.heads * a.group) + head] = empty ? kNegInf : lse_of(top, ls);
+  }
+}
+
+Attend4Plan attend4_plan(int batch, int total, int heads, int group, int d, int64_t max_len, int ncu) {
+  Attend4Plan p{};
+  const int64_t cols = ((int64_t)total + batch - 1) / std::max(batch, 1) * group;  // of a sequence, on average
+  p.nc = cols <= 16 ? 1 : 2;
+  const int64_t most = (int64_t)heads * ((int64_t)total * group / (16 * p.nc) + batch) * std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit);
+  const int per_cu = d == 256 || p.nc > 1 ? 2 : 4;
+  p.workers = (int)std::min<int64_t>((most + 7) / 8 * 8, (int64_t)ncu * per_cu);
+  p.bytes = (int64_t)p.workers * 2 * (16 * p.nc) * (d + 2) * 4;
+  return p;
+}
+
+template <int D, int NC>
+static hipError_t attend_launch(const Attend4Args& a, hipStream_t s) {
+  attend4_kernel<D, NC><<<a.workers, 256, 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  attend4_join_kernel<D, NC><<<a.workers, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_attend4(const Attend4Args& a, int nc, hipStream_t s) {
+  switch (a.c.d * 8 + nc) {
+    case 64 * 8 + 1: return attend_launch<64, 1>(a, s);
+    case 64 * 8 + 2: return attend_launch<64, 2>(a, s);
+    case 128 * 8 + 1: return attend_launch<128, 1>(a, s);
+    case 128 * 8 + 2: return attend_launch<128, 2>(a, s);
+    case 256 * 8 + 1: return attend_launch<256, 1>(a, s);
+    default: return attend_launch<256, 2>(a, s);
+  }
+}
+
+}  // namespace aep

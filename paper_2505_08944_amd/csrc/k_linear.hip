@@ -11,8 +11,8 @@
 // launch 1.5.
 #include <algorithm>
 
+#include "linear4.h"
 #include "linear_epilogue.h"
-#include "linear_tiles.h"
 
 namespace aep {
 
@@ -282,6 +282,10 @@ static hipError_t align_rows(const void* src, int64_t ld, int rows, int k, int64
   linear_align_kernel<<<(unsigned)((chunks + 255) / 256), 256, 0, s>>>(reinterpret_cast<const T*>(src), ld, rows, k,
                                                                        (int)(chunks / rows), reinterpret_cast<uint4*>(dst));
   return hipGetLastError();
+}
+
+hipError_t linear_align_bf16(const void* src, int64_t ld, int rows, int k, int64_t bytes, void* dst, hipStream_t s) {
+  return align_rows<uint16_t>(src, ld, rows, k, bytes, dst, s);
 }
 
 hipError_t launch_linear(const LinearArgs& p, int nwg, float* scratch, int64_t scratch_floats, hipStream_t s) {

@@ -44,42 +44,7 @@ RouterArgs router_args(const aep_router& r) {
   return a;
 }
 
-}  // namespace aep
-
-namespace {
-
-bool off(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
-int esize(int32_t t) { return t == AEP_F32 ? 4 : t == AEP_BF16 ? 2 : 1; }
-
-aep_status check_linear(const aep_linear_desc* l) {
-  if (!l || l->m < 0 || l->n < 1 || l->k < 1) return AEP_ERR_INVALID_ARG;
-  const int32_t types[] = {l->x_dtype, l->w_dtype, l->y_dtype, l->bias_dtype, l->res_dtype};
-  for (int32_t t : types)
-    if (t < AEP_F32 || t > AEP_FP8_E4M3) return AEP_ERR_INVALID_ARG;
-  if (l->fn < AEP_FN_NONE || l->fn > AEP_FN_GELU_TANH) return AEP_ERR_INVALID_ARG;
-  if (l->ldx < l->k || l->ldw < l->k || l->ldy < l->n) return AEP_ERR_INVALID_ARG;
-  const bool f32 = l->x_dtype == AEP_F32 && l->w_dtype == AEP_F32 && l->y_dtype == AEP_F32;
-  const bool bf = l->x_dtype == AEP_BF16 && (l->w_dtype == AEP_BF16 || l->w_dtype == AEP_FP8_E4M3) &&
-                  (l->y_dtype == AEP_BF16 || l->y_dtype == AEP_F32);
-  if (!f32 && !bf) return AEP_ERR_UNSUPPORTED;
-  if (l->bias_dtype == AEP_FP8_E4M3 || l->res_dtype == AEP_FP8_E4M3) return AEP_ERR_UNSUPPORTED;
-  // indices and tile counts are 32-bit (an output of 2^38 values does not fit any GPU)
-  if (std::max({l->m, l->n, l->k}) > 1 << 30 || (int64_t)l->m * l->n > (int64_t)1 << 38) return AEP_ERR_UNSUPPORTED;
-  return AEP_OK;
-}
-
-// One workgroup per CU of the current device, a multiple of the 8 XCDs.
-int persistent_workgroups() {
-  constexpr int kDevices = 64;
-  static std::atomic<int> seen[kDevices];  // 0: not asked yet
-  int dev = -1, n = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kDevices) return 256;
-  if ((n = seen[dev].load(std::memory_order_relaxed)) > 0) return n;
-  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 256;
-  n = ffn_grid(n);
-  seen[dev].store(n, std::memory_order_relaxed);
-  return n;
-}
+static int esize(int32_t t) { return t == AEP_F32 ? 4 : t == AEP_BF16 ? 2 : 1; }
 
 LinearArgs linear_args(const aep_linear_desc& l, const void* x, const void* w, const void* scale, const void* bias,
                        const void* residual, void* y) {
@@ -116,6 +81,41 @@ LinearArgs linear_args(const aep_linear_desc& l, const void* x, const void* w, c
       (!residual || (f32_res ? l.ldr < 1 << 21 : !off(residual, 4) && l.ldr % 2 == 0)))
     p.wide = kWideF32;
   return p;
+}
+
+// One workgroup per CU of the current device, a multiple of the 8 XCDs.
+int persistent_workgroups() {
+  constexpr int kDevices = 64;
+  static std::atomic<int> seen[kDevices];  // 0: not asked yet
+  int dev = -1, n = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kDevices) return 256;
+  if ((n = seen[dev].load(std::memory_order_relaxed)) > 0) return n;
+  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 256;
+  n = ffn_grid(n);
+  seen[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
+}  // namespace aep
+
+namespace {
+
+
+aep_status check_linear(const aep_linear_desc* l) {
+  if (!l || l->m < 0 || l->n < 1 || l->k < 1) return AEP_ERR_INVALID_ARG;
+  const int32_t types[] = {l->x_dtype, l->w_dtype, l->y_dtype, l->bias_dtype, l->res_dtype};
+  for (int32_t t : types)
+    if (t < AEP_F32 || t > AEP_FP8_E4M3) return AEP_ERR_INVALID_ARG;
+  if (l->fn < AEP_FN_NONE || l->fn > AEP_FN_GELU_TANH) return AEP_ERR_INVALID_ARG;
+  if (l->ldx < l->k || l->ldw < l->k || l->ldy < l->n) return AEP_ERR_INVALID_ARG;
+  const bool f32 = l->x_dtype == AEP_F32 && l->w_dtype == AEP_F32 && l->y_dtype == AEP_F32;
+  const bool bf = l->x_dtype == AEP_BF16 && (l->w_dtype == AEP_BF16 || l->w_dtype == AEP_FP8_E4M3) &&
+                  (l->y_dtype == AEP_BF16 || l->y_dtype == AEP_F32);
+  if (!f32 && !bf) return AEP_ERR_UNSUPPORTED;
+  if (l->bias_dtype == AEP_FP8_E4M3 || l->res_dtype == AEP_FP8_E4M3) return AEP_ERR_UNSUPPORTED;
+  // indices and tile counts are 32-bit (an output of 2^38 values does not fit any GPU)
+  if (std::max({l->m, l->n, l->k}) > 1 << 30 || (int64_t)l->m * l->n > (int64_t)1 << 38) return AEP_ERR_UNSUPPORTED;
+  return AEP_OK;
 }
 
 // Bytes of scratch of the cut that is taken where there is enough.
