@@ -72,8 +72,18 @@ struct Attend4Args {
   int group;    // heads of queries per head of the cache
   int window;
   float scale;  // times log2 e
+  int workers, nc;
+  // Scratch: two parts of a tile for each workgroup (of the tile that its share begins inside
+  // of, and of the one that begins in its share and goes on behind it), 16 nc columns of D sums, a
+  // reference and a sum of weights each; then what the second launch has to know of the latter.
   float* parts;
-  int workers;
+  struct Shared {
+    int last;  // its last workgroup (0: there is no such tile)
+    int total, head, tile, cols, row0, pos0, pad;
+  };
+  __host__ __device__ Shared* shared() const {
+    return reinterpret_cast<Shared*>(parts + (int64_t)workers * 2 * (16 * nc) * (c.d + 2));
+  }
 };
 // The attention's launch: columns of 16 per workgroup, workgroups, bytes of scratch.
 struct Attend4Plan {
@@ -81,7 +91,7 @@ struct Attend4Plan {
   int64_t bytes;
 };
 Attend4Plan attend4_plan(int batch, int total, int heads, int group, int d, int64_t max_len, int ncu);
-hipError_t launch_attend4(const Attend4Args& a, int nc, hipStream_t s);
+hipError_t launch_attend4(const Attend4Args& a, hipStream_t s);
 hipError_t launch_cache4_append(const Cache4& c, const Cache4Seqs& q, const uint16_t* k, const uint16_t* v, int64_t k_row,
                                 int64_t k_head, int64_t v_row, int64_t v_head, hipStream_t s);
 hipError_t launch_cache4_read(const Cache4& c, const Cache4Seqs& q, uint16_t* k, uint16_t* v, hipStream_t s);

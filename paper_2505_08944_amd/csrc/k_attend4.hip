@@ -15,6 +15,7 @@
 // Tiles that several workgroups share leave parts in the scratch, which a second launch joins
 // in the order of the tokens.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 
 #include "cache4.h"
@@ -26,6 +27,8 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 namespace {
+
+using Shared = Attend4Args::Shared;
 
 constexpr int kUnit = 128;  // tokens
 constexpr float kNegInf = -INFINITY;
@@ -130,40 +133,45 @@ struct Block {  // 32 tokens in a lane
   uint32_t ks[2];
 };
 
+// Block of 32 tokens, the `at`th of its page, of head `head` of all pages' heads.  (One base for
+// the wave and a lane's own 32-bit offset: addresses take no registers but that.)
 template <int D>
-__device__ __forceinline__ void load_block(Block<D>& x, const Cache4& c, int64_t head, int at, int l, int g) {
-  // at: the block's first token in its page
-  constexpr int W = D / 32;
-  const int64_t tok = (head << c.log_page) + at;
+__device__ __forceinline__ void load_keys(Block<D>& x, const Cache4& c, int64_t head, int at, uint32_t l, uint32_t g) {
+  constexpr uint32_t W = D / 32;
+  const int64_t tok = (head << c.log_page) + at * 32;
   const uint8_t* k = c.k + (tok * D >> 1);
-  const uint8_t* v = c.v + (tok * D >> 1) + (l * 4 + g) * (D / 4);
   const uint8_t* ks = c.ks + tok * W;
+  const uint32_t kl = D == 64 ? (g >> 1) * 256 + l * 16 + (g & 1) * 8 : g * (2 * D) + l * 16;
+  const uint32_t sl = l * W + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const uint8_t* kt = k + t * (8 * D);
-    const uint8_t* st = ks + (t * 16 + l) * W;
     if constexpr (D == 64) {
-      __builtin_memcpy(x.k[t], kt + (g >> 1) * 256 + l * 16 + (g & 1) * 8, 8);
-      x.ks[t] = st[g >> 1];
+      *reinterpret_cast<uint2*>(x.k[t]) = *reinterpret_cast<const uint2*>(k + t * (8 * D) + kl);
+      x.ks[t] = (ks + t * (16 * W))[sl];
     } else if constexpr (D == 128) {
-      __builtin_memcpy(x.k[t], kt + g * 256 + l * 16, 16);
-      x.ks[t] = st[g];
+      *reinterpret_cast<uint4*>(x.k[t]) = *reinterpret_cast<const uint4*>(k + t * (8 * D) + kl);
+      x.ks[t] = (ks + t * (16 * W))[sl];
     } else {
-      __builtin_memcpy(x.k[t], kt + g * 512 + l * 16, 16);
-      __builtin_memcpy(x.k[t] + 4, kt + g * 512 + 256 + l * 16, 16);
-      x.ks[t] = *reinterpret_cast<const uint16_t*>(st + 2 * g);
+      *reinterpret_cast<uint4*>(x.k[t]) = *reinterpret_cast<const uint4*>(k + t * (8 * D) + kl);
+      *reinterpret_cast<uint4*>(x.k[t] + 4) = *reinterpret_cast<const uint4*>(k + t * (8 * D) + 256 + kl);
+      x.ks[t] = *reinterpret_cast<const uint16_t*>(ks + t * (16 * W) + sl);
     }
   }
-  const uint4* v4 = reinterpret_cast<const uint4*>(v);
+}
+template <int D>
+__device__ __forceinline__ void load_values(Block<D>& x, const Cache4& c, int64_t head, int at, uint32_t l, uint32_t g) {
+  const int64_t tok = (head << c.log_page) + at * 32;
+  const uint8_t* v = c.v + (tok * D >> 1);
+  const uint32_t vl = (l * 4 + g) * (D / 4), sl = l * D / 512 * 32 + g * 8;
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) {
-    const uint4 w = v4[i];
+    const uint4 w = *reinterpret_cast<const uint4*>(v + i * 16 + vl);
     x.v[4 * i] = w.x;
     x.v[4 * i + 1] = w.y;
     x.v[4 * i + 2] = w.z;
     x.v[4 * i + 3] = w.w;
   }
-  __builtin_memcpy(x.vs, c.vs + tok * W + l * D / 512 * 32 + g * 8, 8);
+  *reinterpret_cast<uint2*>(x.vs) = *reinterpret_cast<const uint2*>(c.vs + tok * (D / 32) + sl);
 }
 
 // Eight tokens' codes of the values 2 P and 2 P + 1 of a lane, as two operands: token j's
@@ -195,14 +203,18 @@ __device__ __forceinline__ void add_values(f32x4_t (&o)[NC][D / 16], const uint3
       o[c][2 * P + 1] =
           __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, odd), p[c], o[c][2 * P + 1], 0, 0, 0);
     }
+    __builtin_amdgcn_sched_barrier(0);  // (all of it at once would spill)
     add_values<D, NC, P + 1>(o, v, s, p);
   }
 }
 
 }  // namespace
 
+// Workgroups per CU, which are waves per SIMD: as many as registers allow without spilling.
+constexpr int attend_per_cu(int d, int nc) { return d * nc == 64 ? 4 : d * nc == 128 ? 3 : d * nc == 256 ? 2 : 1; }
+
 template <int D, int NC>
-__global__ __launch_bounds__(256) void attend4_kernel(const Attend4Args a) {
+__global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(const Attend4Args a) {
   constexpr int COLS = 16 * NC, STEPS = D / 32, NT = D / 16, PITCH = D + 4;
   __shared__ __attribute__((aligned(16))) float part_o[4][16][PITCH];
   __shared__ float part_m[4][16], part_l[4][16];
@@ -214,6 +226,7 @@ __global__ __launch_bounds__(256) void attend4_kernel(const Attend4Args a) {
   const uint4 ones4 = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
   const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, ones4);
 
+  Shared shared{};  // the tile that begins here and goes on behind
   int u = place.u0, b = place.b, before = place.before;
   while (u < place.u1 && b < a.s.batch) {
     const SeqUnits q = seq_units<COLS>(a, b);
@@ -258,13 +271,29 @@ __global__ __launch_bounds__(256) void attend4_kernel(const Attend4Args a) {
     int blk = (q.first + start) * 4, blk_end = min((q.first + end) * 4, (pos1 + 32) >> 5);
     if (a.window) blk = max(blk, max(0, pos0 - a.window + 1) >> 5);
     blk += wave;
-    const int pages32 = a.c.log_page - 5;
-    Block<D> x[2];
-    auto load = [&](int i, int at) {
-      const int page = seq_page(a.s, a.c.n_pages, b, at >> pages32);
-      load_block<D>(x[i], a.c, (int64_t)page * a.c.heads + h, (at & ((1 << pages32) - 1)) * 32, l, g);
+    const int pages32 = a.c.log_page - 5, in_page = (1 << pages32) - 1;
+    auto head_of = [&](int at) { 
+      const int page = __builtin_amdgcn_readfirstlane(seq_page(a.s, a.c.n_pages, b, at >> pages32));
+      return (int64_t)page * a.c.heads + h;
     };
-    auto step = [&](int i, int at) {
+    const auto at_edge = [&](int at) {  // some column does not see all of its tokens
+      return at * 32 + 31 > pos0 || (a.window && at * 32 <= pos1 - a.window);
+    };
+    Block<D> x;
+    int64_t next = 0;  // the next block's head of its page
+    bool lost = false;  // a block of values that is NaN where some column may not see it
+    const int blk0 = blk;
+    if (blk < blk_end) {
+      next = head_of(blk);
+      load_keys<D>(x, a.c, next, blk & in_page, l, g);
+      load_values<D>(x, a.c, next, blk & in_page, l, g);
+      if (blk + 4 < blk_end) next = head_of(blk + 4);
+    }
+    // A block's keys make room for the next one's as soon as the scores are there, its values when
+    // they have been added: no second set of registers, and the other waves hide the loads.
+    for (; blk < blk_end; blk += 4) {
+      const int64_t after = blk + 8 < blk_end ? head_of(blk + 8) : 0;
+      const bool more = blk + 4 < blk_end;
       f32x4_t sc[2][NC];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -272,36 +301,37 @@ __global__ __launch_bounds__(256) void attend4_kernel(const Attend4Args a) {
         for (int c = 0; c < NC; ++c) sc[t][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         float s0, s1;
         if constexpr (D == 256) {
-          s0 = mx4_scale(x[i].ks[t] & 255u);
-          s1 = mx4_scale(x[i].ks[t] >> 8);
+          s0 = mx4_scale(x.ks[t] & 255u);
+          s1 = mx4_scale(x.ks[t] >> 8);
         } else {
-          s0 = s1 = mx4_scale(x[i].ks[t]);
+          s0 = s1 = mx4_scale(x.ks[t]);
         }
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-          const bf16x8_t kv = __builtin_bit_cast(bf16x8_t, mx4_bf16x8(x[i].k[t][s], s < 4 ? s0 : s1));
+          const bf16x8_t kv = __builtin_bit_cast(bf16x8_t, mx4_bf16x8(x.k[t][s], s < 4 ? s0 : s1));
 #pragma unroll
           for (int c = 0; c < NC; ++c) sc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, qv[c][s], sc[t][c], 0, 0, 0);
         }
       }
-      uint32_t vs[2] = {x[i].vs[0], x[i].vs[1]};
-      const int t0 = at * 32;
-      const bool edge = t0 + 31 > pos0 || (a.window && t0 <= pos1 - a.window);
-      bool lost = false;  // a block of values that is NaN where some column may not see it
-      if (edge) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) load_keys<D>(x, a.c, next, (blk + 4) & in_page, l, g);
+      if (at_edge(blk)) {
+        int from[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) from[c] = a.window ? pos[c] - a.window : INT_MIN;
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
           for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const int tok = t0 + t * 16 + g * 4 + j;
-              if (tok > pos[c] || (a.window && tok <= pos[c] - a.window)) sc[t][c][j] = kNegInf;
+              const int tok = blk * 32 + t * 16 + g * 4 + j;
+              if (tok > pos[c] || tok <= from[c]) sc[t][c][j] = kNegInf;
             }
-        lost = __ballot((any_byte_255(vs[0]) | any_byte_255(vs[1])) != 0) != 0;
-        if (lost) {
-          vs[0] = without_255(vs[0]);
-          vs[1] = without_255(vs[1]);
+        if (__ballot((any_byte_255(x.vs[0]) | any_byte_255(x.vs[1])) != 0)) {
+          lost = true;  // (seen to behind the loop)
+          x.vs[0] = without_255(x.vs[0]);
+          x.vs[1] = without_255(x.vs[1]);
         }
       }
       bf16x8_t p[NC];
@@ -329,17 +359,24 @@ __global__ __launch_bounds__(256) void attend4_kernel(const Attend4Args a) {
         p[c] = __builtin_bit_cast(bf16x8_t, make_uint4(pk[0], pk[1], pk[2], pk[3]));
         sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[c], sum[c], 0, 0, 0);
       }
+      __builtin_amdgcn_sched_barrier(0);
       float fs[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) fs[j] = mx4_scale(vs[j >> 2] >> (8 * (j & 3)) & 255u);
-      add_values<D, NC, 0>(o, x[i].v, fs, p);
-      if (lost) {
-        // columns that see a token whose block is NaN: that token counts 1 for this lane's
-        // values, a token that a column sees 1 for it
+      for (int j = 0; j < 8; ++j) fs[j] = mx4_scale(x.vs[j >> 2] >> (8 * (j & 3)) & 255u);
+      add_values<D, NC, 0>(o, x.v, fs, p);
+      if (more) load_values<D>(x, a.c, next, (blk + 4) & in_page, l, g);
+      next = after;
+    }
+    if (lost) {
+      // Columns that see a token whose block is NaN have NaN there: such a token counts 1 for the
+      // values of this lane, a token that a column sees 1 for it.
+      for (int at = blk0; at < blk_end; at += 4) {
+        if (!at_edge(at)) continue;
+        load_values<D>(x, a.c, head_of(at), at & in_page, l, g);
         uint32_t na[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t pair = x[i].vs[j >> 1] >> (16 * (j & 1));
+          const uint32_t pair = x.vs[j >> 1] >> (16 * (j & 1));
           na[j] = ((pair & 255u) == 255u ? 0x3f80u : 0u) | ((pair >> 8 & 255u) == 255u ? 0x3f800000u : 0u);
         }
         const bf16x8_t nan_at = __builtin_bit_cast(bf16x8_t, make_uint4(na[0], na[1], na[2], na[3]));
@@ -348,7 +385,7 @@ __global__ __launch_bounds__(256) void attend4_kernel(const Attend4Args a) {
           uint32_t se[4];
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const int tok = t0 + (j >> 2) * 16 + g * 4 + (j & 3);
+            const int tok = at * 32 + (j >> 2) * 16 + g * 4 + (j & 3);
             const bool sees = tok <= pos[c] && (!a.window || tok > pos[c] - a.window);
             const uint32_t one = sees ? 0x3f80u << (16 * (j & 1)) : 0u;
             se[j >> 1] = j & 1 ? se[j >> 1] | one : one;
@@ -358,28 +395,19 @@ __global__ __launch_bounds__(256) void attend4_kernel(const Attend4Args a) {
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (hit[j] > 0.f) o[c][n][j] = NAN;
+            for (int j = 0; j < 4; ++j) o[c][n][j] = hit[j] > 0.f ? NAN : o[c][n][j];
         }
-      }
-    };
-    if (blk < blk_end) {
-      load(0, blk);
-      for (;;) {
-        if (blk + 4 < blk_end) load(1, blk + 4);
-        step(0, blk);
-        blk += 4;
-        if (blk >= blk_end) break;
-        if (blk + 4 < blk_end) load(0, blk + 4);
-        step(1, blk);
-        blk += 4;
-        if (blk >= blk_end) break;
       }
     }
 
     // The four waves' sums, 16 columns at a time.
     const bool whole = start == 0 && end == q.nb;
     float* slot = a.parts + (int64_t)(2 * w + (start == 0)) * (COLS * (D + 2));
+    if (start == 0 && !whole) {
+      // its last workgroup is the last one whose share starts at or before its last unit
+      const int64_t behind = (int64_t)u - end + q.nb;
+      shared = Shared{(int)((behind * a.workers - 1) / place.total), place.total, h, tile, cols, q.s.row0, q.s.len - q.s.n, 0};
+    }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       __syncthreads();
@@ -425,48 +453,67 @@ __global__ __launch_bounds__(256) void attend4_kernel(const Attend4Args a) {
       }
     }
   }
+  if (tid == 0) a.shared()[w] = shared;
 }
 
-// The parts of a tile, joined by the workgroup that has its place of the last of them.
+// The parts of a tile, joined: workgroup (w, y) has columns y 256 / D .. of the tile that
+// begins in w's share and goes on behind it, if there is one.  A lane has four values of a
+// column; the eight waves take every eighth part, four at a time, and are joined in LDS.
 template <int D, int NC>
-__global__ __launch_bounds__(256) void attend4_join_kernel(const Attend4Args a) {
-  constexpr int COLS = 16 * NC, SLOT = COLS * (D + 2);
-  const int w = blockIdx.x;
-  const Place place = find_place<COLS>(a, w);
-  if (place.u0 >= place.u1 || place.b >= a.s.batch) return;
-  const SeqUnits q = seq_units<COLS>(a, place.b);
-  const int item = (place.u0 - place.before) / q.nb, start = place.u0 - place.before - item * q.nb;
-  if (start == 0 || place.u1 - place.u0 < q.nb - start) return;  // begins here, or goes on behind
-  const int item_u = place.u0 - start;
-  // the first workgroup of the tile: the last one that starts at or before it
-  const int w0 = (int)((((int64_t)item_u + 1) * a.workers - 1) / place.total);
-  const int h = item / q.ct, tile = item - h * q.ct;
-  const int cols = (int)min((int64_t)COLS, (int64_t)q.s.n * a.group - (int64_t)tile * COLS);
-  for (int e = threadIdx.x; e < cols * (D / 4); e += 256) {
-    const int col = e / (D / 4), d = (e % (D / 4)) * 4;
-    float top = kNegInf, ls = 0.f;
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = w0; i <= w; ++i) {
-      // (the tile starts inside w0's share, at its end or not; a share without units has no part)
-      const int from = share_start(place.total, a.workers, i), to = share_start(place.total, a.workers, i + 1);
-      if (from == to) continue;
-      const float* slot = a.parts + (int64_t)(2 * i + (from <= item_u)) * SLOT;
-      const float m = slot[COLS * D + col], pl = slot[COLS * D + COLS + col];
-      const float4 v = *reinterpret_cast<const float4*>(slot + col * D + d);
-      const float now = fmaxf(top, m);
-      const float f0 = top == now ? 1.f : __builtin_amdgcn_exp2f(top - now), f1 = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
-      s = make_float4(s.x * f0 + v.x * f1, s.y * f0 + v.y * f1, s.z * f0 + v.z * f1, s.w * f0 + v.w * f1);
-      ls = ls * f0 + pl * f1;
-      top = now;
+__global__ __launch_bounds__(512) void attend4_join_kernel(const Attend4Args a) {
+  constexpr int COLS = 16 * NC, SLOT = COLS * (D + 2), LANES = D / 4;
+  __shared__ float4 part_v[8][64];
+  __shared__ float part_m[8][64], part_l[8][64];
+  const int w = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Shared t = a.shared()[w];
+  const int n = t.last - w + 1;  // workgroups that have a part
+  const int col = blockIdx.y * (64 / LANES) + lane / LANES, d = lane % LANES * 4;
+  if (n <= 1 || (int)blockIdx.y * (64 / LANES) >= t.cols) return;
+  const bool real = col < t.cols;
+  const float* at = a.parts + (int64_t)(2 * w) * SLOT;
+  float top = kNegInf, ls = 0.f;
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  const auto add = [&](float m, float l, const float4 v) {
+    const float now = fmaxf(top, m);
+    const float f0 = top == now ? 1.f : __builtin_amdgcn_exp2f(top - now), f1 = m == now ? 1.f : __builtin_amdgcn_exp2f(m - now);
+    s = make_float4(s.x * f0 + v.x * f1, s.y * f0 + v.y * f1, s.z * f0 + v.z * f1, s.w * f0 + v.w * f1);
+    ls = ls * f0 + l * f1;
+    top = now;
+  };
+  for (int i = wave; i < n; i += 32) {
+    float m[4], l[4];
+    float4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int p = i + 8 * j;
+      m[j] = kNegInf;
+      l[j] = 0.f;
+      v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+      // (where there are fewer units than workgroups, some have none)
+      if (real && p < n && share_start(t.total, a.workers, w + p) < share_start(t.total, a.workers, w + p + 1)) {
+        const float* slot = at + (int64_t)(p ? 2 * p : 1) * SLOT;
+        m[j] = slot[COLS * D + col];
+        l[j] = slot[COLS * D + COLS + col];
+        v[j] = *reinterpret_cast<const float4*>(slot + col * D + d);
+      }
     }
-    const int at = tile * COLS + col, r = at / a.group, head = h * a.group + at - r * a.group;
-    const int64_t row = q.s.row0 + r;
-    const bool empty = q.s.len - q.s.n + r < 0;
-    const float inv = 1.f / ls;
-    store4(a.out, kBF16, row * a.o_row + head * a.o_head + d, 4,
-           empty ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv));
-    if (a.lse && d == 0) a.lse[row * ((int64_t)a.c.heads * a.group) + head] = empty ? kNegInf : lse_of(top, ls);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) add(m[j], l[j], v[j]);
   }
+  part_v[wave][lane] = s;
+  part_m[wave][lane] = top;
+  part_l[wave][lane] = ls;
+  __syncthreads();
+  if (wave || !real) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) add(part_m[i][lane], part_l[i][lane], part_v[i][lane]);
+  const int c = t.tile * COLS + col, r = c / a.group, head = t.head * a.group + c - r * a.group;
+  const int64_t row = t.row0 + r;
+  const bool empty = t.pos0 + r < 0;
+  const float inv = 1.f / ls;
+  store4(a.out, kBF16, row * a.o_row + head * a.o_head + d, 4,
+         empty ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv));
+  if (a.lse && d == 0) a.lse[row * ((int64_t)a.c.heads * a.group) + head] = empty ? kNegInf : lse_of(top, ls);
 }
 
 Attend4Plan attend4_plan(int batch, int total, int heads, int group, int d, int64_t max_len, int ncu) {
@@ -474,9 +521,8 @@ Attend4Plan attend4_plan(int batch, int total, int heads, int group, int d, int6
   const int64_t cols = ((int64_t)total + batch - 1) / std::max(batch, 1) * group;  // of a sequence, on average
   p.nc = cols <= 16 ? 1 : 2;
   const int64_t most = (int64_t)heads * ((int64_t)total * group / (16 * p.nc) + batch) * std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit);
-  const int per_cu = d == 256 || p.nc > 1 ? 2 : 4;
-  p.workers = (int)std::min<int64_t>((most + 7) / 8 * 8, (int64_t)ncu * per_cu);
-  p.bytes = (int64_t)p.workers * 2 * (16 * p.nc) * (d + 2) * 4;
+  p.workers = (int)std::min<int64_t>((most + 7) / 8 * 8, (int64_t)ncu * attend_per_cu(d, p.nc));
+  p.bytes = (int64_t)p.workers * (2 * (16 * p.nc) * (d + 2) * 4 + (int64_t)sizeof(Attend4Args::Shared));
   return p;
 }
 
@@ -485,12 +531,14 @@ static hipError_t attend_launch(const Attend4Args& a, hipStream_t s) {
   attend4_kernel<D, NC><<<a.workers, 256, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  attend4_join_kernel<D, NC><<<a.workers, 256, 0, s>>>(a);
+  // (a tile's columns, as many as there can be)
+  const int64_t cols = a.s.rows ? 16 * NC : std::min<int64_t>(16 * NC, (int64_t)a.s.n * a.group);
+  attend4_join_kernel<D, NC><<<dim3(a.workers, (unsigned)((cols * D + 255) / 256)), 512, 0, s>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_attend4(const Attend4Args& a, int nc, hipStream_t s) {
-  switch (a.c.d * 8 + nc) {
+hipError_t launch_attend4(const Attend4Args& a, hipStream_t s) {
+  switch (a.c.d * 8 + a.nc) {
     case 64 * 8 + 1: return attend_launch<64, 1>(a, s);
     case 64 * 8 + 2: return attend_launch<64, 2>(a, s);
     case 128 * 8 + 1: return attend_launch<128, 1>(a, s);

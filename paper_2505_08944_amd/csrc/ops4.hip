@@ -260,7 +260,8 @@ aep_status aep_cache4_attend(const aep_cache4* c, const void* mem, const aep_cac
   g.scale = (float)((double)a->scale * 1.4426950408889634);
   g.parts = reinterpret_cast<float*>(d_ws);
   g.workers = p.workers;
-  return launched(launch_attend4(g, p.nc, stream_of(stream)));
+  g.nc = p.nc;
+  return launched(launch_attend4(g, stream_of(stream)));
 }
 
 }  // extern "C"
