@@ -31,6 +31,7 @@ namespace {
 using Shared = Attend4Args::Shared;
 
 constexpr int kUnit = 128;  // tokens
+constexpr int kAttendWide = 8;  // columns in 16s of the kernel for many
 constexpr float kNegInf = -INFINITY;
 // A column's reference follows its largest score (in powers of two) only when that is this
 // much ahead: most blocks then change nothing, and p stays below 2^8.
@@ -53,54 +54,65 @@ __device__ __forceinline__ SeqUnits seq_units(const Attend4Args& a, int b) {
   return u;
 }
 
-__device__ __forceinline__ int wave_sum(int v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
-}
-
 // Where a workgroup is among the units.
 struct Place {
+  int w, workers;  // its number, of so many that have units
   int total;     // units of all sequences
   int u0, u1;    // this workgroup's
   int b, before; // sequence of u0, units before that sequence
 };
-__device__ __forceinline__ int share_start(int total, int workers, int w) { return (int)((int64_t)total * w / workers); }
+// Units total / workers each, the first total % workers of them one more.
+struct Shares {
+  int each, more;
+  __device__ Shares(int total, int workers) : each((int)((uint32_t)total / (uint32_t)workers)), more(total - each * workers) {}
+  __device__ int start(int w) const { return w * each + min(w, more); }
+  __device__ int of(int unit) const {  // whose unit it is
+    const int behind = unit - more * (each + 1);
+    return behind < 0 ? (int)((uint32_t)unit / (uint32_t)(each + 1)) : more + (int)((uint32_t)behind / (uint32_t)each);
+  }
+};
 
 template <int COLS>
-__device__ __forceinline__ Place find_place(const Attend4Args& a, int w) {
-  const int lane = threadIdx.x & 63;
-  Place p;
-  int mine = 0, first = 0;
-  for (int b = lane; b < a.s.batch; b += 64) {
-    const int n = seq_units<COLS>(a, b).units(a.c.heads);
-    if (b == lane) first = n;
-    mine += n;
-  }
-  p.total = __builtin_amdgcn_readfirstlane(wave_sum(mine));
-  p.u0 = share_start(p.total, a.workers, w);
-  p.u1 = share_start(p.total, a.workers, w + 1);
-  p.b = a.s.batch;  // (found below, unless what is read changes meanwhile)
-  p.before = 0;
-  for (int base = 0; base < a.s.batch; base += 64) {
-    int n = first;
-    if (base) n = base + lane < a.s.batch ? seq_units<COLS>(a, base + lane).units(a.c.heads) : 0;
-    int upto = n;
+__device__ __forceinline__ Place find_place(const Attend4Args& a) {
+  const int lane = threadIdx.x & 63, batch = a.s.batch;
+  const auto units = [&](int b) { return b < batch ? seq_units<COLS>(a, b).units(a.c.heads) : 0; };
+  const auto upto = [&](int n) {  // sums of lanes 0 .. this one
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(upto, d);
-      if (lane >= d) upto += o;
+      const int o = __shfl_up(n, d);
+      if (lane >= d) n += o;
     }
-    const int at = __popcll(__ballot(p.before + upto <= p.u0));  // sequences that end before u0
+    return n;
+  };
+  Place p;
+  int n = units(lane), sum = upto(n), all = 0;
+  for (int base = 64; base < batch; base += 64) all += units(base + lane);
+  p.total = __builtin_amdgcn_readlane(sum, 63);
+  if (batch > 64) p.total += __builtin_amdgcn_readlane(upto(all), 63);
+  // an XCD's workgroups have neighbouring shares, and all XCDs have some
+  p.workers = min(a.workers, p.total);
+  const int each = (p.workers + 7) >> 3, i = (int)(blockIdx.x >> 3);
+  p.w = (int)(blockIdx.x & 7) * each + i;
+  if (i >= each || p.w >= p.workers) {
+    p.w = p.workers + 1;  // (without a share)
+    p.u0 = p.u1 = p.total;
+    return p;
+  }
+  const Shares shares(p.total, p.workers);
+  p.u0 = shares.start(p.w);
+  p.u1 = shares.start(p.w + 1);
+  p.b = batch;  // (found below, unless what is read changes meanwhile)
+  p.before = 0;
+  for (int base = 0; base < batch; base += 64) {
+    if (base) sum = upto(n = units(base + lane));
+    const int at = __popcll(__ballot(p.before + sum <= p.u0));  // sequences that end before u0
     if (at < 64) {
       p.b = base + at;
-      p.before += __builtin_amdgcn_readlane(upto - n, at);
+      p.before += __builtin_amdgcn_readlane(sum - n, at);
       break;
     }
-    p.before += __builtin_amdgcn_readlane(upto, 63);
+    p.before += __builtin_amdgcn_readlane(sum, 63);
   }
-  p.b = __builtin_amdgcn_readfirstlane(p.b);
-  p.before = __builtin_amdgcn_readfirstlane(p.before);
   return p;
 }
 
@@ -136,15 +148,17 @@ struct Block {  // 32 tokens in a lane
 // Block of 32 tokens, the `at`th of its page, of head `head` of all pages' heads.  (One base for
 // the wave and a lane's own 32-bit offset: addresses take no registers but that.)
 template <int D>
-__device__ __forceinline__ void load_keys(Block<D>& x, const Cache4& c, int64_t head, int at, uint32_t l, uint32_t g) {
+__device__ __forceinline__ void load_keys(Block<D>& x, const Cache4& c, int64_t head, int at, uint32_t l, uint32_t g,
+                                          int one = -1) {  // one: of its halves alone, as the first
   constexpr uint32_t W = D / 32;
-  const int64_t tok = (head << c.log_page) + at * 32;
+  const int64_t tok = (head << c.log_page) + at * 32 + max(one, 0) * 16;
   const uint8_t* k = c.k + (tok * D >> 1);
   const uint8_t* ks = c.ks + tok * W;
   const uint32_t kl = D == 64 ? (g >> 1) * 256 + l * 16 + (g & 1) * 8 : g * (2 * D) + l * 16;
   const uint32_t sl = l * W + (D == 64 ? g >> 1 : D == 128 ? g : 2 * g);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
+    if (t && one >= 0) break;
     if constexpr (D == 64) {
       *reinterpret_cast<uint2*>(x.k[t]) = *reinterpret_cast<const uint2*>(k + t * (8 * D) + kl);
       x.ks[t] = (ks + t * (16 * W))[sl];
@@ -208,6 +222,87 @@ __device__ __forceinline__ void add_values(f32x4_t (&o)[NC][D / 16], const uint3
   }
 }
 
+// Operands of the values whose pair number P is of this parity, into LDS.
+template <int D, int P>
+__device__ __forceinline__ void widen_values(unsigned char* to, const uint32_t* v, const float* s) {
+  if constexpr (P < D / 32) {
+    uint4 even, odd;
+    values_pair<D, P>(v, s, even, odd);
+    *reinterpret_cast<uint4*>(to + 2 * P * 1024) = even;
+    *reinterpret_cast<uint4*>(to + (2 * P + 1) * 1024) = odd;
+    widen_values<D, P + 2>(to, v, s);
+  }
+}
+
+// Scores of tokens that a column does not see, of a block whose first one of this lane is t0.
+template <int NC>
+__device__ __forceinline__ void hide_tokens(f32x4_t (&sc)[2][NC], int t0, const int* pos, int window) {
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int from = window ? pos[c] - window : INT_MIN;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int tok = t0 + t * 16 + j;
+        if (tok > pos[c] || tok <= from) sc[t][c][j] = kNegInf;
+      }
+  }
+}
+
+// A column's scores of 32 tokens, eight in a lane: whether its reference m falls behind by more than
+// kAhead somewhere in the wave; the reference that it gets then, with the factor for what was summed
+// up under the old one; and the weights, to bf16.
+__device__ __forceinline__ float largest(const f32x4_t s0, const f32x4_t s1, float scale) {
+  return scale * fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+}
+__device__ __forceinline__ bool rises(const f32x4_t s0, const f32x4_t s1, float scale, float m) {
+  return __ballot(largest(s0, s1, scale) > m + kAhead) != 0;
+}
+__device__ __forceinline__ float raise(const f32x4_t s0, const f32x4_t s1, float scale, float& m, float& off) {
+  const float now = fmaxf(m, max_of_columns(largest(s0, s1, scale)));
+  const float shrink = now == m ? 1.f : __builtin_amdgcn_exp2f(m - now);
+  m = now;
+  off = now == kNegInf ? 0.f : -now;
+  return shrink;
+}
+__device__ __forceinline__ bf16x8_t weights(const f32x4_t s0, const f32x4_t s1, float scale, float off) {
+  const auto pair = [&](float x, float y) {
+    return bf16_pair(__builtin_amdgcn_exp2f(__builtin_fmaf(x, scale, off)), __builtin_amdgcn_exp2f(__builtin_fmaf(y, scale, off)));
+  };
+  return __builtin_bit_cast(bf16x8_t, make_uint4(pair(s0[0], s0[1]), pair(s0[2], s0[3]), pair(s1[0], s1[1]), pair(s1[2], s1[3])));
+}
+
+// Columns that see a token of a block whose values are NaN (scale byte 255 in vs) have NaN there: such a
+// token counts 1 for the values of this lane, a token that a column sees 1 for it.
+template <int NC, int NT>
+__device__ __forceinline__ void mark_lost(f32x4_t (&o)[NC][NT], const uint32_t* vs, int t0, const int* pos, int window) {
+  uint32_t na[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t pair = vs[j >> 1] >> (16 * (j & 1));
+    na[j] = ((pair & 255u) == 255u ? 0x3f80u : 0u) | ((pair >> 8 & 255u) == 255u ? 0x3f800000u : 0u);
+  }
+  const bf16x8_t nan_at = __builtin_bit_cast(bf16x8_t, make_uint4(na[0], na[1], na[2], na[3]));
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    uint32_t se[4];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int tok = t0 + (j >> 2) * 16 + (j & 3);
+      const bool sees = tok <= pos[c] && (!window || tok > pos[c] - window);
+      const uint32_t one = sees ? 0x3f80u << (16 * (j & 1)) : 0u;
+      se[j >> 1] = j & 1 ? se[j >> 1] | one : one;
+    }
+    const f32x4_t hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+        nan_at, __builtin_bit_cast(bf16x8_t, make_uint4(se[0], se[1], se[2], se[3])), f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[c][n][j] = hit[j] > 0.f ? NAN : o[c][n][j];
+  }
+}
+
 }  // namespace
 
 // Workgroups per CU, which are waves per SIMD: as many as registers allow without spilling.
@@ -220,9 +315,11 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
   __shared__ float part_m[4][16], part_l[4][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l = lane & 15, g = lane >> 4;
-  // an XCD's workgroups have neighbouring shares
-  const int w = (int)(blockIdx.x & 7) * (a.workers >> 3) + (int)(blockIdx.x >> 3);
-  const Place place = find_place<COLS>(a, w);
+  const Place place = find_place<COLS>(a);
+  // (the records that belong to no share)
+  if (tid == 0 && (int)blockIdx.x >= place.workers) a.shared()[blockIdx.x] = Shared{};
+  if (place.u0 >= place.u1) return;
+  const int w = place.w;
   const uint4 ones4 = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
   const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, ones4);
 
@@ -316,18 +413,7 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
       __builtin_amdgcn_sched_barrier(0);
       if (more) load_keys<D>(x, a.c, next, (blk + 4) & in_page, l, g);
       if (at_edge(blk)) {
-        int from[NC];
-#pragma unroll
-        for (int c = 0; c < NC; ++c) from[c] = a.window ? pos[c] - a.window : INT_MIN;
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int tok = blk * 32 + t * 16 + g * 4 + j;
-              if (tok > pos[c] || tok <= from[c]) sc[t][c][j] = kNegInf;
-            }
+        hide_tokens<NC>(sc, blk * 32 + g * 4, pos, a.window);
         if (__ballot((any_byte_255(x.vs[0]) | any_byte_255(x.vs[1])) != 0)) {
           lost = true;  // (seen to behind the loop)
           x.vs[0] = without_255(x.vs[0]);
@@ -337,26 +423,13 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
       bf16x8_t p[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        float big = fmaxf(fmaxf(fmaxf(sc[0][c][0], sc[0][c][1]), fmaxf(sc[0][c][2], sc[0][c][3])),
-                          fmaxf(fmaxf(sc[1][c][0], sc[1][c][1]), fmaxf(sc[1][c][2], sc[1][c][3])));
-        big *= a.scale;
-        if (__ballot(big > m[c] + kAhead)) {
-          const float now = fmaxf(m[c], max_of_columns(big));
-          const float shrink = now == m[c] ? 1.f : __builtin_amdgcn_exp2f(m[c] - now);
-          m[c] = now;
-          off[c] = now == kNegInf ? 0.f : -now;
+        if (rises(sc[0][c], sc[1][c], a.scale, m[c])) {
+          const float shrink = raise(sc[0][c], sc[1][c], a.scale, m[c], off[c]);
           sum[c] *= shrink;
 #pragma unroll
           for (int n = 0; n < NT; ++n) o[c][n] *= shrink;
         }
-        uint32_t pk[4];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int j = 0; j < 4; j += 2)
-            pk[t * 2 + (j >> 1)] = bf16_pair(__builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][c][j], a.scale, off[c])),
-                                             __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][c][j + 1], a.scale, off[c])));
-        p[c] = __builtin_bit_cast(bf16x8_t, make_uint4(pk[0], pk[1], pk[2], pk[3]));
+        p[c] = weights(sc[0][c], sc[1][c], a.scale, off[c]);
         sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[c], sum[c], 0, 0, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -368,45 +441,18 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
       next = after;
     }
     if (lost) {
-      // Columns that see a token whose block is NaN have NaN there: such a token counts 1 for the
-      // values of this lane, a token that a column sees 1 for it.
-      for (int at = blk0; at < blk_end; at += 4) {
-        if (!at_edge(at)) continue;
-        load_values<D>(x, a.c, head_of(at), at & in_page, l, g);
-        uint32_t na[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t pair = x.vs[j >> 1] >> (16 * (j & 1));
-          na[j] = ((pair & 255u) == 255u ? 0x3f80u : 0u) | ((pair >> 8 & 255u) == 255u ? 0x3f800000u : 0u);
+      for (int at = blk0; at < blk_end; at += 4)
+        if (at_edge(at)) {
+          load_values<D>(x, a.c, head_of(at), at & in_page, l, g);
+          mark_lost<NC, NT>(o, x.vs, at * 32 + g * 4, pos, a.window);
         }
-        const bf16x8_t nan_at = __builtin_bit_cast(bf16x8_t, make_uint4(na[0], na[1], na[2], na[3]));
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          uint32_t se[4];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int tok = at * 32 + (j >> 2) * 16 + g * 4 + (j & 3);
-            const bool sees = tok <= pos[c] && (!a.window || tok > pos[c] - a.window);
-            const uint32_t one = sees ? 0x3f80u << (16 * (j & 1)) : 0u;
-            se[j >> 1] = j & 1 ? se[j >> 1] | one : one;
-          }
-          const f32x4_t hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              nan_at, __builtin_bit_cast(bf16x8_t, make_uint4(se[0], se[1], se[2], se[3])), f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[c][n][j] = hit[j] > 0.f ? NAN : o[c][n][j];
-        }
-      }
     }
 
     // The four waves' sums, 16 columns at a time.
     const bool whole = start == 0 && end == q.nb;
     float* slot = a.parts + (int64_t)(2 * w + (start == 0)) * (COLS * (D + 2));
     if (start == 0 && !whole) {
-      // its last workgroup is the last one whose share starts at or before its last unit
-      const int64_t behind = (int64_t)u - end + q.nb;
-      shared = Shared{(int)((behind * a.workers - 1) / place.total), place.total, h, tile, cols, q.s.row0, q.s.len - q.s.n, 0};
+      shared = Shared{Shares(place.total, place.workers).of(u - end + q.nb - 1), place.total, h, tile, cols, q.s.row0, q.s.len - q.s.n, 0};
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -456,19 +502,229 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
   if (tid == 0) a.shared()[w] = shared;
 }
 
-// The parts of a tile, joined: workgroup (w, y) has columns y 256 / D .. of the tile that
-// begins in w's share and goes on behind it, if there is one.  A lane has four values of a
-// column; the eight waves take every eighth part, four at a time, and are joined in LDS.
-template <int D, int NC>
+// Many columns: 128 of them in a workgroup, 32 in a wave.  64 tokens at a time are widened once
+// for all four waves, each a quarter, into LDS, in the order of MFMA operands, while the 64 before are
+// used; the codes of those behind are on their way meanwhile.  A wave keeps its columns to the
+// end: nothing is joined in LDS.
+template <int D>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(const Attend4Args a) {
+  constexpr int NC = 2, WCOLS = 16 * NC, COLS = 4 * WCOLS, STEPS = D / 32, NT = D / 16;
+  constexpr int kKeys = 4 * STEPS * 1024, kBuffer = kKeys + 2 * NT * 1024;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * kBuffer];
+  __shared__ int any_lost;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l = lane & 15, g = lane >> 4;
+  const Place place = find_place<COLS>(a);
+  // (the records that belong to no share)
+  if (tid == 0 && (int)blockIdx.x >= place.workers) a.shared()[blockIdx.x] = Shared{};
+  if (place.u0 >= place.u1) return;
+  const int w = place.w;
+  const uint4 ones4 = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+  const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, ones4);
+
+  Shared shared{};  // the tile that begins here and goes on behind
+  int u = place.u0, b = place.b, before = place.before;
+  while (u < place.u1 && b < a.s.batch) {
+    const SeqUnits q = seq_units<COLS>(a, b);
+    const int seq_total = q.units(a.c.heads);
+    if (u - before >= seq_total) {
+      before += seq_total;
+      ++b;
+      continue;
+    }
+    const int item = (u - before) / q.nb, start = u - before - item * q.nb;
+    const int end = min(q.nb, start + place.u1 - u);
+    const int h = item / q.ct, tile = item - h * q.ct;
+    u += end - start;
+
+    const int cols = (int)min((int64_t)COLS, (int64_t)q.s.n * a.group - (int64_t)tile * COLS);  // at least one
+    const int lag = q.s.len - q.s.n;  // a row's token: lag + row
+    const int pos0 = lag + tile * COLS / a.group, pos1 = lag + (tile * COLS + cols - 1) / a.group;
+    // this wave's columns, and the tokens of its first and last one
+    const int mine = min(max(cols - wave * WCOLS, 0), WCOLS), col0 = tile * COLS + wave * WCOLS;
+    const int wpos0 = lag + col0 / a.group, wpos1 = mine ? lag + (col0 + mine - 1) / a.group : INT_MIN;
+    bf16x8_t qv[NC][STEPS];
+    int pos[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int col = min(col0 + c * 16 + l, tile * COLS + cols - 1), r = col / a.group, head = col - r * a.group;
+      pos[c] = lag + r;
+      const uint16_t* at = a.q + (int64_t)(q.s.row0 + r) * a.q_row + (int64_t)(h * a.group + head) * a.q_head + g * (D / 4);
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) __builtin_memcpy(&qv[c][s], at + s * 8, 16);
+    }
+    f32x4_t o[NC][NT], sum[NC];
+    float m[NC], off[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) o[c][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      sum[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      m[c] = kNegInf;
+      off[c] = 0.f;
+    }
+
+    // steps of 64 tokens that any column of the tile sees; blocks of 32 that the sequence has
+    int st = (q.first + start) * 2, st_end = min((q.first + end) * 2, (pos1 + 64) >> 6);
+    if (a.window) st = max(st, max(0, pos0 - a.window + 1) >> 6);
+    const int st0 = st, last_block = (q.s.len - 1) >> 5;
+    const int pages32 = a.c.log_page - 5, in_page = (1 << pages32) - 1;
+    const auto block_of = [&](int at) { return min(at * 2 + (wave >> 1), last_block); };  // this wave's half of a step
+    const auto head_of = [&](int at) {
+      const int page = __builtin_amdgcn_readfirstlane(seq_page(a.s, a.c.n_pages, b, block_of(at) >> pages32));
+      return (int64_t)page * a.c.heads + h;
+    };
+    const auto at_edge = [&](int at) {  // some column of the tile does not see all of its tokens
+      return at * 64 + 63 > pos0 || (a.window && at * 64 <= pos1 - a.window);
+    };
+    Block<D> x;  // (of the keys, 16 tokens)
+    const auto load = [&](int at, int64_t head) {
+      const int blk = block_of(at) & in_page;
+      load_keys<D>(x, a.c, head, blk, l, g, wave & 1);
+      load_values<D>(x, a.c, head, blk, l, g);
+    };
+    // The codes at hand into a buffer.
+    const auto widen = [&](unsigned char* to, int at) {
+#pragma unroll
+      for (int s = 0; s < STEPS; ++s) {
+        const float f = mx4_scale(D == 256 ? (s < 4 ? x.ks[0] & 255u : x.ks[0] >> 8) : x.ks[0]);
+        *reinterpret_cast<uint4*>(to + (wave * STEPS + s) * 1024 + lane * 16) = mx4_bf16x8(x.k[0][s], f);
+      }
+      if (at_edge(at) && __ballot((any_byte_255(x.vs[0]) | any_byte_255(x.vs[1])) != 0)) {
+        any_lost = 1;  // (seen to behind the loop)
+        x.vs[0] = without_255(x.vs[0]);
+        x.vs[1] = without_255(x.vs[1]);
+      }
+      float fs[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) fs[j] = mx4_scale(x.vs[j >> 2] >> (8 * (j & 3)) & 255u);
+      unsigned char* v = to + kKeys + (wave >> 1) * (NT * 1024) + lane * 16;
+      if (wave & 1)
+        widen_values<D, 1>(v, x.v, fs);
+      else
+        widen_values<D, 0>(v, x.v, fs);
+    };
+    __syncthreads();  // (the tile before has been read)
+    if (tid == 0) any_lost = 0;
+    if (st < st_end) {
+      load(st, head_of(st));
+      int64_t next = st + 1 < st_end ? head_of(st + 1) : 0;
+      __syncthreads();
+      widen(smem, st);
+      if (st + 1 < st_end) {
+        load(st + 1, next);
+        if (st + 2 < st_end) next = head_of(st + 2);
+      }
+      __syncthreads();
+      for (int i = 0; st < st_end; ++st, i ^= 1) {
+        const unsigned char* from = smem + i * kBuffer;
+        if (st + 1 < st_end) {
+          widen(smem + (i ^ 1) * kBuffer, st + 1);
+          if (st + 2 < st_end) load(st + 2, next);
+          if (st + 3 < st_end) next = head_of(st + 3);
+        }
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          const int t0 = st * 64 + half * 32;
+          if (t0 > wpos1 || (a.window && t0 + 31 <= wpos0 - a.window)) continue;  // nothing that this wave's columns see
+          f32x4_t sc[2][NC];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) sc[t][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+              const bf16x8_t kv = *reinterpret_cast<const bf16x8_t*>(from + ((half * 2 + t) * STEPS + s) * 1024 + lane * 16);
+#pragma unroll
+              for (int c = 0; c < NC; ++c) sc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, qv[c][s], sc[t][c], 0, 0, 0);
+            }
+          }
+          if (t0 + 31 > wpos0 || (a.window && t0 <= wpos1 - a.window)) hide_tokens<NC>(sc, t0 + g * 4, pos, a.window);
+          bf16x8_t p[NC];
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            if (rises(sc[0][c], sc[1][c], a.scale, m[c])) {
+              const float shrink = raise(sc[0][c], sc[1][c], a.scale, m[c], off[c]);
+              sum[c] *= shrink;
+#pragma unroll
+              for (int n = 0; n < NT; ++n) o[c][n] *= shrink;
+            }
+            p[c] = weights(sc[0][c], sc[1][c], a.scale, off[c]);
+            sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[c], sum[c], 0, 0, 0);
+          }
+          const unsigned char* vals = from + kKeys + half * (NT * 1024) + lane * 16;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            const bf16x8_t vv = *reinterpret_cast<const bf16x8_t*>(vals + n * 1024);
+#pragma unroll
+            for (int c = 0; c < NC; ++c) o[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[c], o[c][n], 0, 0, 0);
+          }
+        }
+        __syncthreads();
+      }
+      if (any_lost) {
+        for (int at = st0 * 2; at < st_end * 2 && at <= last_block; ++at)
+          if (at_edge(at >> 1)) {
+            const int page = __builtin_amdgcn_readfirstlane(seq_page(a.s, a.c.n_pages, b, at >> pages32));
+            load_values<D>(x, a.c, (int64_t)page * a.c.heads + h, at & in_page, l, g);
+            mark_lost<NC, NT>(o, x.vs, at * 32 + g * 4, pos, a.window);
+          }
+      }
+    }
+
+    const bool whole = start == 0 && end == q.nb;
+    float* slot = a.parts + (int64_t)(2 * w + (start == 0)) * (COLS * (D + 2));
+    if (start == 0 && !whole)
+      shared = Shared{Shares(place.total, place.workers).of(u - end + q.nb - 1), place.total, h, tile, cols, q.s.row0, lag, 0};
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int col = wave * WCOLS + c * 16 + l;
+      if (col >= cols) continue;
+      const int at = tile * COLS + col, r = at / a.group, head = h * a.group + at - r * a.group;
+      const int64_t row = q.s.row0 + r;
+      const bool empty = lag + r < 0;
+      const float inv = 1.f / sum[c][0];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int d = (4 * g + j) * NT;
+#pragma unroll
+        for (int n = 0; n < NT; n += 4) {
+          const float4 v = make_float4(o[c][n][j], o[c][n + 1][j], o[c][n + 2][j], o[c][n + 3][j]);
+          if (whole)
+            store4(a.out, kBF16, row * a.o_row + head * a.o_head + d + n, 4,
+                   empty ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+          else
+            *reinterpret_cast<float4*>(slot + col * D + d + n) = v;
+        }
+      }
+      if (g == 0) {
+        if (!whole) {
+          slot[COLS * D + col] = m[c];
+          slot[COLS * D + COLS + col] = sum[c][0];
+        } else if (a.lse) {
+          a.lse[row * ((int64_t)a.c.heads * a.group) + head] = empty ? kNegInf : lse_of(m[c], sum[c][0]);
+        }
+      }
+    }
+  }
+  if (tid == 0) a.shared()[w] = shared;
+}
+
+// The parts of a tile, joined: workgroup (w, y) does that for the tile that begins in w's share and
+// goes on behind it, if there is one.  A lane has four values of a column, a wave 256 / D
+// columns.  SPLIT (few columns, perhaps many parts): the eight waves have the same columns and every eighth
+// part each, and are joined in LDS; else each has columns of its own.
+template <int D, int COLS, bool SPLIT>
 __global__ __launch_bounds__(512) void attend4_join_kernel(const Attend4Args a) {
-  constexpr int COLS = 16 * NC, SLOT = COLS * (D + 2), LANES = D / 4;
+  constexpr int SLOT = COLS * (D + 2), LANES = D / 4, PER = 64 / LANES, STEP = SPLIT ? 8 : 1;
   __shared__ float4 part_v[8][64];
   __shared__ float part_m[8][64], part_l[8][64];
   const int w = blockIdx.x, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Shared t = a.shared()[w];
   const int n = t.last - w + 1;  // workgroups that have a part
-  const int col = blockIdx.y * (64 / LANES) + lane / LANES, d = lane % LANES * 4;
-  if (n <= 1 || (int)blockIdx.y * (64 / LANES) >= t.cols) return;
+  const int first = (SPLIT ? blockIdx.y : blockIdx.y * 8 + wave) * PER;
+  if (n <= 1 || first >= t.cols) return;
+  const int col = first + lane / LANES, d = lane % LANES * 4;
   const bool real = col < t.cols;
   const float* at = a.parts + (int64_t)(2 * w) * SLOT;
   float top = kNegInf, ls = 0.f;
@@ -480,17 +736,16 @@ __global__ __launch_bounds__(512) void attend4_join_kernel(const Attend4Args a) 
     ls = ls * f0 + l * f1;
     top = now;
   };
-  for (int i = wave; i < n; i += 32) {
+  for (int i = SPLIT ? wave : 0; i < n; i += 4 * STEP) {
     float m[4], l[4];
     float4 v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int p = i + 8 * j;
+      const int p = i + STEP * j;
       m[j] = kNegInf;
       l[j] = 0.f;
       v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-      // (where there are fewer units than workgroups, some have none)
-      if (real && p < n && share_start(t.total, a.workers, w + p) < share_start(t.total, a.workers, w + p + 1)) {
+      if (real && p < n) {
         const float* slot = at + (int64_t)(p ? 2 * p : 1) * SLOT;
         m[j] = slot[COLS * D + col];
         l[j] = slot[COLS * D + COLS + col];
@@ -500,13 +755,16 @@ __global__ __launch_bounds__(512) void attend4_join_kernel(const Attend4Args a) 
 #pragma unroll
     for (int j = 0; j < 4; ++j) add(m[j], l[j], v[j]);
   }
-  part_v[wave][lane] = s;
-  part_m[wave][lane] = top;
-  part_l[wave][lane] = ls;
-  __syncthreads();
-  if (wave || !real) return;
+  if constexpr (SPLIT) {
+    part_v[wave][lane] = s;
+    part_m[wave][lane] = top;
+    part_l[wave][lane] = ls;
+    __syncthreads();
+    if (wave) return;
 #pragma unroll
-  for (int i = 1; i < 8; ++i) add(part_m[i][lane], part_l[i][lane], part_v[i][lane]);
+    for (int i = 1; i < 8; ++i) add(part_m[i][lane], part_l[i][lane], part_v[i][lane]);
+  }
+  if (!real) return;
   const int c = t.tile * COLS + col, r = c / a.group, head = t.head * a.group + c - r * a.group;
   const int64_t row = t.row0 + r;
   const bool empty = t.pos0 + r < 0;
@@ -519,32 +777,42 @@ __global__ __launch_bounds__(512) void attend4_join_kernel(const Attend4Args a) 
 Attend4Plan attend4_plan(int batch, int total, int heads, int group, int d, int64_t max_len, int ncu) {
   Attend4Plan p{};
   const int64_t cols = ((int64_t)total + batch - 1) / std::max(batch, 1) * group;  // of a sequence, on average
-  p.nc = cols <= 16 ? 1 : 2;
+  p.nc = cols <= 16 ? 1 : cols <= 32 ? 2 : kAttendWide;
   const int64_t most = (int64_t)heads * ((int64_t)total * group / (16 * p.nc) + batch) * std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit);
-  p.workers = (int)std::min<int64_t>((most + 7) / 8 * 8, (int64_t)ncu * attend_per_cu(d, p.nc));
+  const int per_cu = p.nc < kAttendWide ? attend_per_cu(d, p.nc) : d == 256 ? 1 : 2;
+  p.workers = (int)std::min<int64_t>((most + 7) / 8 * 8, (int64_t)ncu * per_cu);
   p.bytes = (int64_t)p.workers * (2 * (16 * p.nc) * (d + 2) * 4 + (int64_t)sizeof(Attend4Args::Shared));
   return p;
 }
 
 template <int D, int NC>
 static hipError_t attend_launch(const Attend4Args& a, hipStream_t s) {
-  attend4_kernel<D, NC><<<a.workers, 256, 0, s>>>(a);
+  constexpr bool WIDE = NC == kAttendWide;
+  if constexpr (WIDE) {
+    attend4_wide_kernel<D><<<a.workers, 256, 0, s>>>(a);
+  } else {
+    attend4_kernel<D, NC><<<a.workers, 256, 0, s>>>(a);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // (a tile's columns, as many as there can be)
   const int64_t cols = a.s.rows ? 16 * NC : std::min<int64_t>(16 * NC, (int64_t)a.s.n * a.group);
-  attend4_join_kernel<D, NC><<<dim3(a.workers, (unsigned)((cols * D + 255) / 256)), 512, 0, s>>>(a);
+  const int64_t waves = (cols * D + 255) / 256;
+  attend4_join_kernel<D, 16 * NC, !WIDE><<<dim3(a.workers, (unsigned)(WIDE ? (waves + 7) / 8 : waves)), 512, 0, s>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_attend4(const Attend4Args& a, hipStream_t s) {
-  switch (a.c.d * 8 + a.nc) {
+  switch (a.c.d * 8 + (a.nc == kAttendWide ? 3 : a.nc)) {
     case 64 * 8 + 1: return attend_launch<64, 1>(a, s);
     case 64 * 8 + 2: return attend_launch<64, 2>(a, s);
+    case 64 * 8 + 3: return attend_launch<64, kAttendWide>(a, s);
     case 128 * 8 + 1: return attend_launch<128, 1>(a, s);
     case 128 * 8 + 2: return attend_launch<128, 2>(a, s);
+    case 128 * 8 + 3: return attend_launch<128, kAttendWide>(a, s);
     case 256 * 8 + 1: return attend_launch<256, 1>(a, s);
-    default: return attend_launch<256, 2>(a, s);
+    case 256 * 8 + 2: return attend_launch<256, 2>(a, s);
+    default: return attend_launch<256, kAttendWide>(a, s);
   }
 }
 
