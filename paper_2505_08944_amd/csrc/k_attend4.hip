@@ -33,9 +33,9 @@ using Shared = Attend4Args::Shared;
 constexpr int kUnit = 128;  // tokens
 constexpr int kAttendWide = 8;  // columns in 16s of the kernel for many
 constexpr float kNegInf = -INFINITY;
-// A column's reference follows its largest score (in powers of two) only when that is this
-// much ahead: most blocks then change nothing, and p stays below 2^8.
-constexpr float kAhead = 8.f;
+// A column's reference is its largest score (in powers of two) and this much more when it is set, and
+// holds until a weight reaches 2: few blocks change it, and no maximum is needed to see that.
+constexpr float kAhead = 6.f;
 
 // A sequence's units: tiles of columns for each head, units of tokens for each tile.
 struct SeqUnits {
@@ -250,27 +250,25 @@ __device__ __forceinline__ void hide_tokens(f32x4_t (&sc)[2][NC], int t0, const 
   }
 }
 
-// A column's scores of 32 tokens, eight in a lane: whether its reference m falls behind by more than
-// kAhead somewhere in the wave; the reference that it gets then, with the factor for what was summed
-// up under the old one; and the weights, to bf16.
-__device__ __forceinline__ float largest(const f32x4_t s0, const f32x4_t s1, float scale) {
-  return scale * fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-}
-__device__ __forceinline__ bool rises(const f32x4_t s0, const f32x4_t s1, float scale, float m) {
-  return __ballot(largest(s0, s1, scale) > m + kAhead) != 0;
-}
-__device__ __forceinline__ float raise(const f32x4_t s0, const f32x4_t s1, float scale, float& m, float& off) {
-  const float now = fmaxf(m, max_of_columns(largest(s0, s1, scale)));
-  const float shrink = now == m ? 1.f : __builtin_amdgcn_exp2f(m - now);
-  m = now;
-  off = now == kNegInf ? 0.f : -now;
-  return shrink;
-}
-__device__ __forceinline__ bf16x8_t weights(const f32x4_t s0, const f32x4_t s1, float scale, float off) {
+// A column's weights of 32 tokens, eight in a lane, to bf16.
+__device__ __forceinline__ uint4 weights(const f32x4_t s0, const f32x4_t s1, float scale, float off) {
   const auto pair = [&](float x, float y) {
     return bf16_pair(__builtin_amdgcn_exp2f(__builtin_fmaf(x, scale, off)), __builtin_amdgcn_exp2f(__builtin_fmaf(y, scale, off)));
   };
-  return __builtin_bit_cast(bf16x8_t, make_uint4(pair(s0[0], s0[1]), pair(s0[2], s0[3]), pair(s1[0], s1[1]), pair(s1[2], s1[3])));
+  return make_uint4(pair(s0[0], s0[1]), pair(s0[2], s0[3]), pair(s1[0], s1[1]), pair(s1[2], s1[3]));
+}
+// Whether a column of the wave has no reference yet, or one that is too far behind: a weight of 2 or more has
+// bit 14 set, and no other has (a NaN has too).
+__device__ __forceinline__ bool behind(const uint4 p, float m) {
+  return __ballot(((p.x | p.y | p.z | p.w) & 0x40004000u) != 0 || m == kNegInf) != 0;
+}
+// The reference that a column gets then, with the factor for what was summed up under the old one.
+__device__ __forceinline__ float raise(const f32x4_t s0, const f32x4_t s1, float scale, float& m, float& off) {
+  const float big = scale * fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+  const float now = fmaxf(m, max_of_columns(big) + kAhead), shrink = now == m ? 1.f : __builtin_amdgcn_exp2f(m - now);
+  m = now;
+  off = now == kNegInf ? 0.f : -now;
+  return shrink;
 }
 
 // Columns that see a token of a block whose values are NaN (scale byte 255 in vs) have NaN there: such a
@@ -423,13 +421,15 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
       bf16x8_t p[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        if (rises(sc[0][c], sc[1][c], a.scale, m[c])) {
+        uint4 pw = weights(sc[0][c], sc[1][c], a.scale, off[c]);
+        if (behind(pw, m[c])) {
           const float shrink = raise(sc[0][c], sc[1][c], a.scale, m[c], off[c]);
           sum[c] *= shrink;
 #pragma unroll
           for (int n = 0; n < NT; ++n) o[c][n] *= shrink;
+          pw = weights(sc[0][c], sc[1][c], a.scale, off[c]);
         }
-        p[c] = weights(sc[0][c], sc[1][c], a.scale, off[c]);
+        p[c] = __builtin_bit_cast(bf16x8_t, pw);
         sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[c], sum[c], 0, 0, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -617,7 +617,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
       }
       __syncthreads();
       for (int i = 0; st < st_end; ++st, i ^= 1) {
-        const unsigned char* from = smem + i * kBuffer;
+        const unsigned char* from = smem + i * kBuffer + lane * 16;
         if (st + 1 < st_end) {
           widen(smem + (i ^ 1) * kBuffer, st + 1);
           if (st + 2 < st_end) load(st + 2, next);
@@ -628,34 +628,57 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
           const int t0 = st * 64 + half * 32;
           if (t0 > wpos1 || (a.window && t0 + 31 <= wpos0 - a.window)) continue;  // nothing that this wave's columns see
           f32x4_t sc[2][NC];
+          const unsigned char* keys = from + half * (2 * STEPS * 1024);
+          // (all of them requested at once: a wait between reads and MFMAs in turn costs each its latency)
+          constexpr int AT_ONCE = STEPS < 8 ? 2 : 1;
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
+          for (int tt = 0; tt < 2; tt += AT_ONCE) {
+            bf16x8_t kb[AT_ONCE][STEPS];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) sc[t][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < AT_ONCE; ++t)
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-              const bf16x8_t kv = *reinterpret_cast<const bf16x8_t*>(from + ((half * 2 + t) * STEPS + s) * 1024 + lane * 16);
+              for (int s = 0; s < STEPS; ++s) kb[t][s] = *reinterpret_cast<const bf16x8_t*>(keys + ((tt + t) * STEPS + s) * 1024);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-              for (int c = 0; c < NC; ++c) sc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kv, qv[c][s], sc[t][c], 0, 0, 0);
-            }
+            for (int t = 0; t < AT_ONCE; ++t)
+#pragma unroll
+              for (int c = 0; c < NC; ++c) sc[tt + t][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+              for (int t = 0; t < AT_ONCE; ++t)
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+                  sc[tt + t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kb[t][s], qv[c][s], sc[tt + t][c], 0, 0, 0);
           }
-          if (t0 + 31 > wpos0 || (a.window && t0 <= wpos1 - a.window)) hide_tokens<NC>(sc, t0 + g * 4, pos, a.window);
+          // (the first values are on their way while the weights are made)
+          constexpr int EARLY = NT < 8 ? NT : 8;
+          bf16x8_t vb[EARLY];
+          const unsigned char* vals = from + kKeys + half * (NT * 1024);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int n = 0; n < EARLY; ++n) vb[n] = *reinterpret_cast<const bf16x8_t*>(vals + n * 1024);
+          __builtin_amdgcn_sched_barrier(0);
+          if (t0 + 31 > wpos0 || (a.window && t0 <= wpos1 - a.window)) {
+            hide_tokens<NC>(sc, t0 + g * 4, pos, a.window);
+          }
           bf16x8_t p[NC];
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
-            if (rises(sc[0][c], sc[1][c], a.scale, m[c])) {
+            uint4 pw = weights(sc[0][c], sc[1][c], a.scale, off[c]);
+            if (behind(pw, m[c])) {
               const float shrink = raise(sc[0][c], sc[1][c], a.scale, m[c], off[c]);
               sum[c] *= shrink;
 #pragma unroll
               for (int n = 0; n < NT; ++n) o[c][n] *= shrink;
+              pw = weights(sc[0][c], sc[1][c], a.scale, off[c]);
             }
-            p[c] = weights(sc[0][c], sc[1][c], a.scale, off[c]);
+            p[c] = __builtin_bit_cast(bf16x8_t, pw);
             sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[c], sum[c], 0, 0, 0);
           }
-          const unsigned char* vals = from + kKeys + half * (NT * 1024) + lane * 16;
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            const bf16x8_t vv = *reinterpret_cast<const bf16x8_t*>(vals + n * 1024);
+            const bf16x8_t vv = n < EARLY ? vb[n < EARLY ? n : 0] : *reinterpret_cast<const bf16x8_t*>(vals + n * 1024);
 #pragma unroll
             for (int c = 0; c < NC; ++c) o[c][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[c], o[c][n], 0, 0, 0);
           }
