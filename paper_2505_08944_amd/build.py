@@ -24,7 +24,7 @@ LIB = os.path.join(PKG, "libaep.so")
 
 SOURCES = ["api.hip", "k_route.hip", "k_rebatch.hip", "k_ffn.hip", "k_combine.hip", "k_pool.hip", "sched.hip",
            "k_router.hip", "k_linear.hip", "k_linear_tiles.hip", "linear_cut.hip", "k_mx4.hip",
-           "k_linear4.hip", "k_cache4.hip", "k_attend4.hip", "ops.hip", "ops4.hip"]
+           "k_linear4.hip", "linear4_cut.hip", "k_cache4.hip", "k_attend4.hip", "ops.hip", "ops4.hip"]
 ARCH = "gfx950"
 CFLAGS = [
     f"--offload-arch={ARCH}", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

@@ -59,9 +59,7 @@ __global__ __launch_bounds__(256) void mx4_quantize_kernel(const T* __restrict__
   uint32_t m = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(v[j]) & 0x7fffffffu);
-  m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xb1, 0xf, 0xf, true));  // lanes 1 0 3 2 of the quad
-  m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4e, 0xf, 0xf, true));  // lanes 2 3 0 1
-  const uint32_t s = mx4_scale_byte(m);
+  const uint32_t s = mx4_scale_byte(quad_max(m));
   const int64_t row_bytes = (k + 1) / 2;
   store_bytes(codes + row * row_bytes + at / 2, mx4_codes(v, mx4_scale(s == kMx4NaN ? 127 : s)), (k - at + 1) >> 1);
   if ((q & 3) == 0) scale[row * ((k + 31) / 32) + (q >> 2)] = (uint8_t)s;

@@ -16,13 +16,15 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scale, int
 hipError_t launch_linear4_pack(const uint8_t* codes, const uint8_t* scale, int n, int k, uint8_t* packed, hipStream_t s);
 hipError_t launch_linear4_unpack(const uint8_t* packed, int n, int k, int k8, uint16_t* out, hipStream_t s);
 
-// The row kernel's tile (k_linear4.hip), and its time in us.
-RowsPlan rows4_plan(int m, int n, int k, int ncu);
+// The tile of the kernels that take the codes as they are (k_linear4.hip; in 16s, 8 x 8: the tile
+// kernel, if tiles_128), and its time in us.
+RowsPlan rows4_plan(int m, int n, int k, bool tiles_128, int ncu);
 hipError_t launch_linear4_rows(const LinearArgs& p, const RowsPlan& r, hipStream_t s);
 
 // Whether the weights are widened to bf16 first, for the tile kernel, and the scratch
 // of that: the weights, x where its rows are not 16-byte aligned, and the tiles' sums.
 struct Linear4Plan {
+  RowsPlan rows;  // (if not)
   bool widen;
   int k8;
   int64_t w_bytes, x_bytes, tile_floats;

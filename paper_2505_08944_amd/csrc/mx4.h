@@ -33,6 +33,12 @@ __device__ __forceinline__ uint32_t mx4_codes(const float* v, float scale) {
   w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
 }
+// The largest of a quad of lanes.
+__device__ __forceinline__ uint32_t quad_max(uint32_t m) {
+  m = max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0xb1, 0xf, 0xf, true));         // lanes 1 0 3 2
+  return max(m, (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x4e, 0xf, 0xf, true));      // lanes 2 3 0 1
+}
+
 // The scale byte of a block whose largest magnitude has these bits: the smallest
 // power of two, from 2^-126 on, at which it is at most 7 (1.75 * 4): no value is then
 // off by more than the power, and for normally distributed values the mean square of

@@ -64,19 +64,23 @@ def test_sizes(M, N, K):
         check(y, x, w, b, r, fn, (M, N, K, fn, out))
 
 
-# products whose weights are widened for the tile kernel: whole tiles, rows left over, K off 8, x off 16 bytes
-WIDE = [(1024, 2048, 2048, 0, 0), (777, 1531, 4096, 0, 0), (600, 2100, 2731, 0, 0), (513, 2048, 2056, 3, 1),
-        (512, 4096, 1000, 0, 0), (2000, 520, 4001, 8, 0)]
+# larger ones, by the kernel that takes them: rows (tiles of all sizes); the tile kernel; weights widened first.  Whole
+# tiles, rows and channels left over, K off 8 and off 128, x off 16 bytes
+LARGE = [(16, 14336, 520, 0, 0), (40, 9000, 640, 0, 0), (64, 8200, 1000, 0, 0), (130, 4096, 1100, 0, 0), (256, 4096, 2048, 0, 0),
+         (100, 14000, 300, 3, 1)]
+TILE = [(777, 4096, 4096, 0, 0), (890, 4090, 4001, 0, 0), (1000, 4090, 4232, 8, 5), (640, 6001, 4100, 3, 0)]
+WIDE = [(2048, 4096, 4096, 0, 0), (4096, 1408, 2048, 0, 0), (2304, 4104, 4001, 3, 1), (2048, 4096, 4104, 0, 5)]
 
 
-@pytest.mark.parametrize("M,N,K,pad,off", WIDE)
+@pytest.mark.parametrize("M,N,K,pad,off", LARGE + TILE + WIDE)
 @pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
-def test_widened(M, N, K, pad, off, out):
+def test_large(M, N, K, pad, off, out):
     log(f"linear4 {M}x{N}x{K} pad {pad} off {off} {out}")
     x, codes, scale, w, b, r = make(M, N, K, "f32", "bf16", seed=M + K, pad=pad, off=off)
-    # (rows enough for the check: a tile's first and last ones, and the last)
     y = aep.Linear4(codes, scale, K, bias=b, activation="silu", out_dtype=out)(x, r)
-    rows = torch.tensor(sorted({0, 1, 63, 64, 127, 128, 255, 256, 300, M // 2, M - 2, M - 1}))
+    assert bool(torch.isfinite(y).all())
+    # (rows enough for the check: a tile's first and last ones, and the last)
+    rows = torch.tensor(sorted({0, 1, 15} | {i for i in (63, 64, 127, 128, 255, 256, 300) if i < M} | {M // 2, M - 2, M - 1}))
     check(y[rows], x[rows], w, b, r[rows], "silu", (M, N, K, pad, off))
 
 
@@ -132,13 +136,13 @@ def test_little_scratch():
     import ctypes
 
     from paper_2505_08944_amd import _lib as L
-    x, codes, scale, w, b, r = make(2048, 2048, 4096, seed=4)
-    lin, y = aep.Linear4(codes, scale, bias=b), torch.empty(2048, 2048, dtype=torch.bfloat16, device="cuda")
-    d = L.Linear4Desc(2048, 2048, 4096, L.AEP_BF16, L.AEP_F32, L.AEP_BF16, 0, 4096, 2048, 2048)
+    x, codes, scale, w, b, r = make(2048, 4096, 4096, seed=4)
+    lin, y = aep.Linear4(codes, scale, bias=b), torch.empty(2048, 4096, dtype=torch.bfloat16, device="cuda")
+    d = L.Linear4Desc(2048, 4096, 4096, L.AEP_BF16, L.AEP_F32, L.AEP_BF16, 0, 4096, 4096, 4096)
     need = ctypes.c_size_t()
     assert L.lib().aep_linear4_workspace(ctypes.byref(d), x.data_ptr(), None, 16, ctypes.byref(need)) == 0
-    assert need.value >= 2 * 2048 * 4096
-    for size in (need.value, need.value - 16, 2 * 2048 * 4096, 2 * 2048 * 4096 - 1, 0):
+    assert need.value >= 2 * 4096 * 4096
+    for size in (need.value, need.value - 16, 2 * 4096 * 4096, 2 * 4096 * 4096 - 1, 0):
         ws = torch.full((max(size, 1),), 255, dtype=torch.uint8, device="cuda")
         assert L.lib().aep_linear4(ctypes.byref(d), x.data_ptr(), lin.packed.data_ptr(), b.data_ptr(), None, y.data_ptr(),
                                    ws.data_ptr() if size else None, size, L.raw_stream(0)) == 0
