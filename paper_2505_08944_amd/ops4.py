@@ -27,24 +27,42 @@ def _bytes_matrix(t, name, dtypes, shape, dev) -> None:
         raise ValueError(f"{name} must be contiguous")
 
 
+_seen = {}  # what was checked of the quantiser's tensors: shapes, strides, types and devices
+
+
+def _checked(key, check) -> None:
+    """Runs check() for what was not checked before."""
+    if key not in _seen:
+        check()
+        if len(_seen) >= 1024:
+            _seen.clear()
+        _seen[key] = True
+
+
 def quantize_mx4(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """x [n, k] float32 or bfloat16 to codes [n, (k + 1) // 2] and scales [n, (k +
     31) // 32], both uint8 (``aep_mx4_quantize``).  Rows may be strided."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise ValueError("x must be a CUDA (HIP) tensor")
-    dev = x.device
-    _rows(x, "x", _F32_BF16, (None, None), dev)
+    dev, dtype = x.device, x.dtype
+
+    def check():
+        _rows(x, "x", _F32_BF16, (None, None), dev)
+        if x.shape[1] < 1:
+            raise ValueError(f"x has shape {tuple(x.shape)}")
+        _int32(x.shape[1], 1 << 30, "columns", "aep_mx4_quantize")
+
+    _checked((x.shape, x.stride(), dtype, dev), check)
     n, k = x.shape
-    if k < 1:
-        raise ValueError(f"x has shape {tuple(x.shape)}")
-    _int32(k, 1 << 30, "columns", "aep_mx4_quantize")
     if dev.index != L.current_device():
         with torch.cuda.device(dev):
             return quantize_mx4(x)
     codes = torch.empty((n, (k + 1) // 2), dtype=torch.uint8, device=dev)
     scale = torch.empty((n, (k + 31) // 32), dtype=torch.uint8, device=dev)
-    L.check(L.lib().aep_mx4_quantize(x.data_ptr(), _CODE[x.dtype], _ld(x), n, k, codes.data_ptr(), scale.data_ptr(),
-                                     L.raw_stream(dev.index)), "aep_mx4_quantize")
+    st = L.lib().aep_mx4_quantize(x.data_ptr(), _CODE[dtype], _ld(x), n, k, codes.data_ptr(), scale.data_ptr(),
+                                  L.raw_stream(dev.index))
+    if st:
+        L.check(st, "aep_mx4_quantize")
     return codes, scale
 
 
@@ -54,23 +72,33 @@ def dequantize_mx4(codes: torch.Tensor, scale: torch.Tensor, k: int, *, dtype: t
     bfloat16 or float32."""
     if not isinstance(codes, torch.Tensor) or not codes.is_cuda:
         raise ValueError("codes must be a CUDA (HIP) tensor")
-    dev, k = codes.device, arg32(k, "k", "aep_mx4_dequantize")
-    if k < 1:
-        raise ValueError(f"k is {k}")
-    _bytes_matrix(codes, "codes", _BYTE[:2], (None, (k + 1) // 2), dev)
+    if not isinstance(scale, torch.Tensor):
+        raise ValueError("scale must be a tensor")
+    dev = codes.device
+
+    def check():
+        k_ = arg32(k, "k", "aep_mx4_dequantize")
+        if k_ < 1:
+            raise ValueError(f"k is {k}")
+        _bytes_matrix(codes, "codes", _BYTE[:2], (None, (k_ + 1) // 2), dev)
+        _bytes_matrix(scale, "scale", (_BYTE[0], _BYTE[2]), (codes.shape[0], (k_ + 31) // 32), dev)
+        if dtype not in _F32_BF16:
+            raise ValueError(f"dtype {dtype}, expected torch.bfloat16 or torch.float32")
+        if out is not None:
+            _rows(out, "out", (dtype,), (codes.shape[0], k_), dev)
+
+    _checked((k, codes.shape, codes.stride(), codes.dtype, dev, scale.shape, scale.stride(), scale.dtype, scale.device,
+              dtype, out is None or (out.shape, out.stride(), out.dtype, out.device)), check)
     n = codes.shape[0]
-    _bytes_matrix(scale, "scale", (_BYTE[0], _BYTE[2]), (n, (k + 31) // 32), dev)
-    if dtype not in _F32_BF16:
-        raise ValueError(f"dtype {dtype}, expected torch.bfloat16 or torch.float32")
-    if out is not None:
-        _rows(out, "out", (dtype,), (n, k), dev)
     if dev.index != L.current_device():
         with torch.cuda.device(dev):
             return dequantize_mx4(codes, scale, k, dtype=dtype, out=out)
     if out is None:
         out = torch.empty((n, k), dtype=dtype, device=dev)
-    L.check(L.lib().aep_mx4_dequantize(codes.data_ptr(), scale.data_ptr(), n, k, out.data_ptr(), _CODE[dtype], _ld(out),
-                                       L.raw_stream(dev.index)), "aep_mx4_dequantize")
+    st = L.lib().aep_mx4_dequantize(codes.data_ptr(), scale.data_ptr(), n, k, out.data_ptr(), _CODE[dtype], _ld(out),
+                                    L.raw_stream(dev.index))
+    if st:
+        L.check(st, "aep_mx4_dequantize")
     return out
 
 
@@ -184,6 +212,18 @@ def _heads(t, name, shape, dev) -> None:
         raise ValueError(f"{name}: the last dimension must be contiguous")
 
 
+def _tables(pages, lens, rows, flag):
+    """What is checked of a call's sequences."""
+    return (pages.shape, pages.stride(), pages.dtype, pages.device, lens.shape, lens.stride(), lens.dtype, lens.device,
+            rows is None or (rows.shape, rows.stride(), rows.dtype, rows.device),
+            flag is None or (flag.shape, flag.stride(), flag.dtype, flag.device))
+
+
+def _seqs(pages, lens, rows, flag, sizes):
+    return ctypes.byref(L.Cache4Seqs(pages.data_ptr(), lens.data_ptr(), None if rows is None else rows.data_ptr(),
+                                     None if flag is None else flag.data_ptr(), *sizes))
+
+
 class Cache4(_Fixed):
     """A paged cache of keys and values in 4 bits (``aep_cache4``) and the attention
     over it.
@@ -215,9 +255,10 @@ class Cache4(_Fixed):
         if self.device.type != "cuda":
             raise ValueError(f"a cache on {self.device}, expected a CUDA (HIP) device")
         self._mem = self.data.data_ptr()
-        self._calls = {}  # attention calls by what is checked of their tensors
+        self._calls = {}  # calls by what is checked of their tensors
 
-    def _seqs(self, pages, lens, rows, flag, total) -> L.Cache4Seqs:
+    def _sizes(self, pages, lens, rows, flag, total) -> Tuple[int, int, int, int]:
+        """(distance of the pages' rows, pages, sequences, rows) of a call, checked."""
         dev = self.device
         _rows(pages, "pages", (torch.int32,), (None, None), dev)
         B = pages.shape[0]
@@ -230,8 +271,13 @@ class Cache4(_Fixed):
             raise ValueError(f"{total} rows for {B} sequences: rows says whose they are")
         _int32(max(total, pages.shape[1] * self.page_size), 1 << 30, "rows, or tokens of a sequence", "aep_cache4")
         _int32(B, 1 << 24, "sequences", "aep_cache4")
-        return L.Cache4Seqs(pages.data_ptr(), lens.data_ptr(), None if rows is None else rows.data_ptr(),
-                            None if flag is None else flag.data_ptr(), _ld(pages), pages.shape[1], B, total)
+        return _ld(pages), pages.shape[1], B, total
+
+    def _keep(self, key, call):
+        if len(self._calls) >= 1024:
+            self._calls.clear()
+        self._calls[key] = call
+        return call
 
     def append(self, k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, lens: torch.Tensor,
                rows: Optional[torch.Tensor] = None, *, flag: Optional[torch.Tensor] = None) -> None:
@@ -241,39 +287,58 @@ class Cache4(_Fixed):
         if dev.index != L.current_device():
             with torch.cuda.device(dev):
                 return self.append(k, v, pages, lens, rows, flag=flag)
-        _heads(k, "k", (None, self.n_heads, self.head_dim), dev)
-        _heads(v, "v", tuple(k.shape), dev)
-        s = self._seqs(pages, lens, rows, flag, k.shape[0])
-        L.check(self._lib.aep_cache4_append(self._at, self._mem, ctypes.byref(s), k.data_ptr(), k.stride(0), k.stride(1),
-                                            v.data_ptr(), v.stride(0), v.stride(1), L.raw_stream(dev.index)),
-                "aep_cache4_append")
+        # a call like one before, in all that is checked, needs no checks
+        try:
+            key = ("append", k.shape, k.stride(), k.dtype, k.device, v.shape, v.stride(), v.dtype, v.device,
+                   _tables(pages, lens, rows, flag))
+        except AttributeError:
+            raise ValueError("k, v, pages, lens, rows and flag must be tensors") from None
+        fixed = self._calls.get(key)
+        if fixed is None:
+            _heads(k, "k", (None, self.n_heads, self.head_dim), dev)
+            _heads(v, "v", tuple(k.shape), dev)
+            fixed = self._keep(key, self._sizes(pages, lens, rows, flag, k.shape[0]))
+        st = self._lib.aep_cache4_append(self._at, self._mem, _seqs(pages, lens, rows, flag, fixed), k.data_ptr(), k.stride(0),
+                                         k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), L.raw_stream(dev.index))
+        if st:
+            L.check(st, "aep_cache4_append")
 
     def read(self, pages: torch.Tensor, lens: torch.Tensor, n_rows: int, rows: Optional[torch.Tensor] = None, *,
              k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
              flag: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         """The newest tokens' keys and values [n_rows, n_heads, head_dim] bfloat16
-        (``aep_cache4_read``): what the cache keeps of them, zeros where a sequence has no token for a row.
-        Rows of no sequence are left as they were in k and v."""
-        dev, n_rows = self.device, arg32(n_rows, "n_rows", "aep_cache4_read")
-        if n_rows < 0:
-            raise ValueError(f"n_rows is {n_rows}")
+        (``aep_cache4_read``): what the cache keeps of them, zeros where a sequence has
+        no token for a row.  Rows of no sequence are left as they were in k and v."""
+        dev = self.device
         if dev.index != L.current_device():
             with torch.cuda.device(dev):
                 return self.read(pages, lens, n_rows, rows, k=k, v=v, flag=flag)
+        try:
+            key = ("read", n_rows, k is None or (k.shape, k.stride(), k.dtype, k.device, k.data_ptr() & 15),
+                   v is None or (v.shape, v.stride(), v.dtype, v.device, v.data_ptr() & 15),
+                   _tables(pages, lens, rows, flag))
+        except AttributeError:
+            raise ValueError("pages, lens, rows, k, v and flag must be tensors") from None
+        fixed = self._calls.get(key)
         shape = (n_rows, self.n_heads, self.head_dim)
-        s = self._seqs(pages, lens, rows, flag, n_rows)
-        out = []
-        for t, name in ((k, "k"), (v, "v")):
-            if t is None:
-                t = torch.empty(shape, dtype=torch.bfloat16, device=dev)
-            else:
-                _heads(t, name, shape, dev)
-                if not t.is_contiguous():
-                    raise ValueError(f"{name} must be contiguous")
-            out.append(t)
-        L.check(self._lib.aep_cache4_read(self._at, self._mem, ctypes.byref(s), out[0].data_ptr(), out[1].data_ptr(),
-                                          L.raw_stream(dev.index)), "aep_cache4_read")
-        return out[0], out[1]
+        if fixed is None:
+            if arg32(n_rows, "n_rows", "aep_cache4_read") < 0:
+                raise ValueError(f"n_rows is {n_rows}")
+            for t, name in ((k, "k"), (v, "v")):
+                if t is not None:
+                    _heads(t, name, shape, dev)
+                    if not t.is_contiguous():
+                        raise ValueError(f"{name} must be contiguous")
+            fixed = self._keep(key, self._sizes(pages, lens, rows, flag, n_rows))
+        if k is None:
+            k = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        if v is None:
+            v = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        st = self._lib.aep_cache4_read(self._at, self._mem, _seqs(pages, lens, rows, flag, fixed), k.data_ptr(), v.data_ptr(),
+                                       L.raw_stream(dev.index))
+        if st:
+            L.check(st, "aep_cache4_read")
+        return k, v
 
     def attend(self, q: torch.Tensor, pages: torch.Tensor, lens: torch.Tensor, rows: Optional[torch.Tensor] = None, *,
                scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None,
@@ -291,23 +356,18 @@ class Cache4(_Fixed):
                 return self.attend(q, pages, lens, rows, scale=scale, window=window, out=out, lse=lse, flag=flag)
         # a call like one before, in all that is checked, needs no checks
         try:
-            key = (q.shape, q.stride(), q.dtype, q.device, pages.shape, pages.stride(), pages.dtype, pages.device,
-                   lens.shape, lens.stride(), lens.dtype, lens.device, scale, window,
-                   rows is None or (rows.shape, rows.stride(), rows.dtype, rows.device),
+            key = (q.shape, q.stride(), q.dtype, q.device, scale, window,
                    out is None or (out.shape, out.stride(), out.dtype, out.device),
-                   lse is None or (lse.shape, lse.stride(), lse.dtype, lse.device),
-                   flag is None or (flag.shape, flag.stride(), flag.dtype, flag.device))
+                   lse is None or (lse.shape, lse.stride(), lse.dtype, lse.device), _tables(pages, lens, rows, flag))
         except AttributeError:
             raise ValueError("q, pages, lens, rows, out, lse and flag must be tensors") from None
-        need, desc, fixed = self._calls.get(key) or self._describe(key, q, pages, lens, rows, scale, window, out, lse, flag)
+        need, desc, sizes = self._calls.get(key) or self._describe(key, q, pages, lens, rows, scale, window, out, lse, flag)
         if out is None:
             out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None  # held until the launch is in the stream
-        s = L.Cache4Seqs(pages.data_ptr(), lens.data_ptr(), None if rows is None else rows.data_ptr(),
-                         None if flag is None else flag.data_ptr(), *fixed)
-        st = self._lib.aep_cache4_attend(self._at, self._mem, ctypes.byref(s), desc, q.data_ptr(), out.data_ptr(),
-                                         None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(),
-                                         need, L.raw_stream(dev.index))
+        st = self._lib.aep_cache4_attend(self._at, self._mem, _seqs(pages, lens, rows, flag, sizes), desc, q.data_ptr(),
+                                         out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                         None if ws is None else ws.data_ptr(), need, L.raw_stream(dev.index))
         if st:
             L.check(st, "aep_cache4_attend")
         return out
@@ -327,13 +387,10 @@ class Cache4(_Fixed):
         scale = self.head_dim ** -0.5 if scale is None else float(scale)
         if window < 0 or not math.isfinite(scale) or scale <= 0:
             raise ValueError(f"window {window}, scale {scale}")
-        s = self._seqs(pages, lens, rows, flag, T)
+        sizes = self._sizes(pages, lens, rows, flag, T)
         o = (H * self.head_dim, self.head_dim) if out is None else (out.stride(0), out.stride(1))
         d = L.Attend4Desc(H, window, scale, q.stride(0), q.stride(1), *o)
         b = ctypes.c_size_t()
-        L.check(self._lib.aep_cache4_attend_workspace(self._at, ctypes.byref(s), ctypes.byref(d), ctypes.byref(b)),
-                "aep_cache4_attend_workspace")
-        if len(self._calls) >= 1024:
-            self._calls.clear()
-        call = self._calls[key] = (b.value, ctypes.byref(d), (s.ld_pages, s.max_pages, s.batch, s.total))
-        return call
+        L.check(self._lib.aep_cache4_attend_workspace(self._at, _seqs(pages, lens, rows, flag, sizes), ctypes.byref(d),
+                                                      ctypes.byref(b)), "aep_cache4_attend_workspace")
+        return self._keep(key, (b.value, ctypes.byref(d), sizes))
