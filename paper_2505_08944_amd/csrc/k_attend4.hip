@@ -44,13 +44,13 @@ struct SeqUnits {
   __device__ int units(int heads) const { return heads * ct * nb; }
 };
 template <int COLS>
-__device__ __forceinline__ SeqUnits seq_units(const Attend4Args& a, int b) {
+__device__ __forceinline__ SeqUnits seq_units(const Attend4Args& a, const SeqRows& s) {
   SeqUnits u;
-  u.s = seq_rows(a.s, a.c.log_page, b);
+  u.s = s;
   u.first = 0;
-  if (a.window) u.first = max(0, u.s.len - u.s.n - a.window + 1) / kUnit;
-  u.nb = max(1, (u.s.len + kUnit - 1) / kUnit - u.first);
-  u.ct = (int)(((int64_t)u.s.n * a.group + COLS - 1) / COLS);
+  if (a.window) u.first = max(0, s.len - s.n - a.window + 1) / kUnit;
+  u.nb = max(1, (s.len + kUnit - 1) / kUnit - u.first);
+  u.ct = (int)(((int64_t)s.n * a.group + COLS - 1) / COLS);
   return u;
 }
 
@@ -60,6 +60,7 @@ struct Place {
   int total;     // units of all sequences
   int u0, u1;    // this workgroup's
   int b, before; // sequence of u0, units before that sequence
+  SeqRows s;     // that sequence
 };
 // Units total / workers each, the first total % workers of them one more.
 struct Shares {
@@ -72,10 +73,11 @@ struct Shares {
   }
 };
 
+// (by all 256 threads, a sequence in each; what they read of the one that u0 lies in goes along)
 template <int COLS>
 __device__ __forceinline__ Place find_place(const Attend4Args& a) {
-  const int lane = threadIdx.x & 63, batch = a.s.batch;
-  const auto units = [&](int b) { return b < batch ? seq_units<COLS>(a, b).units(a.c.heads) : 0; };
+  __shared__ int of_wave[2][4], found[6];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, batch = a.s.batch;
   const auto upto = [&](int n) {  // sums of lanes 0 .. this one
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -84,35 +86,67 @@ __device__ __forceinline__ Place find_place(const Attend4Args& a) {
     }
     return n;
   };
+  SeqRows s{};
+  const auto units = [&](int b) {
+    if (b >= batch) return 0;
+    s = seq_rows(a.s, a.c.log_page, b);
+    return seq_units<COLS>(a, s).units(a.c.heads);
+  };
+  int all = 0;
+  for (int base = 256; base < batch; base += 256) all += units(base + tid);
+  int n = units(tid), sum = upto(n);
+  if (batch > 256) all = upto(all);
+  if (lane == 63) {
+    of_wave[0][wave] = sum;
+    of_wave[1][wave] = all;
+  }
+  if (tid == 0) found[0] = batch;  // (unless what is read changes meanwhile)
+  __syncthreads();
   Place p;
-  int n = units(lane), sum = upto(n), all = 0;
-  for (int base = 64; base < batch; base += 64) all += units(base + lane);
-  p.total = __builtin_amdgcn_readlane(sum, 63);
-  if (batch > 64) p.total += __builtin_amdgcn_readlane(upto(all), 63);
+  p.total = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p.total += of_wave[0][i] + of_wave[1][i];
+  p.total = __builtin_amdgcn_readfirstlane(p.total);
   // an XCD's workgroups have neighbouring shares, and all XCDs have some
   p.workers = min(a.workers, p.total);
   const int each = (p.workers + 7) >> 3, i = (int)(blockIdx.x >> 3);
   p.w = (int)(blockIdx.x & 7) * each + i;
-  if (i >= each || p.w >= p.workers) {
-    p.w = p.workers + 1;  // (without a share)
+  if (i >= each || p.w >= p.workers) {  // without a share
     p.u0 = p.u1 = p.total;
     return p;
   }
   const Shares shares(p.total, p.workers);
   p.u0 = shares.start(p.w);
   p.u1 = shares.start(p.w + 1);
-  p.b = batch;  // (found below, unless what is read changes meanwhile)
-  p.before = 0;
-  for (int base = 0; base < batch; base += 64) {
-    if (base) sum = upto(n = units(base + lane));
-    const int at = __popcll(__ballot(p.before + sum <= p.u0));  // sequences that end before u0
-    if (at < 64) {
-      p.b = base + at;
-      p.before += __builtin_amdgcn_readlane(sum - n, at);
-      break;
+  int before = 0;
+  for (int base = 0; base < batch; base += 256) {
+    if (base) {
+      __syncthreads();
+      sum = upto(n = units(base + tid));
+      if (lane == 63) of_wave[0][wave] = sum;
+      __syncthreads();
     }
-    p.before += __builtin_amdgcn_readlane(sum, 63);
+    int mine = before + sum - n;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      mine += w < wave ? of_wave[0][w] : 0;
+      before += of_wave[0][w];
+    }
+    if (mine <= p.u0 && p.u0 < mine + n) {
+      found[0] = base + tid;
+      found[1] = mine;
+      found[2] = s.row0;
+      found[3] = s.n;
+      found[4] = s.len;
+    }
+    if (before > p.u0) break;
   }
+  __syncthreads();
+  p.b = __builtin_amdgcn_readfirstlane(found[0]);
+  p.before = __builtin_amdgcn_readfirstlane(found[1]);
+  p.s.row0 = __builtin_amdgcn_readfirstlane(found[2]);
+  p.s.n = __builtin_amdgcn_readfirstlane(found[3]);
+  p.s.len = __builtin_amdgcn_readfirstlane(found[4]);
   return p;
 }
 
@@ -324,7 +358,7 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
   Shared shared{};  // the tile that begins here and goes on behind
   int u = place.u0, b = place.b, before = place.before;
   while (u < place.u1 && b < a.s.batch) {
-    const SeqUnits q = seq_units<COLS>(a, b);
+    const SeqUnits q = seq_units<COLS>(a, b == place.b ? place.s : seq_rows(a.s, a.c.log_page, b));
     const int seq_total = q.units(a.c.heads);
     if (u - before >= seq_total) {
       before += seq_total;
@@ -525,7 +559,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
   Shared shared{};  // the tile that begins here and goes on behind
   int u = place.u0, b = place.b, before = place.before;
   while (u < place.u1 && b < a.s.batch) {
-    const SeqUnits q = seq_units<COLS>(a, b);
+    const SeqUnits q = seq_units<COLS>(a, b == place.b ? place.s : seq_rows(a.s, a.c.log_page, b));
     const int seq_total = q.units(a.c.heads);
     if (u - before >= seq_total) {
       before += seq_total;

@@ -97,6 +97,7 @@ CASES = [
     ([7, 5], 5, 2, 4, 128, 64), ([40, 9, 200], 9, 1, 4, 256, 32), ([130], 130, 1, 1, 128, 64), ([65, 200], 64, 2, 3, 64, 64),
     ([50, 257], 33, 2, 2, 256, 64), ([100, 0, 33, 500], [1, 3, 0, 20], 2, 4, 128, 64), ([70, 300], [70, 1], 1, 4, 64, 32),
     ([3, 2], 6, 2, 4, 128, 64), ([0, 0], 1, 1, 1, 128, 64), ([33] * 70, 1, 1, 4, 128, 32), ([5] * 130, [b % 3 for b in range(130)], 1, 2, 64, 32),
+    ([b % 5 for b in range(600)], [(b * 3) % 4 for b in range(600)], 1, 1, 64, 32), ([40, 0, 1] * 86, 1, 1, 2, 128, 32),
 ]
 
 
