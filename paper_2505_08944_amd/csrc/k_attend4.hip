@@ -486,7 +486,7 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
     const bool whole = start == 0 && end == q.nb;
     float* slot = a.parts + (int64_t)(2 * w + (start == 0)) * (COLS * (D + 2));
     if (start == 0 && !whole) {
-      shared = Shared{Shares(place.total, place.workers).of(u - end + q.nb - 1), place.total, h, tile, cols, q.s.row0, q.s.len - q.s.n, 0};
+      shared = Shared{min(Shares(place.total, place.workers).of(u - end + q.nb - 1), place.workers - 1), place.total, h, tile, cols, q.s.row0, q.s.len - q.s.n, 0};
     }
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -568,7 +568,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
     }
     const int item = (u - before) / q.nb, start = u - before - item * q.nb;
     const int end = min(q.nb, start + place.u1 - u);
-    const int h = item / q.ct, tile = item - h * q.ct;
+    // (early and late tiles in turn: the late ones' rows see more tokens)
+    const int h = item / q.ct, turn = item - h * q.ct, tile = turn & 1 ? q.ct - 1 - (turn >> 1) : turn >> 1;
     u += end - start;
 
     const int cols = (int)min((int64_t)COLS, (int64_t)q.s.n * a.group - (int64_t)tile * COLS);  // at least one
@@ -732,7 +733,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
     const bool whole = start == 0 && end == q.nb;
     float* slot = a.parts + (int64_t)(2 * w + (start == 0)) * (COLS * (D + 2));
     if (start == 0 && !whole)
-      shared = Shared{Shares(place.total, place.workers).of(u - end + q.nb - 1), place.total, h, tile, cols, q.s.row0, lag, 0};
+      shared = Shared{min(Shares(place.total, place.workers).of(u - end + q.nb - 1), place.workers - 1), place.total, h, tile, cols, q.s.row0, lag, 0};
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const int col = wave * WCOLS + c * 16 + l;
