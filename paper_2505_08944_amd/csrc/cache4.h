@@ -52,10 +52,19 @@ __device__ __forceinline__ SeqRows seq_rows(const Cache4Seqs& q, int log_page, i
   if (q.flag && l != s.len) *q.flag = 1;
   return s;
 }
-__device__ __forceinline__ int seq_page(const Cache4Seqs& q, int n_pages, int b, int i) {
-  const int p = q.pages[b * q.ld_pages + i], in = min(max(p, 0), n_pages - 1);
+__device__ __forceinline__ int page_in(const Cache4Seqs& q, int n_pages, int p) {
+  const int in = min(max(p, 0), n_pages - 1);
   if (q.flag && p != in) *q.flag = 1;
   return in;
+}
+__device__ __forceinline__ int seq_page(const Cache4Seqs& q, int n_pages, int b, int i) {
+  return page_in(q, n_pages, q.pages[b * q.ld_pages + i]);
+}
+// The same entry of a wave, not held to bounds yet: through the scalar cache, so that whoever waits
+// for it does not wait for the vector loads in flight.
+__device__ __forceinline__ int seq_page_raw(const Cache4Seqs& q, int b, int i) {
+  typedef const __attribute__((address_space(4))) int32_t* table;
+  return reinterpret_cast<table>(reinterpret_cast<uintptr_t>(q.pages))[b * q.ld_pages + i];
 }
 
 // Place (g, j) of token t of 32: the rows 4 g + i of an MFMA's result over tokens 0 ..

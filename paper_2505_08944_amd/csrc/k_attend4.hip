@@ -401,28 +401,28 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
     if (a.window) blk = max(blk, max(0, pos0 - a.window + 1) >> 5);
     blk += wave;
     const int pages32 = a.c.log_page - 5, in_page = (1 << pages32) - 1;
-    auto head_of = [&](int at) { 
-      const int page = __builtin_amdgcn_readfirstlane(seq_page(a.s, a.c.n_pages, b, at >> pages32));
-      return (int64_t)page * a.c.heads + h;
-    };
+    // (a page is asked for two blocks ahead, and held to bounds where it is used)
+    const auto page_of = [&](int at) { return seq_page_raw(a.s, b, at >> pages32); };
+    const auto head_of = [&](int page) { return (int64_t)page_in(a.s, a.c.n_pages, page) * a.c.heads + h; };
     const auto at_edge = [&](int at) {  // some column does not see all of its tokens
       return at * 32 + 31 > pos0 || (a.window && at * 32 <= pos1 - a.window);
     };
     Block<D> x;
-    int64_t next = 0;  // the next block's head of its page
+    int next = 0;  // the next block's page
     bool lost = false;  // a block of values that is NaN where some column may not see it
     const int blk0 = blk;
     if (blk < blk_end) {
-      next = head_of(blk);
-      load_keys<D>(x, a.c, next, blk & in_page, l, g);
-      load_values<D>(x, a.c, next, blk & in_page, l, g);
-      if (blk + 4 < blk_end) next = head_of(blk + 4);
+      const int page = page_of(blk);
+      if (blk + 4 < blk_end) next = page_of(blk + 4);
+      load_keys<D>(x, a.c, head_of(page), blk & in_page, l, g);
+      load_values<D>(x, a.c, head_of(page), blk & in_page, l, g);
     }
     // A block's keys make room for the next one's as soon as the scores are there, its values when
     // they have been added: no second set of registers, and the other waves hide the loads.
     for (; blk < blk_end; blk += 4) {
-      const int64_t after = blk + 8 < blk_end ? head_of(blk + 8) : 0;
       const bool more = blk + 4 < blk_end;
+      const int64_t head = more ? head_of(next) : 0;
+      if (blk + 8 < blk_end) next = page_of(blk + 8);
       f32x4_t sc[2][NC];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
@@ -443,7 +443,7 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-      if (more) load_keys<D>(x, a.c, next, (blk + 4) & in_page, l, g);
+      if (more) load_keys<D>(x, a.c, head, (blk + 4) & in_page, l, g);
       if (at_edge(blk)) {
         hide_tokens<NC>(sc, blk * 32 + g * 4, pos, a.window);
         if (__ballot((any_byte_255(x.vs[0]) | any_byte_255(x.vs[1])) != 0)) {
@@ -471,13 +471,12 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
 #pragma unroll
       for (int j = 0; j < 8; ++j) fs[j] = mx4_scale(x.vs[j >> 2] >> (8 * (j & 3)) & 255u);
       add_values<D, NC, 0>(o, x.v, fs, p);
-      if (more) load_values<D>(x, a.c, next, (blk + 4) & in_page, l, g);
-      next = after;
+      if (more) load_values<D>(x, a.c, head, (blk + 4) & in_page, l, g);
     }
     if (lost) {
       for (int at = blk0; at < blk_end; at += 4)
         if (at_edge(at)) {
-          load_values<D>(x, a.c, head_of(at), at & in_page, l, g);
+          load_values<D>(x, a.c, head_of(page_of(at)), at & in_page, l, g);
           mark_lost<NC, NT>(o, x.vs, at * 32 + g * 4, pos, a.window);
         }
     }
@@ -605,16 +604,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
     const int st0 = st, last_block = (q.s.len - 1) >> 5;
     const int pages32 = a.c.log_page - 5, in_page = (1 << pages32) - 1;
     const auto block_of = [&](int at) { return min(at * 2 + (wave >> 1), last_block); };  // this wave's half of a step
-    const auto head_of = [&](int at) {
-      const int page = __builtin_amdgcn_readfirstlane(seq_page(a.s, a.c.n_pages, b, block_of(at) >> pages32));
-      return (int64_t)page * a.c.heads + h;
-    };
+    // (a page is asked for a step ahead of its use, and held to bounds there)
+    const auto page_of = [&](int at) { return seq_page_raw(a.s, b, block_of(at) >> pages32); };
+    const auto head_of = [&](int page) { return (int64_t)page_in(a.s, a.c.n_pages, page) * a.c.heads + h; };
     const auto at_edge = [&](int at) {  // some column of the tile does not see all of its tokens
       return at * 64 + 63 > pos0 || (a.window && at * 64 <= pos1 - a.window);
     };
     Block<D> x;  // (of the keys, 16 tokens)
-    const auto load = [&](int at, int64_t head) {
+    const auto load = [&](int at, int page) {
       const int blk = block_of(at) & in_page;
+      const int64_t head = head_of(page);
       load_keys<D>(x, a.c, head, blk, l, g, wave & 1);
       load_values<D>(x, a.c, head, blk, l, g);
     };
@@ -642,13 +641,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
     __syncthreads();  // (the tile before has been read)
     if (tid == 0) any_lost = 0;
     if (st < st_end) {
-      load(st, head_of(st));
-      int64_t next = st + 1 < st_end ? head_of(st + 1) : 0;
+      load(st, page_of(st));
+      int next = st + 1 < st_end ? page_of(st + 1) : 0;
       __syncthreads();
       widen(smem, st);
       if (st + 1 < st_end) {
         load(st + 1, next);
-        if (st + 2 < st_end) next = head_of(st + 2);
+        if (st + 2 < st_end) next = page_of(st + 2);
       }
       __syncthreads();
       for (int i = 0; st < st_end; ++st, i ^= 1) {
@@ -656,7 +655,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
         if (st + 1 < st_end) {
           widen(smem + (i ^ 1) * kBuffer, st + 1);
           if (st + 2 < st_end) load(st + 2, next);
-          if (st + 3 < st_end) next = head_of(st + 3);
+          if (st + 3 < st_end) next = page_of(st + 3);
         }
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
@@ -723,8 +722,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
       if (any_lost) {
         for (int at = st0 * 2; at < st_end * 2 && at <= last_block; ++at)
           if (at_edge(at >> 1)) {
-            const int page = __builtin_amdgcn_readfirstlane(seq_page(a.s, a.c.n_pages, b, at >> pages32));
-            load_values<D>(x, a.c, (int64_t)page * a.c.heads + h, at & in_page, l, g);
+            load_values<D>(x, a.c, head_of(seq_page_raw(a.s, b, at >> pages32)), at & in_page, l, g);
             mark_lost<NC, NT>(o, x.vs, at * 32 + g * 4, pos, a.window);
           }
       }
