@@ -256,7 +256,7 @@ __device__ __forceinline__ void add_values(f32x4_t (&o)[NC][D / 16], const uint3
   }
 }
 
-// Operands of the values whose pair number P is of this parity, into LDS.
+// Operands of every other pair of values from number P on, into LDS.
 template <int D, int P>
 __device__ __forceinline__ void widen_values(unsigned char* to, const uint32_t* v, const float* s) {
   if constexpr (P < D / 32) {
@@ -632,11 +632,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
       float fs[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) fs[j] = mx4_scale(x.vs[j >> 2] >> (8 * (j & 3)) & 255u);
-      unsigned char* v = to + kKeys + (wave >> 1) * (NT * 1024) + lane * 16;
-      if (wave & 1)
-        widen_values<D, 1>(v, x.v, fs);
-      else
-        widen_values<D, 0>(v, x.v, fs);
+      // (the pairs of this wave's parity, all at the even ones' places in the words)
+      uint32_t words[2 * STEPS];
+#pragma unroll
+      for (int i = 0; i < 2 * STEPS; ++i) words[i] = x.v[i] >> ((wave & 1) * 8);
+      widen_values<D, 0>(to + kKeys + (wave >> 1) * (NT * 1024) + (wave & 1) * 2048 + lane * 16, words, fs);
     };
     __syncthreads();  // (the tile before has been read)
     if (tid == 0) any_lost = 0;
