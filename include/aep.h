@@ -615,6 +615,8 @@ aep_status aep_cache4_read(const aep_cache4* c, const void* mem, const aep_cache
 typedef struct {
   int32_t n_heads;          /* of queries: a multiple of the cache's                */
   int32_t window;           /* 0: none                                              */
+  int32_t max_rows;         /* with rows: no sequence has more of them (0: not      */
+                            /* known), which may save launches; not looked at else  */
   float scale;              /* finite, > 0                                          */
   int64_t q_row, q_head;    /* elements from one row, or head, to the next, >= 0    */
   int64_t out_row, out_head; /* the same of out, whose heads must not overlap       */

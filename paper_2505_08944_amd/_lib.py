@@ -74,7 +74,8 @@ class Cache4Seqs(ctypes.Structure):
 
 
 class Attend4Desc(ctypes.Structure):
-    _fields_ = [("n_heads", ctypes.c_int32), ("window", ctypes.c_int32), ("scale", ctypes.c_float)] + \
+    _fields_ = [("n_heads", ctypes.c_int32), ("window", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("scale", ctypes.c_float)] + \
                [(n, ctypes.c_int64) for n in ("q_row", "q_head", "out_row", "out_head")]
 
 

@@ -12,6 +12,7 @@
 #pragma once
 
 #include "aep_internal.h"
+#include "attend4_plan.h"
 #include "mx4.h"
 
 namespace aep {
@@ -80,7 +81,8 @@ struct Attend4Args {
   int64_t q_row, q_head, o_row, o_head;
   int group;    // heads of queries per head of the cache
   int window;
-  float scale;  // times log2 e
+  int over, most;  // sequences of more than `over` columns (a row and a head of a group each), at most `most`
+  float scale;     // times log2 e
   int workers, nc;
   // Scratch: two parts of a tile for each workgroup (of the tile that its share begins inside
   // of, and of the one that begins in its share and goes on behind it), 16 nc columns of D sums, a
@@ -94,12 +96,6 @@ struct Attend4Args {
     return reinterpret_cast<Shared*>(parts + (int64_t)workers * 2 * (16 * nc) * (c.d + 2));
   }
 };
-// The attention's launch: columns of 16 per workgroup, workgroups, bytes of scratch.
-struct Attend4Plan {
-  int nc, workers;
-  int64_t bytes;
-};
-Attend4Plan attend4_plan(int batch, int total, int heads, int group, int d, int64_t max_len, int ncu);
 hipError_t launch_attend4(const Attend4Args& a, hipStream_t s);
 hipError_t launch_cache4_append(const Cache4& c, const Cache4Seqs& q, const uint16_t* k, const uint16_t* v, int64_t k_row,
                                 int64_t k_head, int64_t v_row, int64_t v_head, hipStream_t s);

@@ -29,9 +29,9 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 namespace {
 
 using Shared = Attend4Args::Shared;
+static_assert(sizeof(Shared) == kAttendShared);
 
-constexpr int kUnit = 128;  // tokens
-constexpr int kAttendWide = 8;  // columns in 16s of the kernel for many
+constexpr int kUnit = kAttendUnit;
 constexpr float kNegInf = -INFINITY;
 // A column's reference is its largest score (in powers of two) and this much more when it is set, and
 // holds until a weight reaches 2: few blocks change it, and no maximum is needed to see that.
@@ -50,7 +50,8 @@ __device__ __forceinline__ SeqUnits seq_units(const Attend4Args& a, const SeqRow
   u.first = 0;
   if (a.window) u.first = max(0, s.len - s.n - a.window + 1) / kUnit;
   u.nb = max(1, (s.len + kUnit - 1) / kUnit - u.first);
-  u.ct = (int)(((int64_t)s.n * a.group + COLS - 1) / COLS);
+  const int cols = s.n * a.group;
+  u.ct = cols > a.over && cols <= a.most ? (cols + COLS - 1) / COLS : 0;
   return u;
 }
 
@@ -336,9 +337,6 @@ __device__ __forceinline__ void mark_lost(f32x4_t (&o)[NC][NT], const uint32_t* 
 }
 
 }  // namespace
-
-// Workgroups per CU, which are waves per SIMD: as many as registers allow without spilling.
-constexpr int attend_per_cu(int d, int nc) { return d * nc == 64 ? 4 : d * nc == 128 ? 3 : d * nc == 256 ? 2 : 1; }
 
 template <int D, int NC>
 __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(const Attend4Args a) {
@@ -828,17 +826,6 @@ __global__ __launch_bounds__(512) void attend4_join_kernel(const Attend4Args a) 
   store4(a.out, kBF16, row * a.o_row + head * a.o_head + d, 4,
          empty ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(s.x * inv, s.y * inv, s.z * inv, s.w * inv));
   if (a.lse && d == 0) a.lse[row * ((int64_t)a.c.heads * a.group) + head] = empty ? kNegInf : lse_of(top, ls);
-}
-
-Attend4Plan attend4_plan(int batch, int total, int heads, int group, int d, int64_t max_len, int ncu) {
-  Attend4Plan p{};
-  const int64_t cols = ((int64_t)total + batch - 1) / std::max(batch, 1) * group;  // of a sequence, on average
-  p.nc = cols <= 16 ? 1 : cols <= 32 ? 2 : kAttendWide;
-  const int64_t most = (int64_t)heads * ((int64_t)total * group / (16 * p.nc) + batch) * std::max<int64_t>(1, (max_len + kUnit - 1) / kUnit);
-  const int per_cu = p.nc < kAttendWide ? attend_per_cu(d, p.nc) : d == 256 ? 1 : 2;
-  p.workers = (int)std::min<int64_t>((most + 7) / 8 * 8, (int64_t)ncu * per_cu);
-  p.bytes = (int64_t)p.workers * (2 * (16 * p.nc) * (d + 2) * 4 + (int64_t)sizeof(Attend4Args::Shared));
-  return p;
 }
 
 template <int D, int NC>

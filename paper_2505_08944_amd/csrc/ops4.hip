@@ -122,7 +122,7 @@ bool apart(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t d) {
 aep_status check_attend(const aep_cache4* c, const aep_cache4_seqs* s, const aep_attend4_desc* a) {
   if (const aep_status st = check_cache(c); st != AEP_OK) return st;
   if (const aep_status st = check_seqs(*c, s); st != AEP_OK) return st;
-  if (!a || a->n_heads < 1 || a->n_heads % c->n_heads || a->window < 0) return AEP_ERR_INVALID_ARG;
+  if (!a || a->n_heads < 1 || a->n_heads % c->n_heads || a->window < 0 || a->max_rows < 0) return AEP_ERR_INVALID_ARG;
   if (!std::isfinite(a->scale) || !(a->scale > 0.f)) return AEP_ERR_INVALID_ARG;
   const int64_t most = (int64_t)1 << 40;
   if (a->q_row < 0 || a->q_head < 0 || a->out_row < 0 || a->out_head < 0) return AEP_ERR_INVALID_ARG;
@@ -136,8 +136,8 @@ aep_status check_attend(const aep_cache4* c, const aep_cache4_seqs* s, const aep
   return AEP_OK;
 }
 Attend4Plan plan_of(const aep_cache4& c, const aep_cache4_seqs& s, const aep_attend4_desc& a) {
-  return attend4_plan(s.batch, s.total, c.n_heads, a.n_heads / c.n_heads, c.head_dim, (int64_t)s.max_pages * c.page_size,
-                      persistent_workgroups());
+  return attend4_plan(s.batch, s.total, s.rows != nullptr, a.max_rows ? a.max_rows : s.total, c.n_heads, a.n_heads / c.n_heads,
+                      c.head_dim, (int64_t)s.max_pages * c.page_size, persistent_workgroups());
 }
 
 }  // namespace
@@ -259,9 +259,14 @@ aep_status aep_cache4_attend(const aep_cache4* c, const void* mem, const aep_cac
   g.window = a->window >= (int64_t)s->max_pages * c->page_size ? 0 : a->window;
   g.scale = (float)((double)a->scale * 1.4426950408889634);
   g.parts = reinterpret_cast<float*>(d_ws);
-  g.workers = p.workers;
-  g.nc = p.nc;
-  return launched(launch_attend4(g, stream_of(stream)));
+  for (int i = 0; i < p.passes; ++i) {
+    g.nc = p.pass[i].nc;
+    g.workers = p.pass[i].workers;
+    g.over = p.pass[i].over;
+    g.most = p.pass[i].most;
+    if (launch_attend4(g, stream_of(stream)) != hipSuccess) return AEP_ERR_DEVICE;
+  }
+  return AEP_OK;
 }
 
 }  // extern "C"

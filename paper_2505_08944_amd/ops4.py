@@ -341,27 +341,30 @@ class Cache4(_Fixed):
         return k, v
 
     def attend(self, q: torch.Tensor, pages: torch.Tensor, lens: torch.Tensor, rows: Optional[torch.Tensor] = None, *,
-               scale: Optional[float] = None, window: int = 0, out: Optional[torch.Tensor] = None,
+               scale: Optional[float] = None, window: int = 0, max_rows: int = 0, out: Optional[torch.Tensor] = None,
                lse: Optional[torch.Tensor] = None, flag: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of rows of queries [T, heads, head_dim] bfloat16 to the tokens of
         their sequences up to their own (``aep_cache4_attend``); heads a multiple of n_heads.
 
         scale defaults to head_dim^-0.5.  window: how many tokens a row sees, the last
-        ones (0: all).  out [T, heads, head_dim] bfloat16 (rows and heads may be strided);
+        ones (0: all).  max_rows: with ``rows``, the most of a sequence where that is known
+        (0: not known); it may save launches, and must hold.  out [T, heads, head_dim] bfloat16 (rows and heads may be strided);
         lse [T, heads] float32 receives the logarithms of the sums.  A row without a token
         gets 0, and -inf; rows of no sequence are left as they were."""
         dev = self.device
         if dev.index != L.current_device():
             with torch.cuda.device(dev):
-                return self.attend(q, pages, lens, rows, scale=scale, window=window, out=out, lse=lse, flag=flag)
+                return self.attend(q, pages, lens, rows, scale=scale, window=window, max_rows=max_rows, out=out, lse=lse,
+                                   flag=flag)
         # a call like one before, in all that is checked, needs no checks
         try:
-            key = (q.shape, q.stride(), q.dtype, q.device, scale, window,
+            key = (q.shape, q.stride(), q.dtype, q.device, scale, window, max_rows,
                    out is None or (out.shape, out.stride(), out.dtype, out.device),
                    lse is None or (lse.shape, lse.stride(), lse.dtype, lse.device), _tables(pages, lens, rows, flag))
         except AttributeError:
             raise ValueError("q, pages, lens, rows, out, lse and flag must be tensors") from None
-        need, desc, sizes = self._calls.get(key) or self._describe(key, q, pages, lens, rows, scale, window, out, lse, flag)
+        need, desc, sizes = self._calls.get(key) or self._describe(key, q, pages, lens, rows, scale, window, max_rows, out,
+                                                                   lse, flag)
         if out is None:
             out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
         ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None  # held until the launch is in the stream
@@ -372,7 +375,7 @@ class Cache4(_Fixed):
             L.check(st, "aep_cache4_attend")
         return out
 
-    def _describe(self, key, q, pages, lens, rows, scale, window, out, lse, flag):
+    def _describe(self, key, q, pages, lens, rows, scale, window, max_rows, out, lse, flag):
         """(bytes of scratch, description, sizes of the sequences) of a checked call, kept for the next ones like it."""
         dev = self.device
         _heads(q, "q", (None, None, self.head_dim), dev)
@@ -383,13 +386,13 @@ class Cache4(_Fixed):
             _heads(out, "out", tuple(q.shape), dev)
         if lse is not None:
             _bytes_matrix(lse, "lse", (torch.float32,), (T, H), dev)
-        window = arg32(window, "window", "aep_cache4_attend")
+        window, max_rows = (arg32(n, what, "aep_cache4_attend") for n, what in ((window, "window"), (max_rows, "max_rows")))
         scale = self.head_dim ** -0.5 if scale is None else float(scale)
-        if window < 0 or not math.isfinite(scale) or scale <= 0:
-            raise ValueError(f"window {window}, scale {scale}")
+        if window < 0 or max_rows < 0 or not math.isfinite(scale) or scale <= 0:
+            raise ValueError(f"window {window}, max_rows {max_rows}, scale {scale}")
         sizes = self._sizes(pages, lens, rows, flag, T)
         o = (H * self.head_dim, self.head_dim) if out is None else (out.stride(0), out.stride(1))
-        d = L.Attend4Desc(H, window, scale, q.stride(0), q.stride(1), *o)
+        d = L.Attend4Desc(H, window, max_rows, scale, q.stride(0), q.stride(1), *o)
         b = ctypes.c_size_t()
         L.check(self._lib.aep_cache4_attend_workspace(self._at, _seqs(pages, lens, rows, flag, sizes), ctypes.byref(d),
                                                       ctypes.byref(b)), "aep_cache4_attend_workspace")

@@ -51,8 +51,13 @@ class Case:
         if sum(self.lens):
             self.cache.append(self.k, self.v, self.pages, i32(*self.lens), i32(*self.at))
 
-    def attend(self, **kw):
-        return self.cache.attend(self.q, self.pages, self.dev_lens, self.rows, **kw)
+    def attend(self, many=False, **kw):
+        """many: with a table padded so far that the kernel for many columns takes the sequences that have them."""
+        pages = self.pages
+        if many:
+            need = 8 * 512 * 128 // (self.Hkv * len(self.lens)) // self.cache.page_size + 1
+            pages = torch.nn.functional.pad(pages, (0, max(0, need - pages.shape[1])), value=-7)
+        return self.cache.attend(self.q, pages, self.dev_lens, self.rows, **kw)
 
     def check(self, out, lse=None, window=0, scale=None, what=None, rows=None):
         scale = self.D ** -0.5 if scale is None else scale
@@ -107,10 +112,11 @@ def test_cases(i):
     c = Case(*CASES[i], seed=i)
     for window in (0, 1, 50, 10 ** 6):
         log(f"attend4 case {i} {CASES[i]} window {window}")
-        flag, lse = i32(0), torch.full(c.q.shape[:2], 5.0, device="cuda")
-        out = c.attend(window=window, flag=flag, lse=lse)
-        c.check(out, lse, window, what=(i, window))
-        assert int(flag) == 0
+        for many in (False, True):
+            flag, lse = i32(0), torch.full(c.q.shape[:2], 5.0, device="cuda")
+            out = c.attend(many, window=window, flag=flag, lse=lse)
+            c.check(out, lse, window, what=(i, window, many))
+            assert int(flag) == 0
 
 
 @pytest.mark.parametrize("lens,n,Hkv,group,D,window", [
@@ -122,19 +128,20 @@ def test_long_and_shared(lens, n, Hkv, group, D, window):
     log(f"attend4 {lens} {n} {Hkv}x{group} d {D} window {window}")
     c = Case(lens, n, Hkv, group, D, seed=3)
     lse = torch.empty(c.q.shape[:2], device="cuda")
-    out = c.attend(window=window, lse=lse)
-    c.check(out, lse, window, rows={0, 1, 2, 3, 15, 16, 31, 63, 64, 100, 199, -1, -2})
+    for many in (False, True):
+        out = c.attend(many, window=window, lse=lse)
+        c.check(out, lse, window, rows={0, 1, 2, 3, 15, 16, 31, 63, 64, 100, 199, -1, -2}, what=many)
 
 
 def test_scores_that_grow_and_fall():
     """The reference follows: scores that grow from block to block, one token that outweighs all others at
     each place, scores far below 0."""
-    for grow in (0.01, -0.01, 0.3, -0.3):
-        c = Case([1500], 4, 1, 4, 128, seed=5)
+    for grow, n in ((0.01, 4), (-0.01, 4), (0.3, 4), (-0.3, 4), (0.02, 33), (-0.3, 33), (0.3, 33)):
+        c = Case([1500], n, 1, 4, 128, seed=5)
         c.k.copy_(((torch.arange(1500, device="cuda")[:, None, None] * grow).expand(1500, 1, 128)) / 128)
         c.q.copy_(torch.rand_like(c.q) * 8)
         c.write()
-        c.check(c.attend(scale=1.0), scale=1.0, what=grow)
+        c.check(c.attend(n > 16, scale=1.0), scale=1.0, what=(grow, n), rows={0, 1, 16, -1})
     c = Case([700], 1, 1, 1, 64, seed=6)
     for at in (0, 1, 31, 32, 127, 128, 500, 699):
         c.k.fill_(-1.0)
@@ -162,10 +169,11 @@ def test_values_that_are_not_finite():
         c.v[100 + 3, 0, 1] = float("inf")             # an early one of the second sequence
         c.write()
         lse = torch.empty(c.q.shape[:2], device="cuda")
-        out = c.attend(window=window, lse=lse)
-        c.check(out, None, window, what=(n, window, D))
-        assert not bool(torch.isnan(out[:n - n // 2 - 1]).any())
-        assert bool(torch.isnan(out[n - 1]).any())
+        for many in (False, True):
+            out = c.attend(many, window=window, lse=lse)
+            c.check(out, None, window, what=(n, window, D, many))
+            assert not bool(torch.isnan(out[:n - n // 2 - 1]).any())
+            assert bool(torch.isnan(out[n - 1]).any())
     c = Case([200], 2, 1, 4, 128, seed=10)
     c.q[0, 1, 0] = float("nan")
     out = c.attend()
@@ -223,6 +231,19 @@ def test_what_only_the_device_sees_is_held_to_bounds_and_reported():
     assert torch.equal(c.attend(), want)
 
 
+def test_prompts_beside_single_tokens():
+    """Sequences of many and of few columns in one call, with the most rows known and not; the same bits again and again."""
+    c = Case([700, 90, 0, 2000, 300, 1], [200, 1, 1, 3, 40, 1], 2, 4, 128, seed=18)
+    for many in (False, True):
+        out = c.attend(many)
+        c.check(out, what=many, rows={0, 1, 2, 31, 32, 33, 127, -1})
+        for max_rows in (200, 10 ** 6):
+            assert torch.equal(c.attend(many, max_rows=max_rows), out)
+        c.check(c.attend(many, max_rows=3), what="a bound that does not hold", rows={0, 1, -1})
+        for i in range(5):
+            assert torch.equal(c.attend(many), out)
+
+
 def test_nothing_to_do():
     c = Case([30], 1, 2, 4, 64, seed=15)
     assert c.cache.attend(c.q[:0], c.pages, c.dev_lens).shape == (0, 8, 64)
@@ -258,6 +279,19 @@ def test_lengths_change_under_a_captured_call():
         k, _ = c.cache.read(c.pages, i32(*now), 4)
         codes = aep.quantize_mx4(new_k.view(8, 128))
         assert torch.equal(k.view(8, 128), aep.dequantize_mx4(*codes, 128))
+
+
+def test_a_captured_call_with_many_columns():
+    c = Case([700, 90, 300], [100, 1, 40], 2, 4, 64, seed=19)
+    want, out = c.attend(True), torch.empty_like(c.q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.attend(True, out=out)
+    for i in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(c.attend(True), want), i
 
 
 def test_threads_on_streams_of_their_own():

@@ -105,7 +105,7 @@ def _seqs(**kw):
 
 
 def _desc(**kw):
-    a = dict(n_heads=8, window=0, scale=1.0, q_row=1024, q_head=128, out_row=1024, out_head=128)
+    a = dict(n_heads=8, window=0, max_rows=0, scale=1.0, q_row=1024, q_head=128, out_row=1024, out_head=128)
     a.update(kw)
     return L.Attend4Desc(**a)
 
@@ -147,7 +147,7 @@ def test_sequences(kw, status):
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(n_heads=0), 1), (dict(n_heads=7), 1), (dict(window=-1), 1), (dict(scale=0.0), 1), (dict(scale=-1.0), 1),
+    (dict(n_heads=0), 1), (dict(n_heads=7), 1), (dict(window=-1), 1), (dict(max_rows=-1), 1), (dict(scale=0.0), 1), (dict(scale=-1.0), 1),
     (dict(scale=float("nan")), 1), (dict(scale=float("inf")), 1), (dict(q_row=-1), 1), (dict(q_head=-1), 1), (dict(out_row=-1), 1),
     (dict(out_head=-1), 1), (dict(out_head=127), 1), (dict(out_row=1023), 1), (dict(out_row=0), 1), (dict(q_row=1 << 41), 6),
     (dict(out_row=1 << 41), 6)])
