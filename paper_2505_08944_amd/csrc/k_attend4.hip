@@ -2,18 +2,23 @@
 // of queries o = sum_t p_t v_t / sum_t p_t, p_t = e^(scale q k_t), over the tokens that
 // it sees, in one pass with a running reference for the exponents.
 //
-// A tile of 16 NC columns (a column is a row of queries and one of the heads that share
-// a head of the cache) takes 32 tokens at a time in a wave: scores as K q^T on MFMAs
-// (rows: tokens, columns: queries), which leaves a lane 8 tokens of its column, in the
-// order in which it holds them as an operand of V^T p^T.  Codes become exact bf16 in
-// registers; p is rounded to bf16 once, and its sum is that of the rounded values (an
-// MFMA with ones), so that weights sum to 1.
+// A column is a row of queries and one of the heads that share a head of the cache.
+// Scores are K q^T on MFMAs (rows: tokens, columns: queries), which leaves a lane 8 of 32 tokens
+// of its column in the order in which it holds them as an operand of V^T p^T: the weights
+// need no way through LDS.  Codes become exact bf16 in registers; p is rounded to bf16
+// once, for the second product, and its sum is that of the rounded values (an MFMA with ones), so
+// that weights sum to 1.  Scores, sums and references are f32.
 //
-// Bound by the cache's bytes for few columns, by VALU (conversions, exponentials) for many.
+// Few columns (attend4_kernel): a wave takes 32 tokens for a tile of 16 or 32 columns.
+// Bound by the cache's bytes: 64 sequences of up to 16384 tokens, 8 heads of 128, 101 us
+// of kernel for 507 MB (5.0 TB/s; a large copy 5.2); one sequence of 100003 tokens 25 us for 109 MB.
+// Many columns (attend4_wide_kernel): four waves with 32 columns each share what they
+// widen.  Bound by MFMAs and VALU, which do not run at once here even from two waves of a
+// SIMD (4 x 509 rows to up to 8192 tokens: 41% and 36% of the cycles): 176 us of kernel.
+//
 // The work is divided evenly: all units of 128 tokens of all tiles in a row, an equal share
-// for each workgroup; its four waves take 32 of each unit and are joined in LDS.
-// Tiles that several workgroups share leave parts in the scratch, which a second launch joins
-// in the order of the tokens.
+// for each workgroup.  Tiles that several workgroups share leave parts in the scratch, which a
+// second launch joins in the order of the tokens: no atomics, equal calls give equal bits.
 #include <algorithm>
 #include <climits>
 #include <cmath>

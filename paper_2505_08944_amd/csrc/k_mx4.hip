@@ -1,5 +1,6 @@
 // Matrices to 4 bits and back (mx4.h), and the layout of 4-bit weights that the
-// dense product reads.  All of it is bound by HBM.
+// dense product reads.  All of it is bound by HBM: 14336 x 4096 from bf16 25 us (148 MB, 6 TB/s,
+// part of it in the Infinity Cache), back 23, its layout for the product 14.
 #include <algorithm>
 
 #include "linear4.h"
