@@ -163,14 +163,17 @@ __device__ __forceinline__ float max_of_columns(float v) {  // over the lanes l,
   return fmaxf(__uint_as_float(q[0]), __uint_as_float(q[1]));
 }
 
-__device__ __forceinline__ uint32_t any_byte_255(uint32_t w) { return (~w - 0x01010101u) & w & 0x80808080u; }
-// The word with its bytes of 255 as 0.
-__device__ __forceinline__ uint32_t without_255(uint32_t w) {
+// Scale bytes with which a value may not be finite: 255, and above the quantiser's largest, what places hold that
+// nothing was written to.  (A byte of ~w below 3 borrows.)
+constexpr uint32_t kNotFinite = 253;
+__device__ __forceinline__ uint32_t any_not_finite(uint32_t w) { return (~w - 0x03030303u) & w & 0x80808080u; }
+// The word with these as 0.
+__device__ __forceinline__ uint32_t only_finite(uint32_t w) {
   uint32_t o = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint32_t b = w >> (8 * i) & 255u;
-    o |= (b == 255u ? 0u : b) << (8 * i);
+    o |= (b >= kNotFinite ? 0u : b) << (8 * i);
   }
   return o;
 }
@@ -311,7 +314,7 @@ __device__ __forceinline__ float raise(const f32x4_t s0, const f32x4_t s1, float
   return shrink;
 }
 
-// Columns that see a token of a block whose values are NaN (scale byte 255 in vs) have NaN there: such a
+// Columns that see a token of a block whose values are NaN (by its scale byte in vs) have NaN there: such a
 // token counts 1 for the values of this lane, a token that a column sees 1 for it.
 template <int NC, int NT>
 __device__ __forceinline__ void mark_lost(f32x4_t (&o)[NC][NT], const uint32_t* vs, int t0, const int* pos, int window) {
@@ -319,7 +322,7 @@ __device__ __forceinline__ void mark_lost(f32x4_t (&o)[NC][NT], const uint32_t* 
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const uint32_t pair = vs[j >> 1] >> (16 * (j & 1));
-    na[j] = ((pair & 255u) == 255u ? 0x3f80u : 0u) | ((pair >> 8 & 255u) == 255u ? 0x3f800000u : 0u);
+    na[j] = ((pair & 255u) >= kNotFinite ? 0x3f80u : 0u) | ((pair >> 8 & 255u) >= kNotFinite ? 0x3f800000u : 0u);
   }
   const bf16x8_t nan_at = __builtin_bit_cast(bf16x8_t, make_uint4(na[0], na[1], na[2], na[3]));
 #pragma unroll
@@ -449,10 +452,10 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
       if (more) load_keys<D>(x, a.c, head, (blk + 4) & in_page, l, g);
       if (at_edge(blk)) {
         hide_tokens<NC>(sc, blk * 32 + g * 4, pos, a.window);
-        if (__ballot((any_byte_255(x.vs[0]) | any_byte_255(x.vs[1])) != 0)) {
+        if (__ballot((any_not_finite(x.vs[0]) | any_not_finite(x.vs[1])) != 0)) {
           lost = true;  // (seen to behind the loop)
-          x.vs[0] = without_255(x.vs[0]);
-          x.vs[1] = without_255(x.vs[1]);
+          x.vs[0] = only_finite(x.vs[0]);
+          x.vs[1] = only_finite(x.vs[1]);
         }
       }
       bf16x8_t p[NC];
@@ -627,10 +630,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
         const float f = mx4_scale(D == 256 ? (s < 4 ? x.ks[0] & 255u : x.ks[0] >> 8) : x.ks[0]);
         *reinterpret_cast<uint4*>(to + (wave * STEPS + s) * 1024 + lane * 16) = mx4_bf16x8(x.k[0][s], f);
       }
-      if (at_edge(at) && __ballot((any_byte_255(x.vs[0]) | any_byte_255(x.vs[1])) != 0)) {
+      if (at_edge(at) && __ballot((any_not_finite(x.vs[0]) | any_not_finite(x.vs[1])) != 0)) {
         any_lost = 1;  // (seen to behind the loop)
-        x.vs[0] = without_255(x.vs[0]);
-        x.vs[1] = without_255(x.vs[1]);
+        x.vs[0] = only_finite(x.vs[0]);
+        x.vs[1] = only_finite(x.vs[1]);
       }
       float fs[8];
 #pragma unroll

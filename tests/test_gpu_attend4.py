@@ -180,6 +180,20 @@ def test_values_that_are_not_finite():
     assert bool(torch.isnan(out[0, 1]).all()) and int(torch.isnan(out).sum()) == 128
 
 
+@pytest.mark.parametrize("byte", [0x7f, 0xfc, 0xfd, 0xfe])
+def test_unwritten_places_hold_any_byte(byte):
+    """Behind the last token, scales of 2^125 and more and codes of -6: beyond bf16 with the two largest."""
+    for lens, n, Hkv, group, D in (([1, 40, 33], 1, 2, 4, 128), ([45, 7], 5, 1, 8, 64), ([70, 130], 40, 1, 2, 256),
+                                   ([75], 70, 2, 2, 64), ([35, 161], 30, 1, 8, 128)):
+        c = Case(lens, n, Hkv, group, D, seed=11)
+        c.cache.data.fill_(byte)
+        c.write()
+        for window in (0, 20):
+            for many in (False, True):
+                lse = torch.full(c.q.shape[:2], 5.0, device="cuda")
+                c.check(c.attend(many, window=window, lse=lse), lse, window, what=(byte, lens, window, many))
+
+
 def test_scale():
     c = Case([300, 20], 2, 2, 4, 128, seed=11)
     for scale in (1e-30, 0.01, 1.0, 30.0):
