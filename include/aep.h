@@ -578,7 +578,8 @@ typedef struct {
  * to what there is, so that accesses stay in bounds, and sets *flag to 1 (flag may
  * be NULL; it is never cleared): rows that descend or lie outside 0 .. total, and
  * of what the call's rows need, a page outside the cache, or a length below 0 or
- * beyond max_pages.  What such a sequence's rows get is not defined. */
+ * beyond max_pages.  What such a sequence's rows get is not defined, and with rows
+ * that descend what any row gets. */
 typedef struct {
   const int32_t* pages;  /* [batch][max_pages], rows ld_pages apart                */
   const int32_t* lens;   /* [batch]                                                */

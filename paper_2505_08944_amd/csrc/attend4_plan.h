@@ -16,10 +16,11 @@ constexpr int attend_per_cu(int d, int nc) { return d * nc == 64 ? 4 : d * nc ==
 
 // The attention's launches: each takes the sequences of more than `over` columns and at most `most`, with
 // tiles of nc 16 columns and so many workgroups; bytes of scratch, which they use one after the other.
+// units: as many as sequences of disjoint rows can have (fewer than 2^31 by the caller's checks).
 struct Attend4Plan {
   int passes;
   struct {
-    int nc, workers, over, most;
+    int nc, workers, over, most, units;
   } pass[2];
   int64_t bytes;
 };
@@ -46,6 +47,7 @@ inline Attend4Plan attend4_plan(int batch, int total, bool rows, int max_rows, i
     p.pass[p.passes].workers = workers;
     p.pass[p.passes].over = over;
     p.pass[p.passes].most = upto;
+    p.pass[p.passes].units = (int)units(nc);
     ++p.passes;
     p.bytes = std::max(p.bytes, (int64_t)workers * ((int64_t)2 * (16 * nc) * (d + 2) * 4 + kAttendShared));
   };

@@ -83,7 +83,7 @@ struct Attend4Args {
   int window;
   int over, most;  // sequences of more than `over` columns (a row and a head of a group each), at most `most`
   float scale;     // times log2 e
-  int workers, nc;
+  int workers, nc, units;  // (units: at most, of rows that ascend)
   // Scratch: two parts of a tile for each workgroup (of the tile that its share begins inside
   // of, and of the one that begins in its share and goes on behind it), 16 nc columns of D sums, a
   // reference and a sum of weights each; then what the second launch has to know of the latter.

@@ -88,7 +88,7 @@ __device__ __forceinline__ Place find_place(const Attend4Args& a) {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const int o = __shfl_up(n, d);
-      if (lane >= d) n += o;
+      if (lane >= d) n = __builtin_elementwise_add_sat(n, o);
     }
     return n;
   };
@@ -98,8 +98,9 @@ __device__ __forceinline__ Place find_place(const Attend4Args& a) {
     s = seq_rows(a.s, a.c.log_page, b);
     return seq_units<COLS>(a, s).units(a.c.heads);
   };
+  // (sums stop at 2^31 - 1: with rows that descend, sequences share rows and the units are more than are counted)
   int all = 0;
-  for (int base = 256; base < batch; base += 256) all += units(base + tid);
+  for (int base = 256; base < batch; base += 256) all = __builtin_elementwise_add_sat(all, units(base + tid));
   int n = units(tid), sum = upto(n);
   if (batch > 256) all = upto(all);
   if (lane == 63) {
@@ -111,8 +112,10 @@ __device__ __forceinline__ Place find_place(const Attend4Args& a) {
   Place p;
   p.total = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) p.total += of_wave[0][i] + of_wave[1][i];
+  for (int i = 0; i < 4; ++i)
+    p.total = __builtin_elementwise_add_sat(p.total, __builtin_elementwise_add_sat(of_wave[0][i], of_wave[1][i]));
   p.total = __builtin_amdgcn_readfirstlane(p.total);
+  if (p.total > a.units) p.total = 0;  // nobody has a share (and the rows are reported)
   // an XCD's workgroups have neighbouring shares, and all XCDs have some
   p.workers = min(a.workers, p.total);
   const int each = (p.workers + 7) >> 3, i = (int)(blockIdx.x >> 3);

@@ -264,6 +264,7 @@ aep_status aep_cache4_attend(const aep_cache4* c, const void* mem, const aep_cac
     g.workers = p.pass[i].workers;
     g.over = p.pass[i].over;
     g.most = p.pass[i].most;
+    g.units = p.pass[i].units;
     if (launch_attend4(g, stream_of(stream)) != hipSuccess) return AEP_ERR_DEVICE;
   }
   return AEP_OK;

@@ -245,6 +245,32 @@ def test_what_only_the_device_sees_is_held_to_bounds_and_reported():
     assert torch.equal(c.attend(), want)
 
 
+def test_rows_that_descend_make_more_work_than_is_counted():
+    """Every other sequence has all rows, 65536 times: 4.4 10^9 units, more than 32 bits.  Nobody has a share of them."""
+    B, T, H, D, P = 1 << 17, 1 << 15, 8, 64, 66
+    assert (B // 2) * H * (T // 128) * -(-P * 64 // 128) > 1 << 32
+    cache = aep.Cache4(P, H, D)
+    pages = torch.arange(P, dtype=torch.int32, device="cuda").expand(B, P).contiguous()
+    lens = torch.full((B,), P * 64, dtype=torch.int32, device="cuda")
+    rows = torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    rows[1::2] = T
+    q = torch.zeros(T, H, D, dtype=torch.bfloat16, device="cuda")
+    out, flag = torch.full((T + 2, H, D), 77.0, dtype=torch.bfloat16, device="cuda"), i32(0)
+    log("attend4 rows that descend")
+    cache.attend(q, pages, lens, rows, out=out[1:-1], flag=flag)
+    assert int(flag) == 1 and bool((out == 77).all())
+    log("attend4 rows that descend, fewer")
+    rows = i32(0, 5, 0, 5, 0, 5, 0, 5)
+    flag = i32(0)
+    cache.attend(q[:5], pages[:7, :2], lens[:7], rows, out=out[1:6], flag=flag)
+    assert int(flag) == 1 and bool((out[0] == 77).all()) and bool((out[6:] == 77).all())
+    # and rows that ascend, with the same lengths
+    rows = torch.clamp(torch.arange(B + 1, device="cuda"), max=T).to(torch.int32)
+    flag = i32(0)
+    cache.attend(q[:64], pages[:100, :2], i32(*[128] * 100), torch.clamp(rows[:101], max=64), out=out[1:65], flag=flag)
+    assert int(flag) == 0 and bool((out[1:65] == 0).all()) and bool((out[0] == 77).all()) and bool((out[65:] == 77).all())
+
+
 def test_prompts_beside_single_tokens():
     """Sequences of many and of few columns in one call, with the most rows known and not; the same bits again and again."""
     c = Case([700, 90, 0, 2000, 300, 1], [200, 1, 1, 3, 40, 1], 2, 4, 128, seed=18)
