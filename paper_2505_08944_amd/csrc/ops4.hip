@@ -23,7 +23,7 @@ aep_status check_dtype(int32_t t) {
 aep_status check_matrix(int64_t rows, int32_t k, int64_t ld, int32_t dtype) {
   if (rows < 0 || k < 1 || ld < k) return AEP_ERR_INVALID_ARG;
   if (const aep_status st = check_dtype(dtype); st != AEP_OK) return st;
-  if (k > 1 << 30 || rows > (int64_t)1 << 38 || rows * (int64_t)((k + 31) / 32) > (int64_t)1 << 38) return AEP_ERR_UNSUPPORTED;
+  if (k > 1 << 30 || rows > ((int64_t)1 << 38) / ((k + 31) / 32)) return AEP_ERR_UNSUPPORTED;
   return AEP_OK;
 }
 

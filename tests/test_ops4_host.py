@@ -32,6 +32,14 @@ def test_quantiser():
     assert lib.aep_mx4_quantize(None, 0, 40, 0, 40, None, None, None) == L.AEP_OK
 
 
+def test_more_blocks_than_are_counted():
+    """2^38 blocks at most, also where rows times blocks of a row are more than 64 bits hold."""
+    lib = _lib()
+    for rows, k in ((1 << 38, 1 << 30), ((1 << 38) - 1, 1 << 30), ((1 << 13) + 1, 1 << 30), (1 << 38, 33), ((1 << 38) + 1, 1)):
+        assert lib.aep_mx4_quantize(16, 0, 1 << 30, rows, k, 16, 16, None) == UNSUPPORTED
+        assert lib.aep_mx4_dequantize(16, 16, rows, k, 16, 0, 1 << 30, None) == UNSUPPORTED
+
+
 def test_weights():
     lib = _lib()
     n = ctypes.c_size_t()
