@@ -573,7 +573,7 @@ typedef struct {
  * newest tokens: row i of n is token lens[b] - n + i, lens[b] being all tokens
  * of the sequence with these.  A row whose token would lie before the first
  * (more rows than tokens) has none.  Token t lies in page pages[b][t / page_size].
- * Rows that belong to no sequence are neither read nor written.  pages, lens,
+ * Rows that belong to no sequence do not count and are not written.  pages, lens,
  * rows and flag are device pointers to int32.  What only the device sees is held
  * to what there is, so that accesses stay in bounds, and sets *flag to 1 (flag may
  * be NULL; it is never cleared): rows that descend or lie outside 0 .. total, and

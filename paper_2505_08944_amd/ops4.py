@@ -39,6 +39,11 @@ def _checked(key, check) -> None:
         _seen[key] = True
 
 
+def _number(n, what: str, call: str) -> int:
+    """A whole number as an int: what calls are known by must not change as a tensor's value can."""
+    return n if type(n) is int else arg32(n, what, call)
+
+
 def quantize_mx4(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """x [n, k] float32 or bfloat16 to codes [n, (k + 1) // 2] and scales [n, (k +
     31) // 32], both uint8 (``aep_mx4_quantize``).  Rows may be strided."""
@@ -75,17 +80,17 @@ def dequantize_mx4(codes: torch.Tensor, scale: torch.Tensor, k: int, *, dtype: t
     if not isinstance(scale, torch.Tensor):
         raise ValueError("scale must be a tensor")
     dev = codes.device
+    k = _number(k, "k", "aep_mx4_dequantize")
 
     def check():
-        k_ = arg32(k, "k", "aep_mx4_dequantize")
-        if k_ < 1:
+        if arg32(k, "k", "aep_mx4_dequantize") < 1:
             raise ValueError(f"k is {k}")
-        _bytes_matrix(codes, "codes", _BYTE[:2], (None, (k_ + 1) // 2), dev)
-        _bytes_matrix(scale, "scale", (_BYTE[0], _BYTE[2]), (codes.shape[0], (k_ + 31) // 32), dev)
+        _bytes_matrix(codes, "codes", _BYTE[:2], (None, (k + 1) // 2), dev)
+        _bytes_matrix(scale, "scale", (_BYTE[0], _BYTE[2]), (codes.shape[0], (k + 31) // 32), dev)
         if dtype not in _F32_BF16:
             raise ValueError(f"dtype {dtype}, expected torch.bfloat16 or torch.float32")
         if out is not None:
-            _rows(out, "out", (dtype,), (codes.shape[0], k_), dev)
+            _rows(out, "out", (dtype,), (codes.shape[0], k), dev)
 
     _checked((k, codes.shape, codes.stride(), codes.dtype, dev, scale.shape, scale.stride(), scale.dtype, scale.device,
               dtype, out is None or (out.shape, out.stride(), out.dtype, out.device)), check)
@@ -313,6 +318,7 @@ class Cache4(_Fixed):
         if dev.index != L.current_device():
             with torch.cuda.device(dev):
                 return self.read(pages, lens, n_rows, rows, k=k, v=v, flag=flag)
+        n_rows = _number(n_rows, "n_rows", "aep_cache4_read")
         try:
             key = ("read", n_rows, k is None or (k.shape, k.stride(), k.dtype, k.device, k.data_ptr() & 15),
                    v is None or (v.shape, v.stride(), v.dtype, v.device, v.data_ptr() & 15),
@@ -356,6 +362,10 @@ class Cache4(_Fixed):
             with torch.cuda.device(dev):
                 return self.attend(q, pages, lens, rows, scale=scale, window=window, max_rows=max_rows, out=out, lse=lse,
                                    flag=flag)
+        window = _number(window, "window", "aep_cache4_attend")
+        max_rows = _number(max_rows, "max_rows", "aep_cache4_attend")
+        if scale is not None and type(scale) is not float:
+            scale = float(scale)
         # a call like one before, in all that is checked, needs no checks
         try:
             key = (q.shape, q.stride(), q.dtype, q.device, scale, window, max_rows,
@@ -387,7 +397,7 @@ class Cache4(_Fixed):
         if lse is not None:
             _bytes_matrix(lse, "lse", (torch.float32,), (T, H), dev)
         window, max_rows = (arg32(n, what, "aep_cache4_attend") for n, what in ((window, "window"), (max_rows, "max_rows")))
-        scale = self.head_dim ** -0.5 if scale is None else float(scale)
+        scale = self.head_dim ** -0.5 if scale is None else scale
         if window < 0 or max_rows < 0 or not math.isfinite(scale) or scale <= 0:
             raise ValueError(f"window {window}, max_rows {max_rows}, scale {scale}")
         sizes = self._sizes(pages, lens, rows, flag, T)

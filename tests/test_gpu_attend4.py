@@ -376,3 +376,18 @@ def test_pages_behind_4_gib():
     small.append(k, v, near, i32(T))
     q = rows_of(3, H * 2, D, 13, False)
     assert torch.equal(cache.attend(q, pages, i32(T)), small.attend(q, near, i32(T)))
+
+
+def test_numbers_in_tensors_count_by_their_value():
+    """A scale or a window in a tensor whose value changes between two calls."""
+    c = Case([100, 30], 2, 2, 4, 64, seed=23)
+    scale, window, most = torch.tensor(0.25, dtype=torch.float64), torch.tensor(0), torch.tensor(4)
+    for s, w, m in ((0.25, 0, 4), (0.5, 20, 2), (0.125, 3, 0)):
+        scale.fill_(s), window.fill_(w), most.fill_(m)
+        want = c.attend(scale=s, window=w, max_rows=m)
+        assert torch.equal(c.attend(scale=scale, window=window, max_rows=most), want)
+        c.check(want, window=w, scale=s, what=(s, w))
+    for kw in (dict(window=1.0), dict(max_rows=1.0), dict(window=1 << 40), dict(max_rows=-1), dict(scale=float("nan")), dict(scale="x")):
+        for _ in range(2):
+            with pytest.raises((TypeError, ValueError, aep.AEPError)):
+                c.attend(**kw)

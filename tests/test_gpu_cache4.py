@@ -195,3 +195,19 @@ def test_more_than_32_bits_of_bytes():
     for got, x in ((rk, k), (rv, v)):
         codes, scale = aep.quantize_mx4(x.view(T * H, D))
         assert torch.equal(got, aep.dequantize_mx4(codes, scale, D).view(T, H, D))
+
+
+def test_a_number_of_rows_in_a_tensor_counts_by_its_value():
+    cache = aep.Cache4(4, 1, 64)
+    pages, lens = i32(0, 1)[None], i32(100)
+    k, v = rows_of(100, 1, 64, 1), rows_of(100, 1, 64, 2)
+    cache.append(k, v, pages, lens)
+    n = torch.tensor(3)
+    for rows in (3, 50, 1):
+        n.fill_(rows)
+        for got, x in zip(cache.read(pages, lens, n), (k, v)):
+            assert got.shape == (rows, 1, 64) and equal(got, kept(x[100 - rows:]))
+    for bad in (3.0, 1 << 40, -1, "3"):
+        for _ in range(2):
+            with pytest.raises((TypeError, ValueError, aep.AEPError)):
+                cache.read(pages, lens, bad)

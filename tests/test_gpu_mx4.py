@@ -111,3 +111,18 @@ def test_more_than_32_bits_of_values():
     y = aep.dequantize_mx4(codes, scale, k)
     one = aep.dequantize_mx4(want_c, want_s, k)
     assert bool((y[:-1] == one).all()) and bool((y[-1] == -one).all())
+
+
+def test_a_number_of_columns_in_a_tensor_counts_by_its_value():
+    x = torch.randn(3, 40, generator=torch.Generator().manual_seed(3)).cuda()
+    codes, scale = aep.quantize_mx4(x)
+    want = aep.dequantize_mx4(codes, scale, 40)
+    k = torch.tensor(40)
+    assert torch.equal(aep.dequantize_mx4(codes, scale, k), want)
+    k.fill_(39)
+    assert torch.equal(aep.dequantize_mx4(codes, scale, k), want[:, :39])
+    k.fill_(400)
+    for bad in (k, 40.0, 1 << 40, 0):
+        for _ in range(2):
+            with pytest.raises((TypeError, ValueError, aep.AEPError)):
+                aep.dequantize_mx4(codes, scale, bad)
