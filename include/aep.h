@@ -618,7 +618,7 @@ typedef struct {
   int32_t window;           /* 0: none                                              */
   int32_t max_rows;         /* with rows: no sequence has more of them (0: not      */
                             /* known), which may save launches; not looked at else  */
-  float scale;              /* finite, > 0                                          */
+  float scale;              /* > 0, at most 2^127                                   */
   int64_t q_row, q_head;    /* elements from one row, or head, to the next, >= 0    */
   int64_t out_row, out_head; /* the same of out, whose heads must not overlap       */
 } aep_attend4_desc;

@@ -2,7 +2,6 @@
 // weights, the cache of keys and values and the attention over it.
 #include <algorithm>
 #include <climits>
-#include <cmath>
 
 #include "cache4.h"
 #include "linear4.h"
@@ -123,7 +122,7 @@ aep_status check_attend(const aep_cache4* c, const aep_cache4_seqs* s, const aep
   if (const aep_status st = check_cache(c); st != AEP_OK) return st;
   if (const aep_status st = check_seqs(*c, s); st != AEP_OK) return st;
   if (!a || a->n_heads < 1 || a->n_heads % c->n_heads || a->window < 0 || a->max_rows < 0) return AEP_ERR_INVALID_ARG;
-  if (!std::isfinite(a->scale) || !(a->scale > 0.f)) return AEP_ERR_INVALID_ARG;
+  if (!(a->scale > 0.f) || !(a->scale <= 0x1p127f)) return AEP_ERR_INVALID_ARG;  // (times log2 e it is finite)
   const int64_t most = (int64_t)1 << 40;
   if (a->q_row < 0 || a->q_head < 0 || a->out_row < 0 || a->out_head < 0) return AEP_ERR_INVALID_ARG;
   if (a->q_row > most || a->q_head > most || a->out_row > most || a->out_head > most) return AEP_ERR_UNSUPPORTED;

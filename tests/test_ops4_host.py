@@ -156,7 +156,7 @@ def test_sequences(kw, status):
 
 @pytest.mark.parametrize("kw,status", [
     (dict(n_heads=0), 1), (dict(n_heads=7), 1), (dict(window=-1), 1), (dict(max_rows=-1), 1), (dict(scale=0.0), 1), (dict(scale=-1.0), 1),
-    (dict(scale=float("nan")), 1), (dict(scale=float("inf")), 1), (dict(q_row=-1), 1), (dict(q_head=-1), 1), (dict(out_row=-1), 1),
+    (dict(scale=float("nan")), 1), (dict(scale=float("inf")), 1), (dict(scale=3e38), 1), (dict(q_row=-1), 1), (dict(q_head=-1), 1), (dict(out_row=-1), 1),
     (dict(out_head=-1), 1), (dict(out_head=127), 1), (dict(out_row=1023), 1), (dict(out_row=0), 1), (dict(q_row=1 << 41), 6),
     (dict(out_row=1 << 41), 6)])
 def test_attention_descriptions(kw, status):
