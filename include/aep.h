@@ -578,8 +578,10 @@ typedef struct {
  * to what there is, so that accesses stay in bounds, and sets *flag to 1 (flag may
  * be NULL; it is never cleared): rows that descend or lie outside 0 .. total, and
  * of what the call's rows need, a page outside the cache, or a length below 0 or
- * beyond max_pages.  What such a sequence's rows get is not defined, and with rows
- * that descend what any row gets. */
+ * beyond max_pages.  What such a sequence's rows get from a read or the attention is
+ * not defined, and with rows that descend what any row gets.  An append writes into no
+ * place but the row's own: it leaves out the tokens whose page is outside the cache or
+ * beyond max_pages, and all of a sequence whose rows are out of order or range. */
 typedef struct {
   const int32_t* pages;  /* [batch][max_pages], rows ld_pages apart                */
   const int32_t* lens;   /* [batch]                                                */

@@ -35,21 +35,26 @@ struct Cache4Seqs {
 // What the device reads is held to what the buffers have; what had to be is reported.
 struct SeqRows {
   int row0, n, len;
+  int more;    // tokens behind the last page, which len is without
+  bool given;  // the rows are as they were given
 };
 __device__ __forceinline__ SeqRows seq_rows(const Cache4Seqs& q, int log_page, int b) {
   SeqRows s;
+  s.given = true;
   if (q.rows) {
     const int a = q.rows[b], e = q.rows[b + 1];
     s.row0 = min(max(a, 0), q.total);
     const int last = min(max(e, s.row0), q.total);
     s.n = last - s.row0;
-    if (q.flag && (a != s.row0 || e != last)) *q.flag = 1;
+    s.given = a == s.row0 && e == last;
+    if (q.flag && !s.given) *q.flag = 1;
   } else {
     s.row0 = b * q.n;
     s.n = q.n;
   }
   const int l = q.lens[b];
   s.len = (int)min((int64_t)max(l, 0), (int64_t)q.max_pages << log_page);
+  s.more = max(l, 0) - s.len;
   if (q.flag && l != s.len) *q.flag = 1;
   return s;
 }
@@ -57,9 +62,6 @@ __device__ __forceinline__ int page_in(const Cache4Seqs& q, int n_pages, int p) 
   const int in = min(max(p, 0), n_pages - 1);
   if (q.flag && p != in) *q.flag = 1;
   return in;
-}
-__device__ __forceinline__ int seq_page(const Cache4Seqs& q, int n_pages, int b, int i) {
-  return page_in(q, n_pages, q.pages[b * q.ld_pages + i]);
 }
 // The same entry of a wave, not held to bounds yet: through the scalar cache, so that whoever waits
 // for it does not wait for the vector loads in flight.

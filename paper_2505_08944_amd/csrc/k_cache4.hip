@@ -63,10 +63,21 @@ __global__ __launch_bounds__(256) void cache4_rows_kernel(const Cache4 c, const 
   const int b = seq_of_row(q, t0, r, lane);
   if (t >= q.total || b >= q.batch) return;  // behind the last sequence
   const SeqRows s = seq_rows(q, c.log_page, b);
-  const int pos = s.len - s.n + t - s.row0;
   if (t < s.row0 || t - s.row0 >= s.n) return;
-  if (!READ && pos < 0) return;  // no token of the sequence
-  const int page = pos < 0 ? 0 : seq_page(q, c.n_pages, b, pos >> c.log_page), at = pos & ((1 << c.log_page) - 1);
+  int pos = s.len - s.n + t - s.row0;
+  if constexpr (!READ) {
+    // What has no place is left out: held to bounds, it would take another token's.  (No token of the sequence; rows
+    // that are not all there; a token behind the last page.)
+    pos += s.more;
+    if (pos < 0 || !s.given || pos >> c.log_page >= q.max_pages) return;
+  }
+  int page = 0;
+  if (pos >= 0) {
+    const int p = q.pages[b * q.ld_pages + (pos >> c.log_page)];
+    page = page_in(q, c.n_pages, p);
+    if (!READ && p != page) return;
+  }
+  const int at = pos & ((1 << c.log_page) - 1);
   const int place = cache4_place(at & 31);
 
   // of each block, where this lane's codes are, and the scale

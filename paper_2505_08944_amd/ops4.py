@@ -287,7 +287,8 @@ class Cache4(_Fixed):
     def append(self, k: torch.Tensor, v: torch.Tensor, pages: torch.Tensor, lens: torch.Tensor,
                rows: Optional[torch.Tensor] = None, *, flag: Optional[torch.Tensor] = None) -> None:
         """Quantise rows of keys and values [T, n_heads, head_dim] bfloat16 into the
-        cache (``aep_cache4_append``).  Rows and heads may be strided."""
+        cache (``aep_cache4_append``).  Rows and heads may be strided.  A row whose token
+        has no page in the table, or one outside the cache, is left out."""
         dev = self.device
         if dev.index != L.current_device():
             with torch.cuda.device(dev):

@@ -211,3 +211,76 @@ def test_a_number_of_rows_in_a_tensor_counts_by_its_value():
         for _ in range(2):
             with pytest.raises((TypeError, ValueError, aep.AEPError)):
                 cache.read(pages, lens, bad)
+
+
+# sequences' pages (of 32 tokens, 4 in the cache), lens and rows of 8 rows; what of it has a place: (sequence, its
+# pages, len, first row, rows) of calls that have nothing out of range
+PLACES = [
+    ([[0, -1], [2, 3]], (40, 3), None, [(1, [2, 3], 3, 4, 4)]),
+    ([[0, 4], [2, 3]], (40, 36), None, [(1, [2, 3], 36, 4, 4)]),
+    ([[1, 2 ** 31 - 1], [-2 ** 31, 3]], (34, 36), None, [(0, [1, 0], 32, 0, 2), (1, [0, 3], 36, 4, 4)]),
+    ([[-1, 1], [99, -1]], (34, 1), None, [(0, [0, 1], 34, 2, 2)]),
+    ([[0, 1], [2, 3]], (65, 3), None, [(0, [0, 1], 64, 0, 3), (1, [2, 3], 3, 4, 4)]),
+    ([[0, 1], [2, 3]], (2 ** 31 - 1, 67), None, [(1, [2, 3], 64, 4, 1)]),
+    ([[0, 1], [2, 3]], (-4, 68), None, []),
+    ([[0, 1], [2, 3]], (40, 20), (0, 4, 20), [(0, [0, 1], 40, 0, 4)]),
+    ([[0, 1], [2, 3]], (40, 20), (-3, 4, 8), [(1, [2, 3], 20, 4, 4)]),
+    ([[0, 1], [2, 3]], (40, 20), (0, 3, 9), [(0, [0, 1], 40, 0, 3)]),
+]
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("i", range(len(PLACES)))
+def test_rows_without_a_place_are_left_out(i, D):
+    """A page outside the cache, a token behind the last page, rows that are not there: nothing is written for them,
+    into nobody's place; what has a place is written to it."""
+    log(f"cache4 places {i} d {D}")
+    pages, lens, rows, right = PLACES[i]
+    H = 2
+    k, v = rows_of(8, H, D, 7), rows_of(8, H, D, 8)
+    cache, want, flag = aep.Cache4(4, H, D, page_size=32), aep.Cache4(4, H, D, page_size=32), i32(0)
+    cache.data.random_(0, 256, generator=torch.Generator(device="cuda").manual_seed(i))
+    want.data.copy_(cache.data)
+    for _, p, l, at, n in right:
+        want.append(k[at:at + n], v[at:at + n], i32(*p).view(1, 2), i32(l))
+    t, r = i32(*pages[0], *pages[1]).view(2, 2), None if rows is None else i32(*rows)
+    cache.append(k, v, t, i32(*lens), r, flag=flag)
+    assert int(flag) == 1
+    assert torch.equal(cache.data, want.data)
+    cache.append(k, v, t, i32(*lens), r)  # (reported to nobody)
+    assert torch.equal(cache.data, want.data)
+
+
+def test_a_captured_step_grows_past_its_pages():
+    """A step captured once: a slot without a sequence, and a sequence that has no page yet for its next token, leave all
+    others' tokens as they are, until they have a page."""
+    H, D, page = 2, 128, 32
+    cache, flag = aep.Cache4(3, H, D, page_size=page), i32(0)
+    pages, lens = i32(0, 2, 1, -1, -1, -1).view(3, 2), i32(62, 30, -1)
+    k, v = rows_of(3, H, D, 20), rows_of(3, H, D, 21)
+    old_k, old_v = rows_of(62, H, D, 22), rows_of(62, H, D, 23)
+    cache.append(old_k, old_v, pages[:1], lens[:1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lens.add_(1)
+        cache.append(k, v, pages, lens, flag=flag)
+    for step, now in enumerate(((63, 31, 0), (64, 32, 1))):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert lens.tolist() == list(now) and int(flag) == step
+    flag.zero_()
+    lens[0] = 0  # (a sequence that is full: taken out)
+    before = cache.data.clone()
+    pages[0].fill_(-1)
+    lens[0] = -1
+    graph.replay()  # the second one's token 33 has no page
+    torch.cuda.synchronize()
+    assert lens.tolist() == [0, 33, 2] and int(flag) == 1 and torch.equal(cache.data, before)
+    rk, rv = cache.read(i32(0, 2).view(1, 2), i32(62), 62)
+    assert equal(rk, kept(old_k)) and equal(rv, kept(old_v))
+    pages[1, 1] = 2
+    lens[1] = 32
+    graph.replay()
+    torch.cuda.synchronize()
+    rk, rv = cache.read(pages[1:2], lens[1:2], 1)
+    assert equal(rk, kept(k[1:2])) and equal(rv, kept(v[1:2]))
