@@ -613,7 +613,8 @@ aep_status aep_cache4_read(const aep_cache4* c, const void* mem, const aep_cache
  * these the last `window`.  Head j reads head j / (n_heads / the cache's
  * n_heads) of the cache.  lse = log sum_t exp(scale q . k_t).  A row without a
  * token has out = 0 and lse = -infinity.  Tokens that a row does not see do not
- * count for it, whatever their places hold.  Sums are f32; the p_t of a sum are
+ * count for it, whatever their places hold.  Sums and scores are f32 (out is NaN where
+ * the largest q . k, or scale q . k log2 e, is beyond it, 2^128); the p_t of a sum are
  * rounded to bf16 relative to one reference each, the same in both sums. */
 typedef struct {
   int32_t n_heads;          /* of queries: a multiple of the cache's                */

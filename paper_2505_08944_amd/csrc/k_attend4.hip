@@ -296,8 +296,24 @@ __device__ __forceinline__ void hide_tokens(f32x4_t (&sc)[2][NC], int t0, const 
   }
 }
 
-// A column's weights of 32 tokens, eight in a lane, to bf16.
-__device__ __forceinline__ uint4 weights(const f32x4_t s0, const f32x4_t s1, float scale, float off) {
+// From this size on (powers of two) a reference is `far`: it is a column's largest score as rounded to f32, and the
+// exact product is off that by up to half a step of the score: 2^8 at 2^32, where a weight or its sum would overflow,
+// or all weights underflow.  Below it that half step is at most 0.5, and the 6 ahead are not lost.
+constexpr float kFar = 0x1p24f;
+
+// A column's weights of 32 tokens, eight in a lane, to bf16.  far: whether the wave has a column with a far reference;
+// such a column's scores are rounded as the reference was, so that the largest one's exponent is 0 to -8.
+__device__ __forceinline__ uint4 weights(const f32x4_t s0, const f32x4_t s1, float scale, float off, bool far) {
+  if (__builtin_expect(far, 0)) {
+    const bool mine = fabsf(off) >= kFar;
+    const auto power = [&](float x) {
+#pragma clang fp contract(off)
+      const float score = x * scale;
+      return __builtin_amdgcn_exp2f(mine ? score + off : __builtin_fmaf(x, scale, off));
+    };
+    return make_uint4(bf16_pair(power(s0[0]), power(s0[1])), bf16_pair(power(s0[2]), power(s0[3])),
+                      bf16_pair(power(s1[0]), power(s1[1])), bf16_pair(power(s1[2]), power(s1[3])));
+  }
   const auto pair = [&](float x, float y) {
     return bf16_pair(__builtin_amdgcn_exp2f(__builtin_fmaf(x, scale, off)), __builtin_amdgcn_exp2f(__builtin_fmaf(y, scale, off)));
   };
@@ -309,11 +325,12 @@ __device__ __forceinline__ bool behind(const uint4 p, float m) {
   return __ballot(((p.x | p.y | p.z | p.w) & 0x40004000u) != 0 || m == kNegInf) != 0;
 }
 // The reference that a column gets then, with the factor for what was summed up under the old one.
-__device__ __forceinline__ float raise(const f32x4_t s0, const f32x4_t s1, float scale, float& m, float& off) {
+__device__ __forceinline__ float raise(const f32x4_t s0, const f32x4_t s1, float scale, float& m, float& off, bool& far) {
   const float big = scale * fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
   const float now = fmaxf(m, max_of_columns(big) + kAhead), shrink = now == m ? 1.f : __builtin_amdgcn_exp2f(m - now);
   m = now;
   off = now == kNegInf ? 0.f : -now;
+  far |= __ballot(fabsf(off) >= kFar) != 0;
   return shrink;
 }
 
@@ -396,6 +413,7 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
     }
     f32x4_t o[NC][NT], sum[NC];
     float m[NC], off[NC];
+    bool far = false;  // a column of the wave has a far reference
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
 #pragma unroll
@@ -464,13 +482,13 @@ __global__ __launch_bounds__(256, attend_per_cu(D, NC)) void attend4_kernel(cons
       bf16x8_t p[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        uint4 pw = weights(sc[0][c], sc[1][c], a.scale, off[c]);
+        uint4 pw = weights(sc[0][c], sc[1][c], a.scale, off[c], far);
         if (behind(pw, m[c])) {
-          const float shrink = raise(sc[0][c], sc[1][c], a.scale, m[c], off[c]);
+          const float shrink = raise(sc[0][c], sc[1][c], a.scale, m[c], off[c], far);
           sum[c] *= shrink;
 #pragma unroll
           for (int n = 0; n < NT; ++n) o[c][n] *= shrink;
-          pw = weights(sc[0][c], sc[1][c], a.scale, off[c]);
+          pw = weights(sc[0][c], sc[1][c], a.scale, off[c], far);
         }
         p[c] = __builtin_bit_cast(bf16x8_t, pw);
         sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[c], sum[c], 0, 0, 0);
@@ -598,6 +616,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
     }
     f32x4_t o[NC][NT], sum[NC];
     float m[NC], off[NC];
+    bool far = false;  // a column of the wave has a far reference
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
 #pragma unroll
@@ -708,13 +727,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
           bf16x8_t p[NC];
 #pragma unroll
           for (int c = 0; c < NC; ++c) {
-            uint4 pw = weights(sc[0][c], sc[1][c], a.scale, off[c]);
+            uint4 pw = weights(sc[0][c], sc[1][c], a.scale, off[c], far);
             if (behind(pw, m[c])) {
-              const float shrink = raise(sc[0][c], sc[1][c], a.scale, m[c], off[c]);
+              const float shrink = raise(sc[0][c], sc[1][c], a.scale, m[c], off[c], far);
               sum[c] *= shrink;
 #pragma unroll
               for (int n = 0; n < NT; ++n) o[c][n] *= shrink;
-              pw = weights(sc[0][c], sc[1][c], a.scale, off[c]);
+              pw = weights(sc[0][c], sc[1][c], a.scale, off[c], far);
             }
             p[c] = __builtin_bit_cast(bf16x8_t, pw);
             sum[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[c], sum[c], 0, 0, 0);
