@@ -630,6 +630,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
     int st = (q.first + start) * 2, st_end = min((q.first + end) * 2, (pos1 + 64) >> 6);
     if (a.window) st = max(st, max(0, pos0 - a.window + 1) >> 6);
     const int st0 = st, last_block = (q.s.len - 1) >> 5;
+    // The first block that a column sees.  (The first step's other half lies before a window then and may have no page:
+    // page 0 stands for it, and no column takes what is there.)
+    const auto first_block = [&] { return max(st0 * 2, a.window ? max(0, pos0 - a.window + 1) >> 5 : 0); };
     const int pages32 = a.c.log_page - 5, in_page = (1 << pages32) - 1;
     const auto block_of = [&](int at) { return min(at * 2 + (wave >> 1), last_block); };  // this wave's half of a step
     // (a page is asked for a step ahead of its use, and held to bounds there)
@@ -669,7 +672,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
     __syncthreads();  // (the tile before has been read)
     if (tid == 0) any_lost = 0;
     if (st < st_end) {
-      load(st, page_of(st));
+      const int page = page_of(st);
+      load(st, block_of(st) < first_block() ? 0 : page);
       int next = st + 1 < st_end ? page_of(st + 1) : 0;
       __syncthreads();
       widen(smem, st);
@@ -750,7 +754,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend4_wide_kernel(con
       if (any_lost) {
         for (int at = st0 * 2; at < st_end * 2 && at <= last_block; ++at)
           if (at_edge(at >> 1)) {
-            load_values<D>(x, a.c, head_of(seq_page_raw(a.s, b, at >> pages32)), at & in_page, l, g);
+            load_values<D>(x, a.c, head_of(at < first_block() ? 0 : seq_page_raw(a.s, b, at >> pages32)), at & in_page, l, g);
             mark_lost<NC, NT>(o, x.vs, at * 32 + g * 4, pos, a.window);
           }
       }

@@ -391,3 +391,20 @@ def test_numbers_in_tensors_count_by_their_value():
         for _ in range(2):
             with pytest.raises((TypeError, ValueError, aep.AEPError)):
                 c.attend(**kw)
+
+
+@pytest.mark.parametrize("n,group,D", [(70, 2, 128), (130, 1, 64), (33, 4, 256), (9, 2, 128), (1, 4, 64)])
+def test_pages_before_the_window_may_be_gone(n, group, D):
+    """Entries of pages that lie wholly before every row's window are out of range: nothing of them is needed, or reported."""
+    c = Case([1000, 600], n, 2, group, D, page=32, seed=24)
+    for window in (1, 16, 31, 32, 33, 50, 64, 65, 96, 97):
+        log(f"attend4 window {window} of {n} x {group} d {D}")
+        pages = c.pages.clone()
+        for b, l in enumerate(c.lens):
+            c.pages[b, :max(0, l - n - window + 1) // 32] = -7
+        for many in (False, True):
+            flag, lse = i32(0), torch.empty(c.q.shape[:2], device="cuda")
+            out = c.attend(many, window=window, flag=flag, lse=lse)
+            c.check(out, lse, window, what=(window, many), rows={0, 1, 31, 32, 63, 64, 65, -1})
+            assert int(flag) == 0, (window, many)
+        c.pages.copy_(pages)
