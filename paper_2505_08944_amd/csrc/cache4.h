@@ -55,7 +55,7 @@ __device__ __forceinline__ SeqRows seq_rows(const Cache4Seqs& q, int log_page, i
   const int l = q.lens[b];
   s.len = (int)min((int64_t)max(l, 0), (int64_t)q.max_pages << log_page);
   s.more = max(l, 0) - s.len;
-  if (q.flag && l != s.len) *q.flag = 1;
+  if (q.flag && l != s.len && s.n) *q.flag = 1;  // (without rows, nothing needs it)
   return s;
 }
 __device__ __forceinline__ int page_in(const Cache4Seqs& q, int n_pages, int p) {

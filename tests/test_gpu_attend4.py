@@ -408,3 +408,15 @@ def test_pages_before_the_window_may_be_gone(n, group, D):
             c.check(out, lse, window, what=(window, many), rows={0, 1, 31, 32, 63, 64, 65, -1})
             assert int(flag) == 0, (window, many)
         c.pages.copy_(pages)
+
+
+def test_lengths_of_sequences_without_rows_do_not_count():
+    c = Case([300, 70], [2, 70], 2, 4, 64, seed=25)
+    pages = torch.nn.functional.pad(c.pages, (0, 0, 1, 1), value=-7)
+    for many in (False, True):
+        want, flag = c.attend(many), i32(0)
+        need = 8 * 512 * 128 // (2 * 2) // 64 + 1 if many else 0
+        t = torch.nn.functional.pad(pages, (0, max(0, need - pages.shape[1])), value=-7)
+        for lens in ((-5, 2 ** 31 - 1), (2 ** 31 - 1, -2 ** 31)):
+            got = c.cache.attend(c.q, t, i32(lens[0], 300, 70, lens[1]), i32(0, 0, 2, 72, 72), flag=flag)
+            assert torch.equal(got, want) and int(flag) == 0, (many, lens)

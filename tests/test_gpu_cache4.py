@@ -284,3 +284,13 @@ def test_a_captured_step_grows_past_its_pages():
     torch.cuda.synchronize()
     rk, rv = cache.read(pages[1:2], lens[1:2], 1)
     assert equal(rk, kept(k[1:2])) and equal(rv, kept(v[1:2]))
+
+
+def test_lengths_of_sequences_without_rows_do_not_count():
+    H, D = 2, 64
+    cache, flag = aep.Cache4(2, H, D, page_size=32), i32(0)
+    pages, lens, rows = i32(0, 7, 1).view(3, 1), i32(-5, 2 ** 31 - 1, 20), i32(0, 0, 0, 4)
+    k, v = rows_of(4, H, D, 24), rows_of(4, H, D, 25)
+    cache.append(k, v, pages, lens, rows, flag=flag)
+    rk, rv = cache.read(pages, lens, 4, rows, flag=flag)
+    assert equal(rk, kept(k)) and equal(rv, kept(v)) and int(flag) == 0
