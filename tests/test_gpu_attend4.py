@@ -420,3 +420,19 @@ def test_lengths_of_sequences_without_rows_do_not_count():
         for lens in ((-5, 2 ** 31 - 1), (2 ** 31 - 1, -2 ** 31)):
             got = c.cache.attend(c.q, t, i32(lens[0], 300, 70, lens[1]), i32(0, 0, 2, 72, 72), flag=flag)
             assert torch.equal(got, want) and int(flag) == 0, (many, lens)
+
+
+def test_rows_of_no_sequence_are_zeros_without_out():
+    """New tensors hold nothing that was in their memory before."""
+    c = Case([300, 20], [2, 3], 2, 4, 128, seed=26)
+    want = c.attend()
+    q = torch.cat([c.q, c.q])
+    for rows, own, none in ((c.rows, slice(0, 5), slice(5, 10)), (c.rows + 3, slice(3, 8), [0, 1, 2, 8, 9])):
+        x = torch.zeros_like(q)
+        x[own] = c.q
+        for _ in range(3):
+            junk = [torch.full_like(q, float("nan")) for _ in range(4)]
+            torch.cuda.synchronize()
+            del junk  # (whose memory a new tensor of its size gets)
+            out = c.cache.attend(x, c.pages, c.dev_lens, rows)
+            assert torch.equal(out[own], want) and bool((out[none] == 0).all())

@@ -294,3 +294,19 @@ def test_lengths_of_sequences_without_rows_do_not_count():
     cache.append(k, v, pages, lens, rows, flag=flag)
     rk, rv = cache.read(pages, lens, 4, rows, flag=flag)
     assert equal(rk, kept(k)) and equal(rv, kept(v)) and int(flag) == 0
+
+
+def test_rows_of_no_sequence_read_as_zeros_where_there_is_no_tensor_for_them():
+    H, D = 2, 128
+    cache = aep.Cache4(2, H, D, page_size=32)
+    k, v = rows_of(9, H, D, 26), rows_of(9, H, D, 27)
+    pages, lens, rows = i32(1, 0).view(2, 1), i32(20, 4), i32(2, 4, 6)
+    cache.append(k, v, pages, lens, rows)
+    for _ in range(3):
+        junk = [torch.full_like(k, float("nan")) for _ in range(4)]
+        torch.cuda.synchronize()
+        del junk  # (whose memory a new tensor of its size gets)
+        for got, x in zip(cache.read(pages, lens, 9, rows), (k, v)):
+            want = kept(x)
+            want[:2], want[6:] = 0.0, 0.0
+            assert equal(got, want)
