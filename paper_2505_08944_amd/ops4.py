@@ -17,8 +17,9 @@ import torch
 from . import _lib as L
 from .ops import _CODE, _FN, _Fixed, _int32, _ld, _rows, arg32
 
-_BYTE = (torch.uint8, torch.float4_e2m1fn_x2, torch.float8_e8m0fnu)
-_F32_BF16 = (torch.float32, torch.bfloat16)
+# (torch's own types for these bytes are newer than all else that the package needs of it)
+_CODES = (torch.uint8, getattr(torch, "float4_e2m1fn_x2", torch.uint8))
+_SCALES = (torch.uint8, getattr(torch, "float8_e8m0fnu", torch.uint8))
 
 
 def _bytes_matrix(t, name, dtypes, shape, dev) -> None:
@@ -85,8 +86,8 @@ def dequantize_mx4(codes: torch.Tensor, scale: torch.Tensor, k: int, *, dtype: t
     def check():
         if arg32(k, "k", "aep_mx4_dequantize") < 1:
             raise ValueError(f"k is {k}")
-        _bytes_matrix(codes, "codes", _BYTE[:2], (None, (k + 1) // 2), dev)
-        _bytes_matrix(scale, "scale", (_BYTE[0], _BYTE[2]), (codes.shape[0], (k + 31) // 32), dev)
+        _bytes_matrix(codes, "codes", _CODES, (None, (k + 1) // 2), dev)
+        _bytes_matrix(scale, "scale", _SCALES, (codes.shape[0], (k + 31) // 32), dev)
         if dtype not in _F32_BF16:
             raise ValueError(f"dtype {dtype}, expected torch.bfloat16 or torch.float32")
         if out is not None:
@@ -124,13 +125,13 @@ class Linear4(_Fixed):
         if not isinstance(codes, torch.Tensor) or not codes.is_cuda:
             raise ValueError("codes must be a CUDA (HIP) tensor")
         dev = codes.device
-        _bytes_matrix(codes, "codes", _BYTE[:2], (None, None), dev)
+        _bytes_matrix(codes, "codes", _CODES, (None, None), dev)
         n, half = codes.shape
         k = 2 * half if k is None else arg32(k, "k", "aep_linear4")
         if n < 1 or k < 1 or half != (k + 1) // 2:
             raise ValueError(f"codes have shape {tuple(codes.shape)}, expected [n, {(k + 1) // 2}] for k = {k}")
         _int32(max(n, k), 1 << 30, "channels", "aep_linear4")
-        _bytes_matrix(scale, "scale", (_BYTE[0], _BYTE[2]), (n, (k + 31) // 32), dev)
+        _bytes_matrix(scale, "scale", _SCALES, (n, (k + 31) // 32), dev)
         if bias is not None:
             _rows(bias, "bias", _F32_BF16, (n,), dev)
         if activation not in _FN:
