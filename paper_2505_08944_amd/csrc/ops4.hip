@@ -110,10 +110,11 @@ Cache4Seqs seqs_of(const aep_cache4_seqs& s) {
   return o;
 }
 
-// Rows of heads of d values that do not overlap, whichever of the two goes first.
+// Rows of heads of d values that do not overlap, whichever of the two goes first.  (Counts below 2^31 and distances up to
+// 2^40: their products are more than 64 bits hold.)
 bool apart(int64_t rows, int64_t row, int64_t heads, int64_t head, int64_t d) {
   const auto fits = [&](int64_t n1, int64_t s1, int64_t n2, int64_t s2) {
-    return (n1 < 2 || s1 >= d) && (n2 < 2 || s2 >= (n1 < 2 ? 0 : (n1 - 1) * s1) + d);
+    return (n1 < 2 || s1 >= d) && (n2 < 2 || s2 >= (n1 < 2 ? 0 : (__int128)(n1 - 1) * s1) + d);
   };
   return fits(heads, head, rows, row) || fits(rows, row, heads, head);
 }
