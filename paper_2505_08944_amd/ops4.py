@@ -20,6 +20,7 @@ from .ops import _CODE, _FN, _Fixed, _int32, _ld, _rows, arg32
 # (torch's own types for these bytes are newer than all else that the package needs of it)
 _CODES = (torch.uint8, getattr(torch, "float4_e2m1fn_x2", torch.uint8))
 _SCALES = (torch.uint8, getattr(torch, "float8_e8m0fnu", torch.uint8))
+_F32_BF16 = (torch.float32, torch.bfloat16)
 
 
 def _bytes_matrix(t, name, dtypes, shape, dev) -> None:
