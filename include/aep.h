@@ -509,7 +509,9 @@ aep_status aep_linear(const aep_linear_desc* l, const void* x, const void* w, co
  * held as a byte (2^(byte - 127); 255: NaN); a value is a code of 4 bits, sign
  * and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 .. 7; + 8: negative).  Two
  * codes to a byte, the earlier value in its low half.  Every value is a bf16
- * value.  Quantising: a block's power is the smallest, from 2^-126 to 2^125, at
+ * value, but for those of 2^128 and more, which become infinity (4 and 6 times
+ * 2^126, byte 253; 2, 3, 4 and 6 times 2^127, byte 254; the quantiser's bytes end
+ * at 252).  Quantising: a block's power is the smallest, from 2^-126 to 2^125, at
  * which its largest magnitude is at most 7 times it (2^0 for zeros); a value goes
  * to the nearest code, in the middle to the even one, above 6 to 6.  A block with
  * a NaN or an infinity gets the byte 255: all of it reads back as NaN.
@@ -522,7 +524,8 @@ aep_status aep_linear(const aep_linear_desc* l, const void* x, const void* w, co
  * of an odd k the last half byte is 0).  rows == 0 is a no-op. */
 aep_status aep_mx4_quantize(const void* x, int32_t x_dtype, int64_t ldx, int64_t rows, int32_t k, void* codes,
                             void* scale, void* stream);
-/* And back, exactly, to y [rows][k] F32 or BF16 of row stride ldy. */
+/* And back, exactly (2^128 and more: infinity), to y [rows][k] F32 or BF16 of row
+ * stride ldy. */
 aep_status aep_mx4_dequantize(const void* codes, const void* scale, int64_t rows, int32_t k, void* y, int32_t y_dtype,
                               int64_t ldy, void* stream);
 

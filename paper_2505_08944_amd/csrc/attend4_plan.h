@@ -30,6 +30,10 @@ struct Attend4Plan {
 // than 64, if its workgroups have 8 units each at least (its parts are four times as large).  us, the
 // kernel for many and tiles of 32, 4 heads of 128 in the cache, 32 sequences of up to 8192 tokens: 32 columns
 // 53 and 41, 64 61 and 65, 128 72 and 98, 256 113 and 169; 4 sequences: 64 35 and 28, 256 51 and 37.
+// The lengths lie on the device: max_len is what the table of pages has room for, and of a table that is wider than its
+// longest sequence the rule expects more units than there are.  us, a table of 8192 tokens (or 131072) and one as wide as
+// the sequences, 8 heads of 128: 4 x 64 rows of 1000 tokens 52 and 29, 32 x 32 of 300 37 and 28, 4 x 100 of 300 28 and
+// 26, 1 x 300 of 300 23 and 27, 8 x 600 of 600 77 and 77.
 // Sequences that differ in their rows are taken by both kinds, one after the other, unless none can have
 // many (64 of up to 8192 tokens, one with 512 rows, the others with one, 4 heads to one of the cache: 169;
 // by the one kind 196, by the other 241).

@@ -10,11 +10,11 @@
 // that weights sum to 1.  Scores, sums and references are f32.
 //
 // Few columns (attend4_kernel): a wave takes 32 tokens for a tile of 16 or 32 columns.
-// Bound by the cache's bytes: 64 sequences of up to 16384 tokens, 8 heads of 128, 101 us
-// of kernel for 507 MB (5.0 TB/s; a large copy 5.2); one sequence of 100003 tokens 25 us for 109 MB.
+// Bound by the cache's bytes: 64 sequences of up to 16384 tokens, 8 heads of 128, 104 us
+// of kernel for 507 MB (4.9 TB/s; a large copy 5.2); one sequence of 100003 tokens 24 us for 109 MB.
 // Many columns (attend4_wide_kernel): four waves with 32 columns each share what they
-// widen.  Bound by MFMAs and VALU, which do not run at once here even from two waves of a
-// SIMD (4 x 509 rows to up to 8192 tokens: 41% and 36% of the cycles): 176 us of kernel.
+// widen.  Of 4 x 509 rows to up to 8192 tokens (188 us with the join) MFMAs are busy in 37% of the SIMDs'
+// cycles and VALU in 40%, and waves wait for 25% of their time.
 //
 // The work is divided evenly: all units of 128 tokens of all tiles in a row, an equal share
 // for each workgroup.  Tiles that several workgroups share leave parts in the scratch, which a

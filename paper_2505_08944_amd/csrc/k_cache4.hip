@@ -1,6 +1,7 @@
 // Rows of keys and values into the pages of a cache in 4 bits, and back (cache4.h).
 // Bound by HBM where there are many rows, else by the latency of the loads: the
-// sequence's place, the page, the row.
+// sequence's place, the page, the row.  Where sequences differ in their rows, a row's one is found by a scan of the
+// ends before it, 64 per load: one row of each of 64 sequences 4.1 us, of 1024 9.5, of 4096 28.
 #include <algorithm>
 #include <climits>
 

@@ -178,14 +178,14 @@ __global__ __launch_bounds__(256) void linear4_pack_kernel(const uint8_t* __rest
   o[1024 + lane] = (uint8_t)s;
 }
 
-// Back to bf16 rows of k8 values (a multiple of 8, at most 128 steps).
+// Back to bf16 rows of k8 values (a multiple of 8, at most 128 times `steps`).
 __global__ __launch_bounds__(256) void linear4_unpack_kernel(const uint8_t* __restrict__ packed, int n, int k8, int steps,
                                                              int64_t pieces, uint16_t* __restrict__ out) {
   const int64_t piece = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (piece >= pieces) return;
   const int lane = threadIdx.x & 63;
   const uint8_t* p = packed + piece * kLinear4Piece;
-  // (a quad of lanes stores 256 consecutive bytes of a row: lane l has 8 bytes-quads l % 4 of them)
+  // (16 lanes store 256 consecutive bytes of a row: lane l has the 8 values from 8 (l % 16) on of row 4 i + l / 16)
   const int row0 = (int)(piece / steps) * 16, k0 = (int)(piece % steps) * 128;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {

@@ -2,8 +2,8 @@
 // two, held as its exponent + 127 in a byte; a value is a code of 4 bits, sign and
 // one of 0, 0.5, 1, 1.5, 2, 3, 4, 6, two codes to a byte, the earlier one in its
 // low half.  gfx950 converts both ways: checked on the card for all codes and all
-// scales, the values that come back are exact bf16 (0.5 2^-127 .. 6 2^127 but for
-// the overflow of the last), scale byte 255 gives NaN, and f32 values go to the
+// scales, the values that come back are exact bf16 from 0.5 2^-127 on (of 2^128 and more, under
+// the bytes 253 and 254, infinity), scale byte 255 gives NaN, and f32 values go to the
 // nearest code, in the middle to the even one, at most 6.
 #pragma once
 

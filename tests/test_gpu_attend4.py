@@ -436,3 +436,24 @@ def test_rows_of_no_sequence_are_zeros_without_out():
             del junk  # (whose memory a new tensor of its size gets)
             out = c.cache.attend(x, c.pages, c.dev_lens, rows)
             assert torch.equal(out[own], want) and bool((out[none] == 0).all())
+
+
+def test_rows_of_no_sequence_are_zeros_in_a_captured_call():
+    """A padded batch captured once: who has rows changes between replays, and the rows that had an owner before are zeros."""
+    c = Case([300, 20, 64], [2, 3, 1], 2, 4, 128, seed=27)
+    q, rows = torch.cat([c.q, c.q]), c.rows.clone()
+    ends = (c.rows, i32(0, 2, 2, 2), i32(0, 0, 3, 4), c.rows + 6, c.rows)
+    want = [c.cache.attend(q, c.pages, c.dev_lens, e) for e in ends]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = c.cache.attend(q, c.pages, c.dev_lens, rows)
+        k, v = c.cache.read(c.pages, c.dev_lens, 12, rows)
+    for e, w in zip(ends, want):
+        rows.copy_(e)
+        graph.replay()
+        torch.cuda.synchronize()
+        own = torch.zeros(12, dtype=torch.bool)
+        own[int(e[0]):int(e[-1])] = True
+        assert torch.equal(out, w) and bool((out[~own.cuda()] == 0).all())
+        assert bool((k[~own.cuda()] == 0).all()) and bool((v[~own.cuda()] == 0).all())
+        assert bool((k[own.cuda()] != 0).any(-1).all())
