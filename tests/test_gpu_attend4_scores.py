@@ -155,3 +155,23 @@ def test_large_scores_beside_small_ones(i):
         check(c, every, all_lse, scale, i)
         every[1::2], all_lse[1::2] = out[1::2], lse[1::2]
         check(c, every, all_lse, scale, i)
+
+
+@pytest.mark.parametrize("i", range(len(SHAPES)))
+def test_the_end_of_f32(i):
+    """Largest scores of about 2^127 in powers of two, the last that are f32; behind it NaN, for the columns that have such scores."""
+    *shape, many = SHAPES[i]
+    c = Case(*shape, seed=120 + i)
+    lse = torch.empty(c.q.shape[:2], device="cuda")
+    scale = float(np.float32(2.0 ** 127 / (6.0 * c.D * 1.4427)))
+    for negative in (False, True):
+        log(f"attend4 scores of 2^127 shape {i} negative {negative}")
+        fill(c, i, negative, False)
+        c.write()
+        out = c.attend(many, scale=scale, lse=lse)
+        check(c, out, lse, scale, (i, negative))
+    fill(c, i, False, False)
+    c.write()
+    c.q[-1, -1] *= 16.0
+    last = c.attend(many, scale=scale)
+    assert bool(torch.isnan(last[-1, -1]).all()) and int(torch.isnan(last).sum()) == c.D
